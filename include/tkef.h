@@ -404,6 +404,153 @@ int tkef_lars_rates_execute(tkef_update_plan plan, double gamma, double eta, dou
  * (i = 0..3), 1 for tkef_lars_rates_execute (i = 0..1); NULL otherwise. */
 const char *tkef_lars_launch_name(int32_t dense, int32_t i);
 
+/* ========================================================================
+ * Rows of logits over a vocabulary: a teacher's top logits as (idx, val)
+ * lists, distillation on such lists, verification of drafted tokens
+ *
+ * A row is V consecutive logits x_0 .. x_{V-1} of one type (TKEF_DTYPE_*);
+ * rows lie row_stride elements apart (row_stride >= V; what lies between
+ * them is neither read nor written). s = 1 / temperature. Sums, maxima and
+ * probabilities are held in binary32 whatever the logits' type; log is the
+ * natural logarithm. -inf is a masked word (probability 0).
+ *
+ * The plans below hold sizes only: no buffer is bound, and a call may give
+ * fewer rows than the plan was created for (0 rows: nothing is launched).
+ * Executions are asynchronous, only launch kernels and can be captured into a
+ * graph. Limits: rows, V <= 2^20; k <= min(V, 1024); 1 <= draft <= 63;
+ * 1e-6 <= temperature <= 1e6 (TKEF_ERANGE otherwise).
+ * ====================================================================== */
+
+#define TKEF_DTYPE_F32 0  /* binary32 */
+#define TKEF_DTYPE_F16 1  /* binary16 */
+#define TKEF_DTYPE_BF16 2 /* bfloat16 */
+
+#define TKEF_ROWS_MAX_ROWS (1 << 20)
+#define TKEF_ROWS_MAX_VOCAB (1 << 20)
+#define TKEF_ROWS_MAX_K 1024
+#define TKEF_VERIFY_MAX_DRAFT 63
+
+/* ---- top logits -----------------------------------------------------------
+ * For each row, with S = the k words first in the order (x descending, word
+ * ascending; -0 equals +0, infinities rank as IEEE values):
+ *   idx = S ascending (int32), val_j = x[idx_j] (binary32 exactly, or binary16
+ *   rounded to nearest even), tail = log sum_{i not in S} exp(s x_i)
+ * tail is -inf where nothing is left (k == V, or only masked words) and +inf
+ * where an unselected word is +inf. A NaN in a row sets TKEF_STATUS_NAN; that
+ * row's selection is then unspecified (ascending words within [0, V)) and its
+ * tail is NaN. */
+typedef struct tkef_top_plan_s *tkef_top_plan;
+
+/* Host only. rows: the most rows an execution gives. */
+int tkef_top_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dtype,
+                         int32_t val_format, double temperature, tkef_top_plan *plan_out);
+int tkef_top_plan_destroy(tkef_top_plan plan);
+int tkef_top_plan_info(tkef_top_plan plan, size_t *workspace_bytes);
+
+/* logits: device, `rows` rows. idx_out (int32), val_out (binary32 or binary16):
+ * device, rows * k entries; tail_out: device, rows binary32 values, or NULL. */
+int tkef_top_execute(tkef_top_plan plan, const void *logits, int64_t row_stride, int64_t rows,
+                     int32_t *idx_out, void *val_out, float *tail_out, void *ws,
+                     size_t ws_bytes, uint32_t *status, hipStream_t stream);
+
+/* ---- distillation on a teacher's top logits -------------------------------
+ * Row by row, for student logits z_0 .. z_{V-1} and a teacher's list of c <= k
+ * entries (word idx_j, logit t_j), strictly ascending, with the log-mass tau of
+ * the teacher's other words (tail_out above; -inf: they have none):
+ *   LT = log(sum_j exp(s t_j) + exp(tau)),  p_j = exp(s t_j - LT), p_r = exp(tau - LT)
+ *   LZ = log sum_i exp(s z_i),  q_i = exp(s z_i - LZ),  q_r = sum_{i not listed} q_i
+ *   loss = w temperature^2 [ sum_j p_j (log p_j - log q_{idx_j}) + p_r (log p_r - log q_r) ]
+ * (terms with p = 0 are 0), the Kullback-Leibler divergence over the listed
+ * words and all others as one class. Without tau the listed logits alone are
+ * the teacher's distribution: a list of one entry makes the loss a cross
+ * entropy. The gradient is
+ *   dloss/dz_i = w temperature (q_i - p_i)                for a listed word i
+ *              = w temperature q_i (1 - p_r / q_r)        for the others
+ * A row with w == 0 or c == 0 has loss 0 and gradient 0 whatever its logits
+ * (they are not read). A loss is +inf where p > 0 meets q = 0. NaN or +inf
+ * logits, a row whose logits are all -inf, and a list without mass make the
+ * row's loss and gradient NaN. An entry outside [0, V) or not above the entry
+ * before it is left out and sets TKEF_STATUS_INDEX_RANGE /
+ * TKEF_STATUS_UNSORTED; results of a row whose list names a word twice all the
+ * same are unspecified. */
+typedef struct tkef_distill_plan_s *tkef_distill_plan;
+
+/* Host only. k: entries reserved per row in idx and val; val_format: type of val. */
+int tkef_distill_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dtype,
+                             int32_t val_format, double temperature,
+                             tkef_distill_plan *plan_out);
+int tkef_distill_plan_destroy(tkef_distill_plan plan);
+int tkef_distill_plan_info(tkef_distill_plan plan, size_t *workspace_bytes);
+
+/* Loss of each row. logits: device, `rows` rows of the plan's type; idx, val:
+ * device, rows * k entries; tail (binary32), count (int32, clamped to [0, k])
+ * and weight (binary32): device, one per row, each may be NULL (no other mass;
+ * k entries; weight 1). loss: device, rows binary32 values. stats: device, rows
+ * * 4 binary32 values that the backward pass takes (16-byte aligned; the
+ * student's sums; their layout is the library's), or NULL. */
+int tkef_distill_forward(tkef_distill_plan plan, const void *logits, int64_t row_stride,
+                         int64_t rows, const int32_t *idx, const void *val, const float *tail,
+                         const int32_t *count, const float *weight, float *loss, float *stats,
+                         void *ws, size_t ws_bytes, uint32_t *status, hipStream_t stream);
+
+/* Gradient of sum_rows dloss * loss with respect to the logits, in the logits'
+ * type. dloss: device, one binary32 value per row, or NULL (1). The other
+ * inputs are those of the forward pass, stats what it gave. grad: device, rows
+ * grad_stride elements apart (grad_stride >= V); it may be the logits
+ * themselves (same address and stride), and must not overlap them otherwise. */
+int tkef_distill_backward(tkef_distill_plan plan, const void *logits, int64_t row_stride,
+                          int64_t rows, const int32_t *idx, const void *val, const float *tail,
+                          const int32_t *count, const float *weight, const float *stats,
+                          const float *dloss, void *grad, int64_t grad_stride, void *ws,
+                          size_t ws_bytes, uint32_t *status, hipStream_t stream);
+
+/* Loss and its gradient (dloss = 1) in one call. */
+int tkef_distill_step(tkef_distill_plan plan, const void *logits, int64_t row_stride,
+                      int64_t rows, const int32_t *idx, const void *val, const float *tail,
+                      const int32_t *count, const float *weight, float *loss, void *grad,
+                      int64_t grad_stride, void *ws, size_t ws_bytes, uint32_t *status,
+                      hipStream_t stream);
+
+/* ---- verification of drafted tokens ---------------------------------------
+ * For each of `batch` sequences, a draft model proposed tokens x_0 .. x_{m-1}
+ * (m <= draft) from q_i = softmax(s draft_i), and the target model gave logits
+ * at the m + 1 places: p_i = softmax(s target_i). With given uniform numbers
+ * u_i in [0, 1) and noise e_v > 0 drawn from the exponential distribution:
+ *   n = the first i < m with not (u_i q_i(x_i) < p_i(x_i)), or m
+ *   r = max(0, p_n - q_n) if n < m (p_n if that is 0 everywhere), p_m if n == m
+ *   y = the word with the largest r_v / e_v among those with r_v > 0, ties to
+ *       the lower one; -1 if there is none
+ *   accepted = n; tokens = x_0 .. x_{n-1}, y, -1 ...; logp = log p_i of each
+ *   token (0 beside a -1)
+ * The largest quotient is distributed as a draw from r / sum r, so the
+ * sequence that results is distributed as the target's own. A drafted token
+ * outside [0, V) is rejected and sets TKEF_STATUS_INDEX_RANGE; a NaN or +inf
+ * logit makes its row's probabilities NaN, which accepts nothing and samples
+ * nothing, and sets TKEF_STATUS_NAN where the result depends on it. */
+typedef struct tkef_verify_plan_s *tkef_verify_plan;
+
+/* Host only. batch: the most sequences of an execution (<= 65536); draft: tokens reserved per
+ * sequence. */
+int tkef_verify_plan_create(int64_t batch, int64_t draft, int64_t vocab, int32_t dtype,
+                            double temperature, tkef_verify_plan *plan_out);
+int tkef_verify_plan_destroy(tkef_verify_plan plan);
+int tkef_verify_plan_info(tkef_verify_plan plan, size_t *workspace_bytes);
+
+/* target: device; sequence b's row i at target + b * target_batch_stride + i *
+ * target_stride (elements), draft + 1 rows each; drafts: likewise, draft rows
+ * each. tokens (int32), uniform (binary32): device, batch * draft. noise:
+ * binary32, batch rows of V, noise_stride apart. length: device int32, one per
+ * sequence (clamped to [0, draft]), or NULL (draft). accepted (int32, batch),
+ * tokens_out (int32, batch * (draft + 1)), logp_out (binary32, batch * (draft +
+ * 1), or NULL): device. */
+int tkef_verify_execute(tkef_verify_plan plan, const void *target, int64_t target_batch_stride,
+                        int64_t target_stride, const void *drafts, int64_t draft_batch_stride,
+                        int64_t draft_stride, int64_t batch, const int32_t *tokens,
+                        const float *uniform, const float *noise, int64_t noise_stride,
+                        const int32_t *length, int32_t *accepted, int32_t *tokens_out,
+                        float *logp_out, void *ws, size_t ws_bytes, uint32_t *status,
+                        hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

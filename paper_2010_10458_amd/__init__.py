@@ -12,6 +12,9 @@ the library's HIP kernels. PyTorch supplies device memory and streams.
     up = UpdatePlan(numels, P=128, stride=k)
     up.bind(params, momentum)              # once
     up.execute(idx_all, val_all, lr=0.1, mu=0.9, wd=5e-5)
+
+Operators on rows of logits (TopLogitsPlan, DistillPlan, VerifyPlan and their
+one-shot calls) are in ``rows.py`` and exported here.
 """
 from __future__ import annotations
 
@@ -48,7 +51,7 @@ class TkefError(RuntimeError):
 class TkefStatusError(RuntimeError):
     """A call finished with bits set in its device status word."""
 
-    NAMES = {STATUS_NAN: "NaN in g + r (selection unspecified)",
+    NAMES = {STATUS_NAN: "NaN in g + r (selection unspecified) or in a row of logits",
              STATUS_UNSORTED: "an index list is not ascending",
              STATUS_INDEX_RANGE: "an index lies outside [0, d)",
              STATUS_TIMEOUT: "a wait between workgroups gave up (results invalid)",
@@ -110,6 +113,24 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         "tkef_lars_launch_name": ([i32, i32], ctypes.c_char_p),
         "tkef_sparse_aggregate_update": ([P(vp), P(vp), P(i64), i32, vp, vp, i32, i64, vp, f32,
                                           f32, f32, vp, sz, vp, vp], ctypes.c_int),
+        "tkef_top_plan_create": ([i64, i64, i64, i32, i32, f64, P(vp)], ctypes.c_int),
+        "tkef_top_plan_destroy": ([vp], ctypes.c_int),
+        "tkef_top_plan_info": ([vp, P(sz)], ctypes.c_int),
+        "tkef_top_execute": ([vp, vp, i64, i64, vp, vp, vp, vp, sz, vp, vp], ctypes.c_int),
+        "tkef_distill_plan_create": ([i64, i64, i64, i32, i32, f64, P(vp)], ctypes.c_int),
+        "tkef_distill_plan_destroy": ([vp], ctypes.c_int),
+        "tkef_distill_plan_info": ([vp, P(sz)], ctypes.c_int),
+        "tkef_distill_forward": ([vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp],
+                                 ctypes.c_int),
+        "tkef_distill_backward": ([vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz,
+                                   vp, vp], ctypes.c_int),
+        "tkef_distill_step": ([vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp, vp],
+                              ctypes.c_int),
+        "tkef_verify_plan_create": ([i64, i64, i64, i32, f64, P(vp)], ctypes.c_int),
+        "tkef_verify_plan_destroy": ([vp], ctypes.c_int),
+        "tkef_verify_plan_info": ([vp, P(sz)], ctypes.c_int),
+        "tkef_verify_execute": ([vp, vp, i64, i64, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp,
+                                 vp, vp, vp, sz, vp, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -682,3 +703,8 @@ def sparse_aggregate(outs: Sequence[torch.Tensor], idx: torch.Tensor, val: torch
         _ws(nbytes.value, dev).data_ptr(), max(nbytes.value, 256), status.data_ptr(),
         _stream_handle(None)))
     _finish("tkef_sparse_aggregate", status, own)
+
+
+from .rows import (DTYPE_BF16, DTYPE_F16, DTYPE_F32, ROWS_MAX_K, ROWS_MAX_ROWS,  # noqa: E402,F401
+                   ROWS_MAX_VOCAB, VERIFY_MAX_DRAFT, DistillPlan, TopLogitsPlan, VerifyPlan,
+                   distill_step, top_logits, verify_draft)

@@ -12,7 +12,7 @@ LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libtkef.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-SOURCES = ["tkef_kernels.hip", "tkef_api.cpp"]
+SOURCES = ["tkef_kernels.hip", "tkef_api.cpp", "tkef_rows.hip", "tkef_rows_api.cpp"]
 
 FLAGS = [
     "--offload-arch=gfx950",

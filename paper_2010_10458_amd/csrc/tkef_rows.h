@@ -1,0 +1,66 @@
+// Internal interface of the row operators (top logits, distillation, draft
+// verification): argument blocks the host fills and the gfx950 kernels read.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <hip/hip_runtime_api.h>
+
+namespace tkef {
+
+// A temperature enters the kernels as a = log2(e) / temperature and as inv_t
+// (+ inv_t_lo, what its rounding leaves) = 1 / temperature.
+struct TopArgs {
+  const void* z;
+  int64_t ld, rows;
+  int32_t V, k, dtype, val_format;
+  float a, inv_t;
+  int32_t* idx;
+  void* val;
+  float* tail;     // may be null
+  uint32_t* status;  // may be null
+};
+
+struct DistillArgs {
+  const void* z;
+  int64_t ld, rows;
+  int32_t V, k, dtype, val_format;
+  float a, inv_t, inv_t_lo, temperature;
+  const int32_t* idx;
+  const void* val;
+  const float* tail;      // may be null
+  const int32_t* count;   // may be null
+  const float* weight;    // may be null
+  float* loss;            // forward, step
+  float4* stats;          // forward: out (may be null); backward: in
+  const float* dloss;     // backward; may be null
+  void* grad;             // backward, step
+  int64_t gld;
+  uint32_t* status;       // may be null
+};
+
+struct VerifyArgs {
+  const void* target;
+  const void* drafts;
+  int64_t tb, ti, db, di;  // strides: target batch, target row, draft batch, draft row
+  int32_t batch, draft, V, dtype;
+  float a, inv_t;
+  const int32_t* tokens;
+  const float* uniform;
+  const float* noise;
+  int64_t noise_ld;
+  const int32_t* length;  // may be null
+  int32_t* accepted;
+  int32_t* tokens_out;
+  float* logp;            // may be null
+  uint32_t* status;       // may be null
+};
+
+hipError_t launch_top(const TopArgs& a, hipStream_t s);
+hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t s);
+hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s);
+hipError_t launch_distill_step(const DistillArgs& a, hipStream_t s);
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
+
+}  // namespace tkef

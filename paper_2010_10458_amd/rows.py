@@ -1,0 +1,408 @@
+"""Operators on rows of logits over a vocabulary (include/tkef.h, "Rows of
+logits"): a teacher's top logits as (idx, val) lists, distillation on such
+lists, verification of drafted tokens. Like the rest of the package this module
+only marshals arguments; the computation runs in the library's HIP kernels.
+
+    top = TopLogitsPlan(rows, vocab, k, dtype=torch.bfloat16, temperature=2.0)
+    idx, val, tail = top.execute(teacher_logits)
+
+    dp = DistillPlan(rows, vocab, k, dtype=torch.bfloat16, temperature=2.0)
+    loss, grad = dp.step(student_logits, idx, val, tail=tail)      # or .loss() under autograd
+
+    vp = VerifyPlan(batch, draft, vocab, dtype=torch.bfloat16)
+    accepted, tokens, logp = vp.execute(target_logits, draft_logits, drafted, uniform, noise)
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import torch
+
+from . import _check, _new_status, _raise_on_status, _stream_handle, _val_format, lib
+
+DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
+ROWS_MAX_ROWS = ROWS_MAX_VOCAB = 1 << 20
+ROWS_MAX_K = 1024
+VERIFY_MAX_DRAFT = 63
+
+_DTYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
+
+
+def _dtype_code(dtype) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError("logits are float32, float16 or bfloat16")
+    return code
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return t.data_ptr() if t is not None else None
+
+
+def _check_vector(t: Optional[torch.Tensor], n: int, dtype, what: str) -> None:
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_cuda
+                          or not t.is_contiguous()):
+        raise ValueError(f"{what}: expected {n} contiguous {dtype} CUDA values")
+
+
+class _RowPlan:
+    _destroy = ""
+
+    def __init__(self, rows: int, vocab: int, dtype, temperature: float, check: bool):
+        self.rows, self.vocab = int(rows), int(vocab)
+        self.dtype, self.temperature, self.check = dtype, float(temperature), bool(check)
+        self._h = ctypes.c_void_p()
+        self._free = getattr(lib(), self._destroy)
+        self._ws = {}  # one workspace per stream, so that calls on two streams do not share one
+
+    def __del__(self):
+        if getattr(self, "_h", None) and self._h.value:
+            self._free(self._h)
+            self._h = ctypes.c_void_p()
+
+    def _info(self, name: str) -> None:
+        ws = ctypes.c_size_t()
+        _check(name, getattr(lib(), name)(self._h, ctypes.byref(ws)))
+        self.ws_bytes = ws.value
+
+    def _workspace(self, stream: Optional[int], dev) -> Optional[int]:
+        if not self.ws_bytes:
+            return None
+        ws = self._ws.get((stream, dev))
+        if ws is None:
+            ws = self._ws[(stream, dev)] = torch.empty(self.ws_bytes, dtype=torch.uint8,
+                                                       device=dev)
+        return ws.data_ptr()
+
+    def _logits(self, x: torch.Tensor, what: str) -> Tuple[int, int]:
+        """(rows, row stride) of a 2-D tensor of the plan's type whose rows are
+        contiguous."""
+        if x.dim() != 2 or x.dtype != self.dtype or not x.is_cuda:
+            raise ValueError(f"{what}: expected a 2-D CUDA tensor of {self.dtype}")
+        n, vocab = x.shape
+        if vocab != self.vocab or n > self.rows:
+            raise ValueError(f"{what}: the plan takes up to {self.rows} rows of {self.vocab}")
+        if vocab > 1 and x.stride(1) != 1:
+            raise ValueError(f"{what}: the words of a row must be contiguous")
+        return n, (x.stride(0) if n > 1 else vocab)
+
+    def _status_of(self, status, dev):
+        if status is None and self.check:
+            return _new_status(dev), True
+        return status, False
+
+
+class _On:
+    """Allocations of a call that runs on `stream` come from that stream."""
+
+    def __new__(cls, stream):
+        return torch.cuda.stream(stream) if stream is not None else _NOTHING
+
+
+class _Nothing:
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *a):
+        return None
+
+
+_NOTHING = _Nothing()
+
+
+class TopLogitsPlan(_RowPlan):
+    """Each row's k greatest logits, as lists with ascending words, and the
+    log-mass of the others (tkef_top_execute)."""
+
+    _destroy = "tkef_top_plan_destroy"
+
+    def __init__(self, rows: int, vocab: int, k: int, dtype=torch.bfloat16,
+                 temperature: float = 1.0, val_dtype=torch.float32, check: bool = False):
+        """rows: the most rows a call gives. check=True: every execute without
+        a caller status word uses its own, synchronizes and raises
+        TkefStatusError on any status bit."""
+        super().__init__(rows, vocab, dtype, temperature, check)
+        self.k, self.val_dtype = int(k), val_dtype
+        _check("tkef_top_plan_create", lib().tkef_top_plan_create(
+            self.rows, self.vocab, self.k, _dtype_code(dtype), _val_format(val_dtype),
+            self.temperature, ctypes.byref(self._h)))
+        self._info("tkef_top_plan_info")
+
+    def execute(self, logits: torch.Tensor, idx_out: Optional[torch.Tensor] = None,
+                val_out: Optional[torch.Tensor] = None,
+                tail_out: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None, stream=None
+                ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """Returns idx (n, k) int32, val (n, k) of val_dtype, tail (n,) float32."""
+        n, ld = self._logits(logits, "logits")
+        dev = logits.device
+        h = _stream_handle(stream)
+        with _On(stream):
+            if idx_out is None:
+                idx_out = torch.empty((n, self.k), dtype=torch.int32, device=dev)
+            else:
+                _check_vector(idx_out, n * self.k, torch.int32, "idx_out")
+            if val_out is None:
+                val_out = torch.empty((n, self.k), dtype=self.val_dtype, device=dev)
+            else:
+                _check_vector(val_out, n * self.k, self.val_dtype, "val_out")
+            if tail_out is None:
+                tail_out = torch.empty((n,), dtype=torch.float32, device=dev)
+            else:
+                _check_vector(tail_out, n, torch.float32, "tail_out")
+            status, own = self._status_of(status, dev)
+            ws = self._workspace(h, dev)
+        _check("tkef_top_execute", lib().tkef_top_execute(
+            self._h, logits.data_ptr(), ld, n, idx_out.data_ptr(), val_out.data_ptr(),
+            tail_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h))
+        if own:
+            _raise_on_status("tkef_top_execute", status, stream)
+        return idx_out, val_out, tail_out
+
+
+class DistillPlan(_RowPlan):
+    """Distillation of student logits on a teacher's top-logit lists
+    (tkef_distill_forward / _backward / _step): the loss of each row and its
+    gradient. Every call takes the lists idx (n, k) int32 ascending and val
+    (n, k) of val_dtype, and optionally, one value per row: tail (float32, the
+    log-mass of the teacher's other words), count (int32, used entries of a
+    list) and weight (float32)."""
+
+    _destroy = "tkef_distill_plan_destroy"
+
+    def __init__(self, rows: int, vocab: int, k: int, dtype=torch.bfloat16,
+                 temperature: float = 1.0, val_dtype=torch.float32, check: bool = False):
+        super().__init__(rows, vocab, dtype, temperature, check)
+        self.k, self.val_dtype = int(k), val_dtype
+        _check("tkef_distill_plan_create", lib().tkef_distill_plan_create(
+            self.rows, self.vocab, self.k, _dtype_code(dtype), _val_format(val_dtype),
+            self.temperature, ctypes.byref(self._h)))
+        self._info("tkef_distill_plan_info")
+
+    def _lists(self, n, idx, val, tail, count, weight):
+        _check_vector(idx, n * self.k, torch.int32, "idx")
+        _check_vector(val, n * self.k, self.val_dtype, "val")
+        _check_vector(tail, n, torch.float32, "tail")
+        _check_vector(count, n, torch.int32, "count")
+        _check_vector(weight, n, torch.float32, "weight")
+        return (idx.data_ptr(), val.data_ptr(), _ptr(tail), _ptr(count), _ptr(weight))
+
+    def _grad(self, logits, grad_out):
+        if grad_out is None:
+            grad_out = torch.empty(logits.shape, dtype=self.dtype, device=logits.device)
+        elif grad_out.shape != logits.shape:
+            raise ValueError("grad_out: expected the shape of the logits")
+        return grad_out, self._logits(grad_out, "grad_out")[1]
+
+    def forward(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
+                tail: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                weight: Optional[torch.Tensor] = None, loss_out: Optional[torch.Tensor] = None,
+                stats_out: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None, stream=None
+                ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Returns loss (n,) float32 and stats (n, 4) float32, which backward takes."""
+        n, ld = self._logits(logits, "logits")
+        lists = self._lists(n, idx, val, tail, count, weight)
+        dev = logits.device
+        h = _stream_handle(stream)
+        with _On(stream):
+            if loss_out is None:
+                loss_out = torch.empty((n,), dtype=torch.float32, device=dev)
+            else:
+                _check_vector(loss_out, n, torch.float32, "loss_out")
+            if stats_out is None:
+                stats_out = torch.empty((n, 4), dtype=torch.float32, device=dev)
+            else:
+                _check_vector(stats_out, n * 4, torch.float32, "stats_out")
+            status, own = self._status_of(status, dev)
+            ws = self._workspace(h, dev)
+        _check("tkef_distill_forward", lib().tkef_distill_forward(
+            self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
+            stats_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h))
+        if own:
+            _raise_on_status("tkef_distill_forward", status, stream)
+        return loss_out, stats_out
+
+    def backward(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
+                 stats: torch.Tensor, tail: Optional[torch.Tensor] = None,
+                 count: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                 dloss: Optional[torch.Tensor] = None, grad_out: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Gradient of sum(dloss * loss) (dloss (n,) float32, default 1) in the
+        logits' type. grad_out may be the logits themselves."""
+        n, ld = self._logits(logits, "logits")
+        lists = self._lists(n, idx, val, tail, count, weight)
+        _check_vector(stats, n * 4, torch.float32, "stats")
+        _check_vector(dloss, n, torch.float32, "dloss")
+        dev = logits.device
+        h = _stream_handle(stream)
+        with _On(stream):
+            grad_out, gld = self._grad(logits, grad_out)
+            status, own = self._status_of(status, dev)
+            ws = self._workspace(h, dev)
+        _check("tkef_distill_backward", lib().tkef_distill_backward(
+            self._h, logits.data_ptr(), ld, n, *lists, stats.data_ptr(), _ptr(dloss),
+            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h))
+        if own:
+            _raise_on_status("tkef_distill_backward", status, stream)
+        return grad_out
+
+    def step(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
+             tail: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+             weight: Optional[torch.Tensor] = None, loss_out: Optional[torch.Tensor] = None,
+             grad_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+             stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Loss (n,) float32 and the gradient of its sum, in one call.
+        grad_out may be the logits themselves."""
+        n, ld = self._logits(logits, "logits")
+        lists = self._lists(n, idx, val, tail, count, weight)
+        dev = logits.device
+        h = _stream_handle(stream)
+        with _On(stream):
+            if loss_out is None:
+                loss_out = torch.empty((n,), dtype=torch.float32, device=dev)
+            else:
+                _check_vector(loss_out, n, torch.float32, "loss_out")
+            grad_out, gld = self._grad(logits, grad_out)
+            status, own = self._status_of(status, dev)
+            ws = self._workspace(h, dev)
+        _check("tkef_distill_step", lib().tkef_distill_step(
+            self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
+            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h))
+        if own:
+            _raise_on_status("tkef_distill_step", status, stream)
+        return loss_out, grad_out
+
+    def loss(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
+             tail: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+             weight: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The loss (n,) as a node of torch's autograd graph: its backward
+        pass is `backward` (gradients of the logits only)."""
+        return _DistillLoss.apply(logits, self, idx, val, tail, count, weight)
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, plan, idx, val, tail, count, weight):
+        loss, stats = plan.forward(logits, idx, val, tail=tail, count=count, weight=weight)
+        ctx.plan = plan
+        ctx.save_for_backward(logits, idx, val, stats, tail, count, weight)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        logits, idx, val, stats, tail, count, weight = ctx.saved_tensors
+        grad = ctx.plan.backward(logits, idx, val, stats, tail=tail, count=count, weight=weight,
+                                 dloss=dloss.to(torch.float32).contiguous())
+        return grad, None, None, None, None, None, None
+
+
+class VerifyPlan(_RowPlan):
+    """Verification of drafted tokens against a target model's logits from
+    given random numbers (tkef_verify_execute)."""
+
+    _destroy = "tkef_verify_plan_destroy"
+
+    def __init__(self, batch: int, draft: int, vocab: int, dtype=torch.bfloat16,
+                 temperature: float = 1.0, check: bool = False):
+        """batch: the most sequences a call gives; draft: tokens per sequence."""
+        super().__init__(batch, vocab, dtype, temperature, check)
+        self.batch, self.draft = self.rows, int(draft)
+        _check("tkef_verify_plan_create", lib().tkef_verify_plan_create(
+            self.rows, self.draft, self.vocab, _dtype_code(dtype), self.temperature,
+            ctypes.byref(self._h)))
+        self._info("tkef_verify_plan_info")
+
+    def _block(self, x: torch.Tensor, places: int, what: str) -> Tuple[int, int]:
+        if x.dim() != 3 or x.dtype != self.dtype or not x.is_cuda:
+            raise ValueError(f"{what}: expected a 3-D CUDA tensor of {self.dtype}")
+        if x.shape[1] != places or x.shape[2] != self.vocab or x.shape[0] > self.batch:
+            raise ValueError(f"{what}: the plan takes up to {self.batch} x {places} x "
+                             f"{self.vocab}")
+        if self.vocab > 1 and x.stride(2) != 1:
+            raise ValueError(f"{what}: the words of a row must be contiguous")
+        return x.stride(0), (x.stride(1) if places > 1 else self.vocab)
+
+    def execute(self, target: torch.Tensor, drafts: torch.Tensor, tokens: torch.Tensor,
+                uniform: torch.Tensor, noise: torch.Tensor,
+                length: Optional[torch.Tensor] = None,
+                accepted_out: Optional[torch.Tensor] = None,
+                tokens_out: Optional[torch.Tensor] = None,
+                logp_out: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None, stream=None
+                ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """target (b, draft + 1, vocab) and drafts (b, draft, vocab) logits,
+        tokens (b, draft) int32, uniform (b, draft) float32 in [0, 1), noise
+        (b, vocab) float32 from the exponential distribution, length (b,) int32.
+        Returns accepted (b,) int32, tokens (b, draft + 1) int32 (accepted
+        drafts, the token after them, then -1) and their log-probabilities
+        under the target (b, draft + 1) float32."""
+        tb, ti = self._block(target, self.draft + 1, "target")
+        db, di = self._block(drafts, self.draft, "drafts")
+        b = target.shape[0]
+        if drafts.shape[0] != b:
+            raise ValueError("target and drafts differ in their number of sequences")
+        _check_vector(tokens, b * self.draft, torch.int32, "tokens")
+        _check_vector(uniform, b * self.draft, torch.float32, "uniform")
+        _check_vector(length, b, torch.int32, "length")
+        if noise.dtype != torch.float32 or not noise.is_cuda or \
+                noise.shape != (b, self.vocab) or (self.vocab > 1 and noise.stride(1) != 1):
+            raise ValueError("noise: expected (batch, vocab) float32 CUDA values in rows")
+        dev = target.device
+        h = _stream_handle(stream)
+        with _On(stream):
+            if accepted_out is None:
+                accepted_out = torch.empty((b,), dtype=torch.int32, device=dev)
+            else:
+                _check_vector(accepted_out, b, torch.int32, "accepted_out")
+            if tokens_out is None:
+                tokens_out = torch.empty((b, self.draft + 1), dtype=torch.int32, device=dev)
+            else:
+                _check_vector(tokens_out, b * (self.draft + 1), torch.int32, "tokens_out")
+            if logp_out is None:
+                logp_out = torch.empty((b, self.draft + 1), dtype=torch.float32, device=dev)
+            else:
+                _check_vector(logp_out, b * (self.draft + 1), torch.float32, "logp_out")
+            status, own = self._status_of(status, dev)
+            ws = self._workspace(h, dev)
+        _check("tkef_verify_execute", lib().tkef_verify_execute(
+            self._h, target.data_ptr(), tb, ti, drafts.data_ptr(), db, di, b,
+            tokens.data_ptr(), uniform.data_ptr(), noise.data_ptr(),
+            noise.stride(0) if b > 1 else self.vocab, _ptr(length), accepted_out.data_ptr(),
+            tokens_out.data_ptr(), logp_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h))
+        if own:
+            _raise_on_status("tkef_verify_execute", status, stream)
+        return accepted_out, tokens_out, logp_out
+
+
+# ----------------------------------------------------------------------------
+# one-shot calls: a plan, one execution, and TkefStatusError on any status bit
+# (they synchronize), unless the caller gives a status word to check itself
+
+def top_logits(logits: torch.Tensor, k: int, temperature: float = 1.0,
+               val_dtype=torch.float32, status: Optional[torch.Tensor] = None):
+    """(idx, val, tail) of each row's k greatest logits: TopLogitsPlan."""
+    plan = TopLogitsPlan(max(1, logits.shape[0]), logits.shape[1], k, logits.dtype, temperature,
+                         val_dtype, check=status is None)
+    return plan.execute(logits, status=status)
+
+
+def distill_step(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
+                 temperature: float = 1.0, tail: Optional[torch.Tensor] = None,
+                 count: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None):
+    """(loss, grad) of each row: DistillPlan.step."""
+    plan = DistillPlan(max(1, logits.shape[0]), logits.shape[1], idx.shape[1], logits.dtype,
+                       temperature, val.dtype, check=status is None)
+    return plan.step(logits, idx, val, tail=tail, count=count, weight=weight, status=status)
+
+
+def verify_draft(target: torch.Tensor, drafts: torch.Tensor, tokens: torch.Tensor,
+                 uniform: torch.Tensor, noise: torch.Tensor, temperature: float = 1.0,
+                 length: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """(accepted, tokens, logp) of each sequence: VerifyPlan.execute."""
+    plan = VerifyPlan(max(1, target.shape[0]), drafts.shape[1], target.shape[2], target.dtype,
+                      temperature, check=status is None)
+    return plan.execute(target, drafts, tokens, uniform, noise, length=length, status=status)

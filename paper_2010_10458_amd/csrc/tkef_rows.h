@@ -58,9 +58,13 @@ struct VerifyArgs {
 };
 
 hipError_t launch_top(const TopArgs& a, hipStream_t s);
-hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t s);
+// A row that is too long for one workgroup's registers is taken in this many
+// chunks (1: whole); ws then holds kPartBytes for each.
+constexpr size_t kPartBytes = 32;
+int distill_chunks(int64_t V, int32_t dtype);
+hipError_t launch_distill_forward(const DistillArgs& a, void* ws, hipStream_t s);
 hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s);
-hipError_t launch_distill_step(const DistillArgs& a, hipStream_t s);
+hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
 
 }  // namespace tkef

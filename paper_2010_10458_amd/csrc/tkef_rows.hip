@@ -109,6 +109,168 @@ __device__ __forceinline__ void raise_status(uint32_t* status, uint32_t bits) {
   if (status != nullptr && bits != 0u) atomicOr(status, bits);
 }
 
+// ----------------------------------------------------------------------------
+// rows in 16-byte vectors
+
+// Elements before the first 16-byte boundary (the head) and those after the
+// last whole vector are "extras", at most 14: every vector access is aligned
+// whatever the row's address. Vector v holds elements head + v * N ...
+template <typename T>
+struct Span {
+  static constexpr int N = 16 / (int)sizeof(T);
+  const T* p;
+  int head, nvec, extras;
+  __device__ Span(const T* row, int V) : p(row) {
+    head = (int)((16u - (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u)) & 15u) /
+           (int)sizeof(T);
+    head = head < V ? head : V;
+    nvec = (V - head) / N;
+    extras = V - nvec * N;
+  }
+  __device__ const T* vec(int v) const { return p + head + (int64_t)v * N; }
+  // element index of extra i
+  __device__ int extra(int i) const { return i < head ? i : i + nvec * N; }
+};
+
+__device__ __forceinline__ void unpack(uint4 r, float (&x)[4], const float*) {
+  x[0] = __uint_as_float(r.x);
+  x[1] = __uint_as_float(r.y);
+  x[2] = __uint_as_float(r.z);
+  x[3] = __uint_as_float(r.w);
+}
+__device__ __forceinline__ void unpack(uint4 r, float (&x)[8], const __bf16*) {
+  const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(u[i] << 16);
+    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
+typedef _Float16 half2_ __attribute__((ext_vector_type(2)));
+typedef __bf16 bfloat2_ __attribute__((ext_vector_type(2)));
+typedef float float2_ __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void unpack(uint4 r, float (&x)[8], const _Float16*) {
+  const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const half2_ h = __builtin_bit_cast(half2_, u[i]);
+    x[2 * i] = (float)h.x;
+    x[2 * i + 1] = (float)h.y;
+  }
+}
+
+__device__ __forceinline__ uint4 pack(const float (&x)[4], const float*) {
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                    __float_as_uint(x[3]));
+}
+template <typename H2>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const float2_ v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, H2));
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8], const __bf16*) {
+  return make_uint4(pack2<bfloat2_>(x[0], x[1]), pack2<bfloat2_>(x[2], x[3]),
+                    pack2<bfloat2_>(x[4], x[5]), pack2<bfloat2_>(x[6], x[7]));
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8], const _Float16*) {
+  return make_uint4(pack2<half2_>(x[0], x[1]), pack2<half2_>(x[2], x[3]),
+                    pack2<half2_>(x[4], x[5]), pack2<half2_>(x[6], x[7]));
+}
+
+// four -inf words of a type
+__device__ __forceinline__ uint4 none_of(const float*) {
+  return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u);
+}
+__device__ __forceinline__ uint4 none_of(const __bf16*) {
+  return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+}
+__device__ __forceinline__ uint4 none_of(const _Float16*) {
+  return make_uint4(0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u);
+}
+
+// -inf in the places of a vector whose bit is set
+__device__ __forceinline__ uint4 strike(uint4 r, uint32_t bits, const float*) {
+  r.x = (bits & 1u) ? 0xFF800000u : r.x;
+  r.y = (bits & 2u) ? 0xFF800000u : r.y;
+  r.z = (bits & 4u) ? 0xFF800000u : r.z;
+  r.w = (bits & 8u) ? 0xFF800000u : r.w;
+  return r;
+}
+template <uint32_t kNone>
+__device__ __forceinline__ uint32_t strike2(uint32_t w, uint32_t bits) {
+  w = (bits & 1u) ? (w & 0xFFFF0000u) | kNone : w;
+  return (bits & 2u) ? (w & 0x0000FFFFu) | (kNone << 16) : w;
+}
+__device__ __forceinline__ uint4 strike(uint4 r, uint32_t bits, const __bf16*) {
+  return make_uint4(strike2<0xFF80u>(r.x, bits), strike2<0xFF80u>(r.y, bits >> 2),
+                    strike2<0xFF80u>(r.z, bits >> 4), strike2<0xFF80u>(r.w, bits >> 6));
+}
+__device__ __forceinline__ uint4 strike(uint4 r, uint32_t bits, const _Float16*) {
+  return make_uint4(strike2<0xFC00u>(r.x, bits), strike2<0xFC00u>(r.y, bits >> 2),
+                    strike2<0xFC00u>(r.z, bits >> 4), strike2<0xFC00u>(r.w, bits >> 6));
+}
+
+__device__ __forceinline__ uint4 load16(const void* p) {
+  return *static_cast<const uint4*>(p);
+}
+// a store to any address of the element's alignment
+struct __attribute__((packed, aligned(2))) Loose16 {
+  uint32_t x, y, z, w;
+};
+__device__ __forceinline__ void store16(void* p, uint4 r) {
+  Loose16 l;
+  l.x = r.x;
+  l.y = r.y;
+  l.z = r.z;
+  l.w = r.w;
+  *static_cast<Loose16*>(p) = l;
+}
+
+// Makes the registers opaque: without it the compiler keeps the unpacked
+// values of one pass for the next, in twice the registers.
+__device__ __forceinline__ void renew(uint4& r) {
+  asm("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w));
+}
+
+template <int N>
+__device__ __forceinline__ float max_of(float m, const float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2) m = fmaxf(m, fmaxf(x[i], x[i + 1]));
+  return m;
+}
+
+// Wave reductions over DPP row shifts: lane 15 of each row of 16 lanes ends
+// with its row's result; the four are then read and joined.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float old, float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL,
+                                                    0xF, 0xF, false));
+}
+__device__ __forceinline__ float lane_value(float x, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, dpp<0x111>(x, x));
+  x = fmaxf(x, dpp<0x112>(x, x));
+  x = fmaxf(x, dpp<0x114>(x, x));
+  return fmaxf(x, dpp<0x118>(x, x));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp<0x111>(0.f, x);
+  x += dpp<0x112>(0.f, x);
+  x += dpp<0x114>(0.f, x);
+  return x + dpp<0x118>(0.f, x);
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = row_max(x);
+  return fmaxf(fmaxf(lane_value(x, 15), lane_value(x, 31)),
+               fmaxf(lane_value(x, 47), lane_value(x, 63)));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x = row_sum(x);
+  return (lane_value(x, 15) + lane_value(x, 31)) + (lane_value(x, 47) + lane_value(x, 63));
+}
+
 constexpr int kNT = 256;
 
 // ----------------------------------------------------------------------------
@@ -268,137 +430,389 @@ __device__ __forceinline__ bool entry_ok(const int32_t* idx, int j, int V, uint3
   return true;
 }
 
-constexpr int kTileWords = 1024;                // LDS bitmap of listed words
-constexpr int kTileElems = kTileWords * 32;
+// What a part of a row (a wave's share, or a chunk's) adds to its sums: the
+// unlisted words' and the listed words' student sums, the list's teacher sum,
+// and sum_j 2^((t_j - tm) a) (t_j - z_j) a over its listed words.
+struct Part {
+  float rm, rs, zm, zs, tm, ts, cross, pad;
+};
+static_assert(sizeof(Part) == kPartBytes, "workspace layout");
 
-// loss and the student's sums, one workgroup per row, reading it in tiles
-template <typename T>
-__global__ __launch_bounds__(kNT) void k_distill_loss(DistillArgs A) {
-  __shared__ uint32_t listed[kTileWords];
-  __shared__ float red[kNT / 64];
-  const int tid = threadIdx.x;
+// fmaxf passes over a NaN; the sums carry it
+__device__ __forceinline__ float join_sum(float m, float s, float top, float a) {
+  return s * rescale(m, top, a);
+}
+
+__device__ __forceinline__ Part wave_join(Part p, float a) {
+  Part r;
+  r.rm = wave_max(p.rm);
+  r.zm = wave_max(p.zm);
+  r.tm = wave_max(p.tm);
+  r.rs = wave_sum(join_sum(p.rm, p.rs, r.rm, a));
+  r.zs = wave_sum(join_sum(p.zm, p.zs, r.zm, a));
+  const float f = rescale(p.tm, r.tm, a);
+  r.ts = wave_sum(p.ts * f);
+  r.cross = wave_sum(f > 0.f ? p.cross * f : 0.f);
+  r.pad = 0.f;
+  return r;
+}
+
+// what a row's gradient needs
+struct RowSums {
+  Teacher t;
+  float rm, rs, zm, zs;  // student sums: unlisted, listed
+  float loss;            // divergence, natural units
+};
+
+__device__ __forceinline__ RowSums row_sums(const Part& p, const DistillArgs& A, int64_t row) {
+  RowSums r;
+  LogSum list;
+  list.m = p.tm;
+  list.S = p.ts;
+  r.t = teacher_of(list, A, row);
+  r.rm = p.rm;
+  r.rs = p.rs;
+  r.zm = p.zm;
+  r.zs = p.zs;
+  const float top = fmaxf(p.rm, p.zm);
+  const float total = join_sum(p.rm, p.rs, top, A.a) + join_sum(p.zm, p.zs, top, A.a);
+  // sum_j p_j (log p_j - log q_j) = sum_j p_j s (t_j - z_j) + (LZ - LT) sum_j p_j, and
+  // with the others' term p_r (log p_r - log q_r) = p_r (tau - LR) + p_r (LZ - LT)
+  const float f = rescale(p.tm, r.t.m, A.a) * r.t.inv;
+  float loss = (f > 0.f ? p.cross * f : 0.f) +
+               ((top - r.t.m) * A.a + (log2_(total) - log2_(r.t.S)));
+  if (r.t.p_rest > 0.f)
+    loss += p.rs == 0.f
+                ? kInf
+                : r.t.p_rest * (tail_over(r.t.tau, p.rm, A.inv_t, A.inv_t_lo) - log2_(p.rs));
+  if (!(total > 0.f) || !has_mass(r.t)) loss = __uint_as_float(0x7FC00000u);
+  r.loss = loss * kLn2;
+  return r;
+}
+
+// the factors of a row's gradient: unlisted words get 2^((x - rm) a) * rest,
+// listed ones 2^((z - zm) a) * list - p_j * up
+struct GradScale {
+  float rm, rest, zm, list, up;
+};
+
+__device__ __forceinline__ GradScale grad_scale(const RowSums& r, const DistillArgs& A, float up) {
+  GradScale g;
+  const float top = fmaxf(r.rm, r.zm);
+  const float s_rest = rescale(r.rm, top, A.a), s_list = rescale(r.zm, top, A.a);
+  const float total = r.rs * s_rest + r.zs * s_list;
+  const float inv = 1.f / total;
+  g.up = up;
+  g.rm = r.rm == -kInf ? 0.f : r.rm;
+  g.zm = r.zm == -kInf ? 0.f : r.zm;
+  // q_i (1 - p_r / q_r) = 2^((x_i - rm) a) (s_rest / total - p_r / rs)
+  g.rest = up * (s_rest * inv - (r.t.p_rest > 0.f && r.rs > 0.f ? r.t.p_rest / r.rs : 0.f));
+  g.list = up * (s_list * inv);
+  if (!(total > 0.f) || !has_mass(r.t)) g.rest = g.list = __uint_as_float(0x7FC00000u);
+  return g;
+}
+
+// listed words of a row in LDS
+struct ListLds {
+  int32_t word[TKEF_ROWS_MAX_K];  // -1: left out
+  float t[TKEF_ROWS_MAX_K], z[TKEF_ROWS_MAX_K];
+};
+
+__device__ __forceinline__ int used_entries(const DistillArgs& A, int64_t row) {
+  if (A.count == nullptr) return A.k;
+  const int c = A.count[row];
+  return c < 0 ? 0 : c < A.k ? c : A.k;
+}
+
+// Zeros over elements [v0, v1) of vectors and, where `edges`, the extras of a
+// row of grad (its own span: the gradient's address decides the vectors).
+template <typename T, int TPB>
+__device__ __forceinline__ void zero_row(T* g, int V, int chunk, int chunks) {
+  const Span<T> s(g, V);
+  const int per = (s.nvec + chunks - 1) / chunks;
+  const int v0 = chunk * per, v1 = v0 + per < s.nvec ? v0 + per : s.nvec;
+  for (int v = v0 + (int)threadIdx.x; v < v1; v += TPB)
+    *reinterpret_cast<uint4*>(g + s.head + (int64_t)v * Span<T>::N) = make_uint4(0u, 0u, 0u, 0u);
+  if (chunk == 0 && (int)threadIdx.x < s.extras) g[s.extra((int)threadIdx.x)] = (T)0.f;
+}
+
+enum { kLoss = 0, kStep = 1, kPart = 2 };
+
+// One workgroup takes a row, or one of a row's chunks, and holds it in
+// registers: NV vectors a thread, loaded once.
+//   kLoss  whole row: loss and sums
+//   kStep  whole row: loss and gradient, from the one read
+//   kPart  chunk blockIdx.y of gridDim.y: its Part into `parts`
+// Listed words are marked in LDS (a byte a vector) and struck from the
+// registers before the maximum and the sum, so the unlisted sum is exact even
+// where the list has nearly all the mass; the gradient's listed words are
+// written over the vectors' stores after a barrier.
+template <typename T, int TPB, int NV, int MODE>
+__global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts) {
+  constexpr int N = Span<T>::N, NW = TPB / 64;
+  __shared__ __align__(16) uint8_t mark[TPB * NV];  // thread t's vectors at t * NV
+  __shared__ uint32_t mark_extra;
+  __shared__ ListLds list;
+  __shared__ Part red[NW];
+  const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x;
-  const T* p = static_cast<const T*>(A.z) + row * A.ld;
-  const int32_t* idx = A.idx + row * A.k;
-  int cnt = A.k;
-  if (A.count != nullptr) cnt = A.count[row] < 0 ? 0 : A.count[row] < A.k ? A.count[row] : A.k;
+  const int cnt = used_entries(A, row);
   const float w = A.weight != nullptr ? A.weight[row] : 1.f;
   if (cnt == 0 || w == 0.f) {
-    if (tid == 0) {
-      if (A.loss != nullptr) A.loss[row] = 0.f;
-      if (A.stats != nullptr) A.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (MODE == kStep) zero_row<T, TPB>(static_cast<T*>(A.grad) + row * A.gld, A.V, 0, 1);
+    if (MODE != kPart && tid == 0) {
+      A.loss[row] = 0.f;
+      if (MODE == kLoss && A.stats != nullptr) A.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     return;
   }
+  const Span<T> s(static_cast<const T*>(A.z) + row * A.ld, A.V);
+  const int v0 = MODE == kPart ? (int)blockIdx.y * (TPB * NV) : 0;
+  const bool edges = MODE != kPart || blockIdx.y == 0;
+  const T* type = nullptr;
+  uint4 r[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    r[i] = v < s.nvec ? load16(s.vec(v)) : none_of(type);
+  }
+  float ex = edges && tid < s.extras ? (float)s.p[s.extra(tid)] : -kInf;
+  for (int i = tid; i < TPB * NV / 16; i += TPB)
+    reinterpret_cast<uint4*>(mark)[i] = make_uint4(0u, 0u, 0u, 0u);
+  if (tid == 0) mark_extra = 0u;
+  __syncthreads();
+  // the list: marks, and the sums over listed words
+  Part part = {-kInf, 0.f, -kInf, 0.f, -kInf, 0.f, 0.f, 0.f};
   uint32_t bits = 0u;
-  LogSum teach, zl;
-  for (int j = tid; j < cnt; j += kNT) {
-    if (!entry_ok(idx, j, A.V, &bits)) continue;
-    const float t = load_val(A.val, A.val_format, row * A.k + j);
-    teach.add(t, A.a);
-    zl.add(load1(p, idx[j]), A.a);
-  }
-  raise_status(A.status, bits);
-  teach = block_join<kNT>(teach, A.a, red);
-  zl = block_join<kNT>(zl, A.a, red);
-  LogSum rest;
-  for (int base = 0; base < A.V; base += kTileElems) {
-    for (int i = tid; i < kTileWords; i += kNT) listed[i] = 0u;
-    __syncthreads();
-    for (int j = tid; j < cnt; j += kNT) {
-      uint32_t ignore = 0u;
-      const int32_t i = idx[j] - base;
-      if (entry_ok(idx, j, A.V, &ignore) && i >= 0 && i < kTileElems)
-        atomicOr(&listed[i >> 5], 1u << (i & 31));
+  const int32_t* idx = A.idx + row * A.k;
+  for (int j = tid; j < cnt; j += TPB) {
+    bool mine = entry_ok(idx, j, A.V, &bits);
+    if (mine) {
+      const int e = idx[j] - s.head;
+      const int v = e / N - v0;
+      if (e < 0 || e >= s.nvec * N) {
+        mine = edges;
+        const int x = e < 0 ? idx[j] : idx[j] - s.nvec * N;
+        if (mine) atomicOr(&mark_extra, 1u << x);
+      } else if (v < 0 || v >= TPB * NV) {
+        mine = false;
+      } else {
+        const int at = (v % TPB) * NV + v / TPB;
+        atomicOr(reinterpret_cast<uint32_t*>(mark) + (at >> 2), (1u << (e % N)) << ((at & 3) * 8));
+      }
     }
-    __syncthreads();
-    const int end = A.V - base < kTileElems ? A.V - base : kTileElems;
-    for (int i = tid; i < end; i += kNT)
-      if (!((listed[i >> 5] >> (i & 31)) & 1u)) rest.add(load1(p, base + i), A.a);
-    __syncthreads();
+    float t = 0.f, z = 0.f;
+    if (mine) {
+      t = load_val(A.val, A.val_format, row * A.k + j);
+      z = (float)s.p[idx[j]];
+      LogSum zs, ts;
+      zs.m = part.zm;
+      zs.S = part.zs;
+      zs.add(z, A.a);
+      part.zm = zs.m;
+      part.zs = zs.S;
+      const float before = part.tm;
+      ts.m = part.tm;
+      ts.S = part.ts;
+      ts.add(t, A.a);
+      part.tm = ts.m;
+      part.ts = ts.S;
+      const float f = before == ts.m ? 1.f : rescale(before, ts.m, A.a);
+      const float p = ts.m == -kInf ? 0.f : exp2_((t - ts.m) * A.a);
+      part.cross = (f > 0.f ? part.cross * f : 0.f) + (p > 0.f ? p * ((t - z) * A.a) : 0.f);
+    }
+    list.word[j] = mine ? idx[j] : -1;
+    list.t[j] = t;
+    list.z[j] = z;
   }
-  rest = block_join<kNT>(rest, A.a, red);
-  const Teacher t = teacher_of(teach, A, row);
-  LogSum all;
-  all.m = rest.m > zl.m ? rest.m : zl.m;
-  all.S = rest.S * rescale(rest.m, all.m, A.a) + zl.S * rescale(zl.m, all.m, A.a);
-  // sum_j p_j (log p_j - log q_j) = sum_j p_j s (t_j - z_j) + (LZ - LT) sum_j p_j
-  float cross = 0.f;
-  for (int j = tid; j < cnt; j += kNT) {
-    uint32_t ignore = 0u;
-    if (!entry_ok(idx, j, A.V, &ignore)) continue;
-    const float v = load_val(A.val, A.val_format, row * A.k + j);
-    const float pj = teacher_prob(v, A.a, t);
-    if (pj > 0.f) cross += pj * ((v - load1(p, idx[j])) * A.a);
+  if (MODE != kPart || blockIdx.y == 0) raise_status(A.status, bits);
+  __syncthreads();
+  // strike the listed words, then the maximum and the sum of what is left
+  if ((mark_extra >> (tid < 32 ? tid : 31)) & (tid < 32 ? 1u : 0u)) ex = -kInf;
+  float m = ex;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const uint32_t b = mark[tid * NV + i];
+    if (b != 0u) r[i] = strike(r[i], b, type);
+    float x[N];
+    unpack(r[i], x, type);
+    m = max_of(m, x);
   }
-  cross = block_reduce<kNT>(cross, red, AddOp());
-  if (tid == 0) {
-    float loss = cross + ((all.m - t.m) * A.a + (log2_(all.S) - log2_(t.S)));
-    if (t.p_rest > 0.f)
-      loss += rest.S == 0.f
-                  ? kInf
-                  : t.p_rest * (tail_over(t.tau, rest.m, A.inv_t, A.inv_t_lo) - log2_(rest.S));
-    if (!(all.S > 0.f) || !has_mass(t)) loss = __uint_as_float(0x7FC00000u);
-    if (A.loss != nullptr) A.loss[row] = loss * (kLn2 * w) * (A.temperature * A.temperature);
-    if (A.stats != nullptr) A.stats[row] = make_float4(rest.m, rest.S, zl.m, zl.S);
+  const float ref = m == -kInf ? 0.f : m;
+  float sum = exp2_((ex - ref) * A.a);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float x[N];
+    renew(r[i]);
+    unpack(r[i], x, type);
+    float e = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * A.a);
+    sum += e;
+  }
+  part.rm = m;
+  part.rs = sum;
+  part = wave_join(part, A.a);
+  if (lane == 0) red[tid >> 6] = part;
+  __syncthreads();
+  {
+    const int o = lane < NW ? lane : 0;
+    part = red[o];
+    if (lane >= NW) part.rs = part.zs = part.ts = part.cross = 0.f;
+    part = wave_join(part, A.a);
+  }
+  if constexpr (MODE == kPart) {
+    if (tid == 0) parts[row * gridDim.y + blockIdx.y] = part;
+  } else {
+    const RowSums sums = row_sums(part, A, row);
+    if (tid == 0) {
+      A.loss[row] = sums.loss * w * (A.temperature * A.temperature);
+      if (MODE == kLoss && A.stats != nullptr)
+        A.stats[row] = make_float4(sums.rm, sums.rs, sums.zm, sums.zs);
+    }
+    if constexpr (MODE == kStep) {
+      const GradScale g = grad_scale(sums, A, w * A.temperature);
+      T* grad = static_cast<T*>(A.grad) + row * A.gld;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int v = i * TPB + tid;
+        float x[N];
+        renew(r[i]);
+        unpack(r[i], x, type);
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] = exp2_((x[n] - g.rm) * A.a) * g.rest;
+        if (v < s.nvec) store16(grad + s.head + (int64_t)v * N, pack(x, type));
+      }
+      if (tid < s.extras) grad[s.extra(tid)] = (T)(exp2_((ex - g.rm) * A.a) * g.rest);
+      __syncthreads();
+      for (int j = tid; j < cnt; j += TPB)
+        if (list.word[j] >= 0)
+          grad[list.word[j]] = (T)(exp2_((list.z[j] - g.zm) * A.a) * g.list -
+                                   teacher_prob(list.t[j], A.a, sums.t) * g.up);
+    }
   }
 }
 
-// gradient from the student's sums, one workgroup per row
-template <typename T>
-__global__ __launch_bounds__(kNT) void k_distill_grad(DistillArgs A) {
-  __shared__ float red[kNT / 64];
-  __shared__ float patch[TKEF_ROWS_MAX_K];  // gradients of the listed words
-  const int tid = threadIdx.x;
+// Sum of a row's chunk parts, by every wave of a workgroup.
+__device__ __forceinline__ Part join_parts(const Part* parts, int n, float a) {
+  Part p = {-kInf, 0.f, -kInf, 0.f, -kInf, 0.f, 0.f, 0.f};
+  for (int i = (int)(threadIdx.x & 63); i < n; i += 64) {
+    const Part q = parts[i];
+    const float rm = fmaxf(p.rm, q.rm), zm = fmaxf(p.zm, q.zm), tm = fmaxf(p.tm, q.tm);
+    p.rs = join_sum(p.rm, p.rs, rm, a) + join_sum(q.rm, q.rs, rm, a);
+    p.zs = join_sum(p.zm, p.zs, zm, a) + join_sum(q.zm, q.zs, zm, a);
+    const float fp = rescale(p.tm, tm, a), fq = rescale(q.tm, tm, a);
+    p.ts = p.ts * fp + q.ts * fq;
+    p.cross = (fp > 0.f ? p.cross * fp : 0.f) + (fq > 0.f ? q.cross * fq : 0.f);
+    p.rm = rm;
+    p.zm = zm;
+    p.tm = tm;
+  }
+  return wave_join(p, a);
+}
+
+// loss and sums of a row from its parts, one wave a row
+__global__ __launch_bounds__(64) void k_distill_join(DistillArgs A, const Part* parts, int chunks) {
   const int64_t row = blockIdx.x;
-  const T* p = static_cast<const T*>(A.z) + row * A.ld;
-  T* g = static_cast<T*>(A.grad) + row * A.gld;
-  const int32_t* idx = A.idx + row * A.k;
-  int cnt = A.k;
-  if (A.count != nullptr) cnt = A.count[row] < 0 ? 0 : A.count[row] < A.k ? A.count[row] : A.k;
+  const float w = A.weight != nullptr ? A.weight[row] : 1.f;
+  float loss = 0.f;
+  float4 stats = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (used_entries(A, row) != 0 && w != 0.f) {
+    const RowSums s = row_sums(join_parts(parts + row * chunks, chunks, A.a), A, row);
+    loss = s.loss * w * (A.temperature * A.temperature);
+    stats = make_float4(s.rm, s.rs, s.zm, s.zs);
+  }
+  if (threadIdx.x == 0) {
+    A.loss[row] = loss;
+    if (A.stats != nullptr) A.stats[row] = stats;
+  }
+}
+
+// Gradient of one chunk (blockIdx.y of gridDim.y) of a row, from the saved
+// sums or (parts != nullptr) from the parts of the row, then with the loss.
+template <typename T, int TPB, int NV>
+__global__ __launch_bounds__(TPB) void k_distill_grad(DistillArgs A, const Part* parts) {
+  constexpr int N = Span<T>::N, NW = TPB / 64;
+  __shared__ ListLds list;
+  __shared__ float2 red[NW];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t row = blockIdx.x;
+  T* grad = static_cast<T*>(A.grad) + row * A.gld;
+  const int cnt = used_entries(A, row);
   const float w = A.weight != nullptr ? A.weight[row] : 1.f;
   if (cnt == 0 || w == 0.f) {
-    for (int i = tid; i < A.V; i += kNT) g[i] = (T)0.f;
+    zero_row<T, TPB>(grad, A.V, (int)blockIdx.y, (int)gridDim.y);
+    if (parts != nullptr && blockIdx.y == 0 && tid == 0) A.loss[row] = 0.f;
     return;
   }
-  uint32_t bits = 0u;
+  const Span<T> s(static_cast<const T*>(A.z) + row * A.ld, A.V);
+  const int v0 = (int)blockIdx.y * (TPB * NV);
+  const bool edges = blockIdx.y == 0;
+  const T* type = nullptr;
+  uint4 r[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    r[i] = v < s.nvec ? load16(s.vec(v)) : none_of(type);
+  }
+  const float ex = edges && tid < s.extras ? (float)s.p[s.extra(tid)] : -kInf;
+  // the list: this chunk's words with their logits, and the teacher's sum
   LogSum teach;
-  for (int j = tid; j < cnt; j += kNT) {
-    if (!entry_ok(idx, j, A.V, &bits)) continue;
-    const float t = load_val(A.val, A.val_format, row * A.k + j);
-    teach.add(t, A.a);
+  uint32_t bits = 0u;
+  const int32_t* idx = A.idx + row * A.k;
+  for (int j = tid; j < cnt; j += TPB) {
+    const bool ok = entry_ok(idx, j, A.V, &bits);
+    bool mine = false;
+    float t = 0.f, z = 0.f;
+    if (ok) {
+      const int e = idx[j] - s.head;
+      mine = e < 0 || e >= s.nvec * N ? edges : e / N >= v0 && e / N < v0 + TPB * NV;
+      t = load_val(A.val, A.val_format, row * A.k + j);
+      teach.add(t, A.a);
+      if (mine) z = (float)s.p[idx[j]];
+    }
+    list.word[j] = mine ? idx[j] : -1;
+    list.t[j] = t;
+    list.z[j] = z;
   }
-  raise_status(A.status, bits);
-  teach = block_join<kNT>(teach, A.a, red);
-  const Teacher t = teacher_of(teach, A, row);
-  const float4 st = A.stats[row];  // rest (m, S), listed (m, S)
-  const float top = st.x > st.z ? st.x : st.z;
-  const float s_rest = rescale(st.x, top, A.a), s_list = rescale(st.z, top, A.a);
-  const float total = st.y * s_rest + st.w * s_list;
-  const float inv = 1.f / total;
+  if (blockIdx.y == 0 && parts == nullptr) raise_status(A.status, bits);
+  RowSums sums;
+  if (parts != nullptr) {
+    sums = row_sums(join_parts(parts + row * gridDim.y, (int)gridDim.y, A.a), A, row);
+    if (blockIdx.y == 0 && tid == 0) A.loss[row] = sums.loss * w * (A.temperature * A.temperature);
+    __syncthreads();
+  } else {
+    const float tm = wave_max(teach.m);
+    const float ts = wave_sum(join_sum(teach.m, teach.S, tm, A.a));
+    if (lane == 0) red[tid >> 6] = make_float2(tm, ts);
+    __syncthreads();
+    const float2 o = red[lane < NW ? lane : 0];
+    teach.m = wave_max(o.x);
+    teach.S = wave_sum(lane < NW ? join_sum(o.x, o.y, teach.m, A.a) : 0.f);
+    const float4 st = A.stats[row];
+    sums.t = teacher_of(teach, A, row);
+    sums.rm = st.x;
+    sums.rs = st.y;
+    sums.zm = st.z;
+    sums.zs = st.w;
+  }
   const float up = w * A.temperature * (A.dloss != nullptr ? A.dloss[row] : 1.f);
-  // q_i (1 - p_r / q_r) = 2^((x - m) a) (s_rest / total - p_r / S)
-  float coef = s_rest * inv - (t.p_rest > 0.f && st.y > 0.f ? t.p_rest / st.y : 0.f);
-  coef *= up;
-  if (!(total > 0.f) || !has_mass(t)) coef = __uint_as_float(0x7FC00000u);
-  for (int j = tid; j < cnt; j += kNT) {
-    uint32_t ignore = 0u;
-    if (!entry_ok(idx, j, A.V, &ignore)) continue;
-    const float v = load_val(A.val, A.val_format, row * A.k + j);
-    const float pj = teacher_prob(v, A.a, t);
-    const float z = load1(p, idx[j]);
-    const float q = z == -kInf ? 0.f * inv : exp2_((z - st.z) * A.a) * (s_list * inv);
-    patch[j] = up * (q - pj);
+  const GradScale g = grad_scale(sums, A, up);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    float x[N];
+    unpack(r[i], x, type);
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n] = exp2_((x[n] - g.rm) * A.a) * g.rest;
+    if (v < s.nvec) store16(grad + s.head + (int64_t)v * N, pack(x, type));
   }
+  if (edges && tid < s.extras) grad[s.extra(tid)] = (T)(exp2_((ex - g.rm) * A.a) * g.rest);
   __syncthreads();
-  const float m = st.x == -kInf ? 0.f : st.x;
-  for (int i = tid; i < A.V; i += kNT)
-    g[i] = (T)(exp2_((load1(p, i) - m) * A.a) * coef);
-  __syncthreads();
-  for (int j = tid; j < cnt; j += kNT) {
-    uint32_t ignore = 0u;
-    if (entry_ok(idx, j, A.V, &ignore)) g[idx[j]] = (T)patch[j];
-  }
+  for (int j = tid; j < cnt; j += TPB)
+    if (list.word[j] >= 0)
+      grad[list.word[j]] = (T)(exp2_((list.z[j] - g.zm) * A.a) * g.list -
+                               teacher_prob(list.t[j], A.a, sums.t) * g.up);
 }
 
 // ----------------------------------------------------------------------------
@@ -536,23 +950,81 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
   });
 }
 
-hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t s) {
+// Registers hold a row of up to 16 vectors for each of 1,024 threads.
+constexpr int kRowVecs = 1024 * 16;
+constexpr int kChunkVecs = 256 * 8;
+
+int distill_chunks(int64_t V, int32_t dtype) {
+  const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
+  return vecs <= kRowVecs ? 1 : (int)((vecs + kChunkVecs - 1) / kChunkVecs);
+}
+
+namespace {
+
+template <typename T, int MODE>
+void launch_row(const DistillArgs& a, hipStream_t s) {
+  const int vecs = a.V / Span<T>::N;
+  const dim3 grid((unsigned)a.rows);
+  if (vecs <= 256 * 4)
+    k_distill_row<T, 256, 4, MODE><<<grid, 256, 0, s>>>(a, nullptr);
+  else if (vecs <= 256 * 8)
+    k_distill_row<T, 256, 8, MODE><<<grid, 256, 0, s>>>(a, nullptr);
+  else if (vecs <= 256 * 16)
+    k_distill_row<T, 256, 16, MODE><<<grid, 256, 0, s>>>(a, nullptr);
+  else if (vecs <= 512 * 16)
+    k_distill_row<T, 512, 16, MODE><<<grid, 512, 0, s>>>(a, nullptr);
+  else
+    k_distill_row<T, 1024, 16, MODE><<<grid, 1024, 0, s>>>(a, nullptr);
+}
+
+template <typename T>
+void launch_parts(const DistillArgs& a, Part* parts, int chunks, hipStream_t s) {
+  k_distill_row<T, 256, 8, kPart>
+      <<<dim3((unsigned)a.rows, (unsigned)chunks), 256, 0, s>>>(a, parts);
+}
+
+template <typename T>
+void launch_grad(const DistillArgs& a, const Part* parts, hipStream_t s) {
+  const int vecs = a.V / Span<T>::N;
+  const int chunks = vecs > kChunkVecs ? (vecs + kChunkVecs - 1) / kChunkVecs : 1;
+  k_distill_grad<T, 256, 8><<<dim3((unsigned)a.rows, (unsigned)chunks), 256, 0, s>>>(a, parts);
+}
+
+}  // namespace
+
+hipError_t launch_distill_forward(const DistillArgs& a, void* ws, hipStream_t s) {
+  const int chunks = distill_chunks(a.V, a.dtype);
+  Part* parts = static_cast<Part*>(ws);
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;
-    k_distill_loss<T><<<dim3((unsigned)a.rows), dim3(kNT), 0, s>>>(a);
+    if (chunks == 1) {
+      launch_row<T, kLoss>(a, s);
+    } else {
+      launch_parts<T>(a, parts, chunks, s);
+      k_distill_join<<<dim3((unsigned)a.rows), 64, 0, s>>>(a, parts, chunks);
+    }
   });
 }
 
 hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s) {
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;
-    k_distill_grad<T><<<dim3((unsigned)a.rows), dim3(kNT), 0, s>>>(a);
+    launch_grad<T>(a, nullptr, s);
   });
 }
 
-hipError_t launch_distill_step(const DistillArgs& a, hipStream_t s) {
-  const hipError_t e = launch_distill_forward(a, s);
-  return e != hipSuccess ? e : launch_distill_backward(a, s);
+hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
+  const int chunks = distill_chunks(a.V, a.dtype);
+  Part* parts = static_cast<Part*>(ws);
+  return by_dtype(a.dtype, [&](auto* t) {
+    using T = typename Pointee<decltype(t)>::type;
+    if (chunks == 1) {
+      launch_row<T, kStep>(a, s);
+    } else {
+      launch_parts<T>(a, parts, chunks, s);
+      launch_grad<T>(a, parts, s);
+    }
+  });
 }
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {

@@ -186,8 +186,9 @@ int tkef_distill_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dty
   p->dtype = dtype;
   p->val_format = val_format;
   p->temperature = temperature;
-  // the step's sums, between its two kernels
-  p->ws_bytes = (((size_t)rows * sizeof(float4)) + 255) & ~(size_t)255;
+  const int chunks = tkef::distill_chunks(vocab, dtype);
+  if (chunks > 1)
+    p->ws_bytes = ((size_t)rows * (size_t)chunks * tkef::kPartBytes + 255) & ~(size_t)255;
   *plan_out = p;
   return TKEF_OK;
 }
@@ -219,7 +220,7 @@ int tkef_distill_forward(tkef_distill_plan plan, const void* logits, int64_t row
       distill_args(*plan, logits, row_stride, rows, idx, val, tail, count, weight, status);
   a.loss = loss;
   a.stats = reinterpret_cast<float4*>(stats);
-  return done(tkef::launch_distill_forward(a, stream));
+  return done(tkef::launch_distill_forward(a, ws, stream));
 }
 
 int tkef_distill_backward(tkef_distill_plan plan, const void* logits, int64_t row_stride,
@@ -260,10 +261,9 @@ int tkef_distill_step(tkef_distill_plan plan, const void* logits, int64_t row_st
   tkef::DistillArgs a =
       distill_args(*plan, logits, row_stride, rows, idx, val, tail, count, weight, status);
   a.loss = loss;
-  a.stats = static_cast<float4*>(ws);
   a.grad = grad;
   a.gld = grad_stride;
-  return done(tkef::launch_distill_step(a, stream));
+  return done(tkef::launch_distill_step(a, ws, stream));
 }
 
 int tkef_verify_plan_create(int64_t batch, int64_t draft, int64_t vocab, int32_t dtype,

@@ -57,7 +57,9 @@ struct VerifyArgs {
   uint32_t* status;       // may be null
 };
 
-hipError_t launch_top(const TopArgs& a, hipStream_t s);
+// Bytes of ws that launch_top uses (0: rows short enough for one workgroup).
+size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype);
+hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s);
 // A row that is too long for one workgroup's registers is taken in this many
 // chunks (1: whole); ws then holds kPartBytes for each.
 constexpr size_t kPartBytes = 32;

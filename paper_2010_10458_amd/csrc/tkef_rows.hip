@@ -274,88 +274,384 @@ __device__ __forceinline__ float wave_sum(float x) {
 constexpr int kNT = 256;
 
 // ----------------------------------------------------------------------------
-// top logits, one workgroup per row: radix select of the k-th largest order
-// key over four 8-bit digits, then the ordered compaction and the rest's sum.
-// Takes any row; reads it seven times.
-template <typename T>
-__global__ __launch_bounds__(kNT) void k_top_radix(TopArgs A) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t red[kNT / 64];
-  __shared__ float fred[kNT / 64];
-  __shared__ uint32_t pick[2];
+// top logits
+
+constexpr uint32_t kNaNBits = 0x7FC00000u;
+
+// What a selection writes to. A whole row's results are the caller's; a row
+// too long for one workgroup is selected in chunks, each writing its own list
+// and its rest as a pair, and the lists of a row, one after the other, are
+// then selected from like a row of logits.
+struct TopStage {
+  float* list_val;     // rows x chunks x k
+  int32_t* list_word;
+  float2* rests;       // rows x chunks: (m, S)
+  int32_t chunks;
+};
+enum { kWhole = 0, kChunk = 1, kLists = 2 };
+
+template <int STAGE>
+__device__ __forceinline__ void put_pair(const TopArgs& A, const TopStage& G, int64_t row,
+                                         int chunk, uint32_t pos, int32_t word, float x) {
+  if constexpr (STAGE == kChunk) {
+    const int64_t o = (row * G.chunks + chunk) * A.k + pos;
+    G.list_word[o] = word;
+    G.list_val[o] = x;
+  } else {
+    const int64_t o = row * A.k + pos;
+    A.idx[o] = STAGE == kLists ? G.list_word[row * A.ld + word] : word;
+    if (A.val_format == TKEF_VAL_F16)
+      static_cast<_Float16*>(A.val)[o] = (_Float16)x;
+    else
+      static_cast<float*>(A.val)[o] = x;
+  }
+}
+
+// The rest of a selection: S * 2^(m a), by one thread.
+template <int STAGE>
+__device__ __forceinline__ void put_rest(const TopArgs& A, const TopStage& G, int64_t row,
+                                         int chunk, float m, float S) {
+  if constexpr (STAGE == kChunk) {
+    G.rests[row * G.chunks + chunk] = make_float2(m, S);
+  } else {
+    if (A.tail == nullptr) return;
+    bool nan = S != S;
+    if constexpr (STAGE == kLists) {
+      for (int c = 0; c < G.chunks; ++c) {
+        const float2 r = G.rests[row * G.chunks + c];
+        const float top = fmaxf(m, r.x);
+        if (top != kInf) S = S * rescale(m, top, A.a) + r.y * rescale(r.x, top, A.a);
+        m = top;
+        nan |= r.y != r.y;
+      }
+    }
+    A.tail[row] = nan ? __uint_as_float(kNaNBits)
+                      : m == kInf ? kInf : S > 0.f ? m * A.inv_t + kLn2 * log2_(S) : -kInf;
+  }
+}
+
+struct RadixLds {
+  uint32_t hist[256];
+  uint32_t red[16];
+  float fred[16];
+  uint32_t pick[2];
+};
+
+// Selection among words [e0, e1) of a row that takes any values: radix select
+// of the k-th largest order key over four 8-bit digits, then the ordered
+// compaction and the rest's sum. Seven passes over the words; the kernel below
+// comes here with rows whose words nearly all tie (constant rows, rows with few
+// words left unmasked), rows with NaN, and rows whose rest lies more than 2^-60
+// below their k-th word.
+template <typename T, int NT, int STAGE>
+__device__ __forceinline__ void top_radix(const TopArgs& A, const TopStage& G, RadixLds& L,
+                                       const T* p, int e0, int e1, int64_t row, int chunk) {
   const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  const T* p = static_cast<const T*>(A.z) + row * A.ld;
-  const int V = A.V;
-  uint32_t prefix = 0u, need = (uint32_t)A.k;
+  uint32_t prefix = 0u;
+  uint32_t need = (uint32_t)(A.k < e1 - e0 ? A.k : e1 - e0);
+  const uint32_t taken = need;
   for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[tid] = 0u;
+    if (tid < 256) L.hist[tid] = 0u;
     __syncthreads();
-    for (int i = tid; i < V; i += kNT) {
+    for (int i = e0 + tid; i < e1; i += NT) {
       const uint32_t key = order_key(load1(p, i));
       if (shift == 24 || (key >> (shift + 8)) == prefix)
-        atomicAdd(&hist[(key >> shift) & 255u], 1u);
+        atomicAdd(&L.hist[(key >> shift) & 255u], 1u);
     }
     __syncthreads();
     // digit 255 - tid: the exclusive prefix counts the keys in higher digits
-    const uint32_t mine = hist[255 - tid];
+    const uint32_t mine = tid < 256 ? L.hist[255 - tid] : 0u;
     uint32_t total;
-    const uint32_t above = block_scan<kNT>(mine, red, &total);
+    const uint32_t above = block_scan<NT>(mine, L.red, &total);
     if (above < need && need <= above + mine) {
-      pick[0] = 255u - (uint32_t)tid;
-      pick[1] = need - above;
+      L.pick[0] = 255u - (uint32_t)tid;
+      L.pick[1] = need - above;
     }
     __syncthreads();
-    prefix = (prefix << 8) | pick[0];
-    need = pick[1];
+    prefix = (prefix << 8) | L.pick[0];
+    need = L.pick[1];
   }
   // the k-th key, and how many of its class are taken (the lowest words)
   const uint32_t kth = prefix, quota = need;
   uint32_t done_gt = 0u, done_eq = 0u;
   float top = -kInf;
-  bool nan = false;
-  for (int base = 0; base < V; base += kNT) {
+  int nan = 0;
+  for (int base = e0; base < e1; base += NT) {
     const int i = base + tid;
-    const float x = i < V ? load1(p, i) : 0.f;
-    const uint32_t key = i < V ? order_key(x) : 0u;
-    const bool gt = i < V && key > kth, eq = i < V && key == kth;
-    uint32_t tot_gt, tot_eq;
-    const uint32_t r_gt = done_gt + block_scan<kNT>(gt, red, &tot_gt);
-    const uint32_t r_eq = done_eq + block_scan<kNT>(eq, red, &tot_eq);
-    const bool take = gt || (eq && r_eq < quota);
-    if (take) {
-      const int64_t o = row * A.k + r_gt + (r_eq < quota ? r_eq : quota);
-      A.idx[o] = i;
-      if (A.val_format == TKEF_VAL_F16)
-        static_cast<_Float16*>(A.val)[o] = (_Float16)x;
-      else
-        static_cast<float*>(A.val)[o] = x;
-    } else if (i < V) {
+    const float x = i < e1 ? load1(p, i) : 0.f;
+    const uint32_t key = i < e1 ? order_key(x) : 0u;
+    const bool gt = i < e1 && key > kth, eq = i < e1 && key == kth;
+    uint32_t total;
+    // (both counts in one scan: at most 1,024 of each in a round)
+    const uint32_t before =
+        block_scan<NT>((gt ? 1u : 0u) | (eq ? 1u << 16 : 0u), L.red, &total);
+    const uint32_t r_gt = done_gt + (before & 0xFFFFu), r_eq = done_eq + (before >> 16);
+    if (gt || (eq && r_eq < quota))
+      put_pair<STAGE>(A, G, row, chunk, r_gt + (r_eq < quota ? r_eq : quota), i, x);
+    else if (i < e1)
       top = x > top ? x : top;
-    }
-    nan |= i < V && x != x;
-    done_gt += tot_gt;
-    done_eq += tot_eq;
+    nan |= i < e1 && x != x;
+    done_gt += total & 0xFFFFu;
+    done_eq += total >> 16;
   }
+  if constexpr (STAGE == kChunk)
+    for (uint32_t j = taken + tid; j < (uint32_t)A.k; j += NT)
+      put_pair<STAGE>(A, G, row, chunk, j, e1 - 1, -kInf);
   nan = __syncthreads_or(nan);
   if (nan && tid == 0) raise_status(A.status, TKEF_STATUS_NAN);
-  if (A.tail == nullptr) return;
-  top = block_reduce<kNT>(top, fred, MaxOp());
+  top = block_reduce<NT>(top, L.fred, MaxOp());
   const float m = top == -kInf ? 0.f : top;
   float sum = 0.f;
-  for (int i = tid; i < V; i += kNT) {
+  for (int i = e0 + tid; i < e1; i += NT) {
     const float x = load1(p, i);
     if (order_key(x) < kth) sum += exp2_((x - m) * A.a);
   }
-  sum = block_reduce<kNT>(sum, fred, AddOp());
+  sum = block_reduce<NT>(sum, L.fred, AddOp());
   if (tid == 0) {
     // the class of the k-th key that was not taken
     const float tie = key_value(kth);
     if (done_eq > quota && tie > -kInf)
       sum += (float)(done_eq - quota) * exp2_((tie - m) * A.a);
-    const float tail = top == kInf ? kInf : sum > 0.f ? m * A.inv_t + kLn2 * log2_(sum) : -kInf;
-    A.tail[row] = nan ? __uint_as_float(0x7FC00000u) : tail;
+    if (top == kInf) sum = 1.f;
+    put_rest<STAGE>(A, G, row, chunk, nan ? 0.f : top, nan ? __uint_as_float(kNaNBits) : sum);
   }
+}
+
+// Smallest difference of two order keys of a type's values.
+__device__ __forceinline__ uint32_t key_step(const float*) { return 1u; }
+__device__ __forceinline__ uint32_t key_step(const _Float16*) { return 1u << 13; }
+__device__ __forceinline__ uint32_t key_step(const __bf16*) { return 1u << 16; }
+
+// One workgroup selects from a row (or a chunk of one) that it holds in
+// registers, NV vectors a thread.
+//   1. Each thread's maximum over each of its SUB shares. The k-th largest of
+//      these TPB * SUB maxima (bisected on order keys by one wave) is at most the
+//      k-th largest word: every selected word is at least that bound, and few
+//      others are (for 64 of 256 shares of 125 words, about 74 in all).
+//   2. One pass over the registers puts the words at or above the bound into
+//      LDS and sums the exponentials of the others.
+//   3. The exact k-th key among those candidates, by bisection again; ties go to
+//      the lower words. A bitmap over the row and its prefix counts give each
+//      selected word its place in ascending order.
+// More candidates than kCap, a NaN (in the sum) or a rest that vanishes beside
+// its bound send the row to top_radix.
+template <typename T, int TPB, int NV, int SUB, int STAGE>
+__global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, TopStage G) {
+  constexpr int N = Span<T>::N, NW = TPB / 64;
+  constexpr int kCap = SUB > 1 ? 8224 : TPB == 256 ? 1024 : 2080;
+  constexpr int kWords = (TPB * NV * N + 28 + 31) / 32;
+  constexpr int kPer = (kWords + TPB - 1) / TPB;
+  constexpr int kGroups = TPB * SUB;
+  __shared__ uint32_t group[kGroups];
+  __shared__ float cand_x[kCap];
+  __shared__ int32_t cand_i[kCap];
+  __shared__ uint32_t bitmap[kPer * TPB];
+  __shared__ uint16_t before[kPer * TPB];
+  __shared__ float red[NW];
+  __shared__ RadixLds radix;
+  __shared__ uint32_t ncand, bound_key, thr_key, thr_count;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x;
+  const int chunk = STAGE == kChunk ? (int)blockIdx.y : 0;
+  const T* type = nullptr;
+  const Span<T> s(static_cast<const T*>(A.z) + row * A.ld, A.V);
+  const int v0 = chunk * (TPB * NV);
+  const bool first = chunk == 0, last = STAGE != kChunk || chunk == G.chunks - 1;
+  const int e0 = first ? 0 : s.head + v0 * N;
+  const int e1 = last ? A.V : s.head + (v0 + TPB * NV) * N;
+  const int k = A.k < e1 - e0 ? A.k : e1 - e0;
+  uint4 r[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    r[i] = v < s.nvec ? load16(s.vec(v)) : none_of(type);
+  }
+  const int xi = s.extra(tid < s.extras ? tid : 0);
+  const bool has_ex = tid < s.extras && xi >= e0 && xi < e1;
+  const float ex = has_ex ? (float)s.p[xi] : -kInf;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) bitmap[i * TPB + tid] = 0u;
+  if (tid == 0) ncand = 0u;
+  // 1. the bound
+#pragma unroll
+  for (int q = 0; q < SUB; ++q) {
+    float m = q == 0 ? ex : -kInf;
+#pragma unroll
+    for (int i = q; i < NV; i += SUB) {
+      float x[N];
+      unpack(r[i], x, type);
+      m = max_of(m, x);
+    }
+    group[q * TPB + tid] = order_key(m);
+  }
+  __syncthreads();
+  if (wave == 0) {
+    uint32_t g[kGroups / 64];
+    uint32_t lo = 0xFFFFFFFFu, hi = 0u;
+#pragma unroll
+    for (int i = 0; i < kGroups / 64; ++i) {
+      g[i] = group[i * 64 + lane];
+      lo = g[i] < lo ? g[i] : lo;
+      hi = g[i] > hi ? g[i] : hi;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      const uint32_t a = __shfl_xor(lo, d), b = __shfl_xor(hi, d);
+      lo = a < lo ? a : lo;
+      hi = b > hi ? b : hi;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi) + 1u;
+    // at least k maxima have keys >= lo, fewer than k have keys >= hi
+    const uint32_t step = key_step(type), enough = (uint32_t)k + ((uint32_t)k >> 3) + 1u;
+    while (hi - lo > step) {
+      const uint32_t mid = lo + (hi - lo) / 2u;
+      uint32_t c = 0u;
+#pragma unroll
+      for (int i = 0; i < kGroups / 64; ++i)
+        c += (uint32_t)__popcll(__ballot(g[i] >= mid));
+      if (c >= (uint32_t)k) {
+        lo = mid;
+        if (c <= enough) break;
+      } else {
+        hi = mid;
+      }
+    }
+    if (lane == 0) bound_key = lo;
+  }
+  __syncthreads();
+  const float bound = key_value(bound_key);
+  // 2. candidates, and the sum of the others
+  const float ref = bound == -kInf ? 0.f : bound;
+  float sum = 0.f;
+  const auto offer = [&](float x, int32_t i) {
+    const uint32_t at = atomicAdd(&ncand, 1u);
+    if (at < (uint32_t)kCap) {
+      cand_x[at] = x;
+      cand_i[at] = i;
+    }
+  };
+  if (has_ex) {
+    if (ex >= bound)
+      offer(ex, xi);
+    else
+      sum = exp2_((ex - ref) * A.a);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    float x[N];
+    renew(r[i]);
+    unpack(r[i], x, type);
+    if (max_of(-kInf, x) >= bound && v < s.nvec) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if (x[n] >= bound) {
+          offer(x[n], s.head + v * N + n);
+          x[n] = -kInf;
+        }
+    }
+    float e = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * A.a);
+    sum += e;
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) red[wave] = sum;
+  __syncthreads();
+  const int C = (int)ncand;
+  sum = wave_sum(lane < NW ? red[lane] : 0.f);
+  bool hard = C > kCap || sum != sum;  // (the same for the whole workgroup)
+  if (!hard) {
+  // 3. the k-th key of the candidates
+  if (wave == 0) {
+    uint32_t lo = bound_key, hi = lo, n_lo = (uint32_t)C;
+    for (int i = lane; i < C; i += 64) {
+      const uint32_t key = order_key(cand_x[i]);
+      hi = key > hi ? key : hi;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      const uint32_t b = __shfl_xor(hi, d);
+      hi = b > hi ? b : hi;
+    }
+    hi = __builtin_amdgcn_readfirstlane(hi) + 1u;
+    // n_lo >= k candidates have keys >= lo, fewer than k have keys >= hi
+    while (n_lo > (uint32_t)k && hi - lo > 1u) {
+      const uint32_t mid = lo + (hi - lo) / 2u;
+      uint32_t c = 0u;
+      for (int i = 0; i < C; i += 64)
+        c += (uint32_t)__popcll(
+            __ballot(i + lane < C && order_key(cand_x[i + lane < C ? i + lane : 0]) >= mid));
+      if (c >= (uint32_t)k) {
+        lo = mid;
+        n_lo = c;
+      } else {
+        hi = mid;
+      }
+    }
+    if (lane == 0) {
+      thr_key = lo;
+      thr_count = n_lo;
+    }
+  }
+  __syncthreads();
+  // all n_lo candidates at or above the threshold, or (ties at it) the ones
+  // above it and the lowest words of those at it
+  const uint32_t thr = thr_key, surplus = thr_count - (uint32_t)k;
+  const float at_thr = key_value(thr), base = at_thr == -kInf ? 0.f : at_thr;
+  float left = 0.f;
+  for (int i = tid; i < C; i += TPB) {
+    const float x = cand_x[i];
+    const int32_t w = cand_i[i];
+    const uint32_t key = order_key(x);
+    bool take = key >= thr;
+    if (surplus != 0u && key == thr) {
+      uint32_t higher = 0u;  // ties at higher words
+      for (int j = 0; j < C; ++j)
+        higher += order_key(cand_x[j]) == thr && cand_i[j] > w ? 1u : 0u;
+      take = higher >= surplus;
+    }
+    if (take)
+      atomicOr(&bitmap[(w - e0) >> 5], 1u << ((w - e0) & 31));
+    else
+      left += exp2_((x - base) * A.a);
+  }
+  left = wave_sum(left);
+  __syncthreads();  // (red is read above)
+  if (lane == 0) red[wave] = left;
+  // prefix counts of the bitmap's words
+  uint32_t mine = 0u, total;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) mine += (uint32_t)__popc(bitmap[tid * kPer + i]);
+  mine = block_scan<TPB>(mine, radix.red, &total);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    before[tid * kPer + i] = (uint16_t)mine;
+    mine += (uint32_t)__popc(bitmap[tid * kPer + i]);
+  }
+  left = wave_sum(lane < NW ? red[lane] : 0.f);
+  // the rest relative to the threshold
+  const float rest = sum * rescale(bound, base, A.a) + left;
+  const bool more = k < e1 - e0;
+  hard = more && !(rest > 0x1p-60f);
+  if (!hard) {
+    __syncthreads();
+    for (int i = tid; i < C; i += TPB) {
+      const int32_t w = cand_i[i] - e0;
+      const uint32_t word = bitmap[w >> 5], bit = 1u << (w & 31);
+      if (word & bit)
+        put_pair<STAGE>(A, G, row, chunk,
+                        before[w >> 5] + (uint32_t)__popc(word & (bit - 1u)), cand_i[i],
+                        cand_x[i]);
+    }
+    if constexpr (STAGE == kChunk)
+      for (int j = k + tid; j < A.k; j += TPB)
+        put_pair<STAGE>(A, G, row, chunk, (uint32_t)j, e1 - 1, -kInf);
+    if (tid == 0) put_rest<STAGE>(A, G, row, chunk, more ? base : -kInf, more ? rest : 0.f);
+  }
+  }
+  if (hard) top_radix<T, TPB, STAGE>(A, G, radix, s.p, e0, e1, row, chunk);
 }
 
 // ----------------------------------------------------------------------------
@@ -943,16 +1239,79 @@ struct Pointee<T*> {
 
 }  // namespace
 
-hipError_t launch_top(const TopArgs& a, hipStream_t s) {
-  return by_dtype(a.dtype, [&](auto* t) {
-    using T = typename Pointee<decltype(t)>::type;
-    k_top_radix<T><<<dim3((unsigned)a.rows), dim3(kNT), 0, s>>>(a);
-  });
-}
-
 // Registers hold a row of up to 16 vectors for each of 1,024 threads.
 constexpr int kRowVecs = 1024 * 16;
 constexpr int kChunkVecs = 256 * 8;
+// the longest row's lists fit the kernel that selects from them
+static_assert((TKEF_ROWS_MAX_VOCAB / 4 + kRowVecs - 1) / kRowVecs * TKEF_ROWS_MAX_K / 4 <= 1024 * 4,
+              "lists of a row's chunks");
+
+int top_chunks(int64_t V, int32_t dtype) {
+  const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
+  return vecs <= kRowVecs ? 1 : (int)((vecs + kRowVecs - 1) / kRowVecs);
+}
+
+size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype) {
+  const int chunks = top_chunks(V, dtype);
+  if (chunks == 1) return 0;
+  return (size_t)rows * (size_t)chunks * (sizeof(float2) + (size_t)k * 8);
+}
+
+namespace {
+
+template <typename T>
+void launch_top_whole(const TopArgs& a, hipStream_t s) {
+  const int vecs = a.V / Span<T>::N;
+  const dim3 grid((unsigned)a.rows);
+  const TopStage g{};
+  if (a.k <= 64 && vecs <= 256 * 16) {
+    if (vecs <= 256 * 4)
+      k_top_row<T, 256, 4, 1, kWhole><<<grid, 256, 0, s>>>(a, g);
+    else
+      k_top_row<T, 256, 16, 1, kWhole><<<grid, 256, 0, s>>>(a, g);
+  } else if (a.k <= 256) {
+    if (vecs <= 1024 * 4)
+      k_top_row<T, 1024, 4, 1, kWhole><<<grid, 1024, 0, s>>>(a, g);
+    else if (vecs <= 1024 * 8)
+      k_top_row<T, 1024, 8, 1, kWhole><<<grid, 1024, 0, s>>>(a, g);
+    else
+      k_top_row<T, 1024, 16, 1, kWhole><<<grid, 1024, 0, s>>>(a, g);
+  } else if (vecs <= 1024 * 4) {
+    k_top_row<T, 1024, 4, 4, kWhole><<<grid, 1024, 0, s>>>(a, g);
+  } else {
+    k_top_row<T, 1024, 16, 4, kWhole><<<grid, 1024, 0, s>>>(a, g);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
+  const int chunks = top_chunks(a.V, a.dtype);
+  return by_dtype(a.dtype, [&](auto* t) {
+    using T = typename Pointee<decltype(t)>::type;
+    if (chunks == 1) {
+      launch_top_whole<T>(a, s);
+      return;
+    }
+    TopStage g{};
+    g.chunks = chunks;
+    g.rests = static_cast<float2*>(ws);
+    g.list_val = reinterpret_cast<float*>(g.rests + a.rows * chunks);
+    g.list_word = reinterpret_cast<int32_t*>(g.list_val + a.rows * chunks * a.k);
+    const dim3 grid((unsigned)a.rows, (unsigned)chunks);
+    TopArgs lists = a;
+    lists.z = g.list_val;
+    lists.ld = (int64_t)chunks * a.k;
+    lists.V = chunks * a.k;
+    if (a.k <= 256) {
+      k_top_row<T, 1024, 16, 1, kChunk><<<grid, 1024, 0, s>>>(a, g);
+      k_top_row<float, 1024, 4, 1, kLists><<<dim3((unsigned)a.rows), 1024, 0, s>>>(lists, g);
+    } else {
+      k_top_row<T, 1024, 16, 4, kChunk><<<grid, 1024, 0, s>>>(a, g);
+      k_top_row<float, 1024, 4, 4, kLists><<<dim3((unsigned)a.rows), 1024, 0, s>>>(lists, g);
+    }
+  });
+}
 
 int distill_chunks(int64_t V, int32_t dtype) {
   const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);

@@ -127,6 +127,7 @@ int tkef_top_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dtype,
   p->dtype = dtype;
   p->val_format = val_format;
   p->temperature = temperature;
+  p->ws_bytes = (tkef::top_workspace(rows, vocab, k, dtype) + 255) & ~(size_t)255;
   *plan_out = p;
   return TKEF_OK;
 }
@@ -167,7 +168,7 @@ int tkef_top_execute(tkef_top_plan plan, const void* logits, int64_t row_stride,
   a.val = val_out;
   a.tail = tail_out;
   a.status = status;
-  return done(tkef::launch_top(a, stream));
+  return done(tkef::launch_top(a, ws, stream));
 }
 
 int tkef_distill_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dtype,

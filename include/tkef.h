@@ -414,7 +414,7 @@ const char *tkef_lars_launch_name(int32_t dense, int32_t i);
  * probabilities are held in binary32 whatever the logits' type; log is the
  * natural logarithm. -inf is a masked word (probability 0).
  *
- * The plans below hold sizes only: no buffer is bound, and a call may give
+ * The plans below hold sizes only, no buffers, and a call may give
  * fewer rows than the plan was created for (0 rows: nothing is launched).
  * Executions are asynchronous, only launch kernels and can be captured into a
  * graph. Limits: rows, V <= 2^20; k <= min(V, 1024); 1 <= draft <= 63;
@@ -429,6 +429,7 @@ const char *tkef_lars_launch_name(int32_t dense, int32_t i);
 #define TKEF_ROWS_MAX_VOCAB (1 << 20)
 #define TKEF_ROWS_MAX_K 1024
 #define TKEF_VERIFY_MAX_DRAFT 63
+#define TKEF_VERIFY_MAX_BATCH 32768
 
 /* ---- top logits -----------------------------------------------------------
  * For each row, with S = the k words first in the order (x descending, word
@@ -529,12 +530,20 @@ int tkef_distill_step(tkef_distill_plan plan, const void *logits, int64_t row_st
  * nothing, and sets TKEF_STATUS_NAN where the result depends on it. */
 typedef struct tkef_verify_plan_s *tkef_verify_plan;
 
-/* Host only. batch: the most sequences of an execution (<= 65536); draft: tokens reserved per
- * sequence. */
+/* Host only. batch: the most sequences of an execution (<= 32768); draft: tokens
+ * reserved per sequence. batch * (draft + 1) rows may hold at most 2^21 pieces
+ * of 64 KB (each row at least one; TKEF_ERANGE otherwise). */
 int tkef_verify_plan_create(int64_t batch, int64_t draft, int64_t vocab, int32_t dtype,
                             double temperature, tkef_verify_plan *plan_out);
 int tkef_verify_plan_destroy(tkef_verify_plan plan);
 int tkef_verify_plan_info(tkef_verify_plan plan, size_t *workspace_bytes);
+
+/* Readies a workspace for the plan's executions: clears its counters on
+ * `stream` (asynchronous). Every execution leaves them cleared, so a workspace
+ * is bound once; a plan may have several (one for each stream that it runs
+ * on). A workspace that another call has written must be bound again. */
+int tkef_verify_plan_bind(tkef_verify_plan plan, void *ws, size_t ws_bytes,
+                          hipStream_t stream);
 
 /* target: device; sequence b's row i at target + b * target_batch_stride + i *
  * target_stride (elements), draft + 1 rows each; drafts: likewise, draft rows

@@ -129,6 +129,7 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         "tkef_verify_plan_create": ([i64, i64, i64, i32, f64, P(vp)], ctypes.c_int),
         "tkef_verify_plan_destroy": ([vp], ctypes.c_int),
         "tkef_verify_plan_info": ([vp, P(sz)], ctypes.c_int),
+        "tkef_verify_plan_bind": ([vp, vp, sz, vp], ctypes.c_int),
         "tkef_verify_execute": ([vp, vp, i64, i64, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp,
                                  vp, vp, vp, sz, vp, vp], ctypes.c_int),
     }
@@ -706,5 +707,5 @@ def sparse_aggregate(outs: Sequence[torch.Tensor], idx: torch.Tensor, val: torch
 
 
 from .rows import (DTYPE_BF16, DTYPE_F16, DTYPE_F32, ROWS_MAX_K, ROWS_MAX_ROWS,  # noqa: E402,F401
-                   ROWS_MAX_VOCAB, VERIFY_MAX_DRAFT, DistillPlan, TopLogitsPlan, VerifyPlan,
-                   distill_step, top_logits, verify_draft)
+                   ROWS_MAX_VOCAB, VERIFY_MAX_BATCH, VERIFY_MAX_DRAFT, DistillPlan, TopLogitsPlan,
+                   VerifyPlan, distill_step, top_logits, verify_draft)

@@ -67,6 +67,23 @@ int distill_chunks(int64_t V, int32_t dtype);
 hipError_t launch_distill_forward(const DistillArgs& a, void* ws, hipStream_t s);
 hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s);
 hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s);
-hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
+// Offsets into a verification's workspace. Everything below `zeroed` is zero
+// between executions.
+struct VerifyLayout {
+  size_t best, rejected, raced, arrived, zeroed, sums, parts, bytes;
+};
+// Whether the grid over places and units of 64 KB stays within a launch's limits.
+bool verify_fits(int64_t batch, int64_t draft, int64_t V, int32_t dtype);
+VerifyLayout verify_layout(int64_t batch, int64_t draft, int64_t V, int32_t dtype);
+
+struct VerifyScratch {
+  uint64_t* best;       // per sequence: the race's best key of the residual, of the target
+  uint32_t* rejected;   // per sequence: 64 - place of the first rejection, 0: none
+  uint32_t* raced;      // per sequence: chunks of the race that have ended
+  uint32_t* arrived;    // per sequence and place: chunks of the sums that have ended
+  float4* sums;         // per sequence and place: target (m, S), draft (m, S)
+  float4* parts;        // per sequence, place and chunk: the same of a chunk
+};
+hipError_t launch_verify(const VerifyArgs& a, const VerifyScratch& w, hipStream_t s);
 
 }  // namespace tkef

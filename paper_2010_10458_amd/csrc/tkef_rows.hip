@@ -271,8 +271,6 @@ __device__ __forceinline__ float wave_sum(float x) {
   return (lane_value(x, 15) + lane_value(x, 31)) + (lane_value(x, 47) + lane_value(x, 63));
 }
 
-constexpr int kNT = 256;
-
 // ----------------------------------------------------------------------------
 // top logits
 
@@ -1112,110 +1110,295 @@ __global__ __launch_bounds__(TPB) void k_distill_grad(DistillArgs A, const Part*
 }
 
 // ----------------------------------------------------------------------------
-// verification, one workgroup per sequence, row by row
+// verification
 
-struct Best {
-  float score = 0.f;
-  int word = -1;
-  __device__ void offer(float s, int w) {
-    if (s > score || (s == score && s > 0.f && w < word)) {
-      score = s;
-      word = w;
+// 16 bytes from any address of the element's alignment
+__device__ __forceinline__ uint4 load16_loose(const void* p) {
+  const Loose16 l = *static_cast<const Loose16*>(p);
+  return make_uint4(l.x, l.y, l.z, l.w);
+}
+
+template <typename V>
+__device__ __forceinline__ V agent_load(const V* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename V>
+__device__ __forceinline__ void agent_store(V* p, V v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Counts an arrival at a counter of `of` workgroups; true for the last one,
+// which then sees what the others stored (agent scope) before theirs.
+__device__ __forceinline__ bool arrive_last(uint32_t* ticket, uint32_t of) {
+  return __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
+         of - 1u;
+}
+
+__device__ __forceinline__ int draft_length(const VerifyArgs& A, int64_t b) {
+  if (A.length == nullptr) return A.draft;
+  const int n = A.length[b];
+  return n < 0 ? 0 : n < A.draft ? n : A.draft;
+}
+
+// probability of logit x in a row whose sum is v (a row without words: 0)
+__device__ __forceinline__ float prob(float x, float a, LogSum v) {
+  return v.m == -kInf && v.S == 0.f ? 0.f : exp2_((x - v.m) * a) / v.S;
+}
+
+template <typename T, int NV>
+__device__ __forceinline__ LogSum regs_sum(const uint4 (&r)[NV], float ex, float a) {
+  constexpr int N = Span<T>::N;
+  const T* type = nullptr;
+  LogSum v;
+  v.m = ex;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float x[N];
+    unpack(r[i], x, type);
+    v.m = max_of(v.m, x);
+  }
+  const float ref = v.m == -kInf ? 0.f : v.m;
+  v.S = exp2_((ex - ref) * a);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float x[N];
+    uint4 w = r[i];
+    renew(w);
+    unpack(w, x, type);
+    float e = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * a);
+    v.S += e;
+  }
+  const float m = wave_max(v.m);
+  v.S = wave_sum(join_sum(v.m, v.S, m, a));
+  v.m = m;
+  return v;
+}
+
+// Sums of the rows at one place of a sequence, or of one chunk of them:
+// workgroup (place, sequence, chunk), places outermost. The last chunk to end
+// joins the place's sums and decides about its token; a rejection is posted, and
+// workgroups of later places that start after it leave at once, so a large
+// batch reads little beyond each sequence's first rejection. Nothing waits.
+template <typename T, int TPB, int NV>
+__global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch W, int chunks) {
+  constexpr int NW = TPB / 64;
+  __shared__ float4 red[NW];
+  __shared__ uint32_t posted;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const uint32_t unit = blockIdx.x, chunk = unit % (uint32_t)chunks;
+  const int64_t b = (unit / (uint32_t)chunks) % (uint32_t)A.batch;
+  const int place = (int)(unit / (uint32_t)chunks / (uint32_t)A.batch);
+  const int len = draft_length(A, b);
+  if (place > len) return;
+  if (place > 0) {
+    if (tid == 0) posted = agent_load(&W.rejected[b]);
+    __syncthreads();
+    if (posted > (uint32_t)(TKEF_VERIFY_MAX_DRAFT + 1 - place)) return;
+  }
+  const bool drafted = place < len;
+  const T* type = nullptr;
+  const T* tp = static_cast<const T*>(A.target) + b * A.tb + place * A.ti;
+  const T* dp = static_cast<const T*>(A.drafts) + b * A.db + (drafted ? place : 0) * A.di;
+  const Span<T> ts(tp, A.V), ds(dp, A.V);
+  const int v0 = (int)chunk * (TPB * NV);
+  uint4 r[NV], q[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    r[i] = v < ts.nvec ? load16(ts.vec(v)) : none_of(type);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    q[i] = drafted && v < ds.nvec ? load16(ds.vec(v)) : none_of(type);
+  }
+  const float rx = chunk == 0u && tid < ts.extras ? (float)tp[ts.extra(tid)] : -kInf;
+  const float qx = drafted && chunk == 0u && tid < ds.extras ? (float)dp[ds.extra(tid)] : -kInf;
+  LogSum p = regs_sum<T, NV>(r, rx, A.a), d;
+  if (drafted) d = regs_sum<T, NV>(q, qx, A.a);
+  if (lane == 0) red[tid >> 6] = make_float4(p.m, p.S, d.m, d.S);
+  __syncthreads();
+  if (tid >= 64) return;
+  // the first wave alone from here on
+  float4 s = red[lane < NW ? lane : 0];
+  if (lane >= NW) s.y = s.w = 0.f;
+  const int64_t at = b * (A.draft + 1) + place;
+  if (chunks > 1) {
+    float m0 = wave_max(s.x), m1 = wave_max(s.z);
+    const float s0 = wave_sum(join_sum(s.x, s.y, m0, A.a));
+    const float s1 = wave_sum(join_sum(s.z, s.w, m1, A.a));
+    float* mine = reinterpret_cast<float*>(W.parts + at * chunks + chunk);
+    uint32_t last = 0u;
+    if (lane == 0) {
+      agent_store(mine, m0);
+      agent_store(mine + 1, s0);
+      agent_store(mine + 2, m1);
+      agent_store(mine + 3, s1);
+      last = arrive_last(&W.arrived[at], (uint32_t)chunks) ? 1u : 0u;
+    }
+    if (__builtin_amdgcn_readfirstlane(last) == 0u) return;
+    s = make_float4(-kInf, 0.f, -kInf, 0.f);
+    for (int c = lane; c < chunks; c += 64) {
+      const float* o = reinterpret_cast<const float*>(W.parts + at * chunks + c);
+      const float om = agent_load(o), os = agent_load(o + 1);
+      const float dm = agent_load(o + 2), dS = agent_load(o + 3);
+      m0 = fmaxf(s.x, om);
+      m1 = fmaxf(s.z, dm);
+      s.y = join_sum(s.x, s.y, m0, A.a) + join_sum(om, os, m0, A.a);
+      s.w = join_sum(s.z, s.w, m1, A.a) + join_sum(dm, dS, m1, A.a);
+      s.x = m0;
+      s.z = m1;
     }
   }
-};
+  p.m = wave_max(s.x);
+  p.S = wave_sum(join_sum(s.x, s.y, p.m, A.a));
+  d.m = wave_max(s.z);
+  d.S = wave_sum(join_sum(s.z, s.w, d.m, A.a));
+  if (lane != 0) return;
+  W.sums[at] = make_float4(p.m, p.S, d.m, d.S);
+  if (!drafted) return;
+  const int x = A.tokens[b * A.draft + place];
+  bool ok = x >= 0 && x < A.V;
+  if (ok)
+    ok = A.uniform[b * A.draft + place] * prob((float)dp[x], A.a, d) < prob((float)tp[x], A.a, p);
+  if (!ok)
+    __hip_atomic_fetch_max(&W.rejected[b], (uint32_t)(TKEF_VERIFY_MAX_DRAFT + 1 - place),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
-template <int NT>
-__device__ __forceinline__ Best block_best(Best v, uint64_t* red) {
-  // larger score first, then the lower word
-  uint64_t key = v.word < 0 ? 0ull
-                            : ((uint64_t)__float_as_uint(v.score) << 32) | (0xFFFFFFFFu - v.word);
+// a candidate of the race: larger score first, then the lower word
+__device__ __forceinline__ uint64_t race_key(float score, int word) {
+  return ((uint64_t)__float_as_uint(score) << 32) | (0xFFFFFFFFu - (uint32_t)word);
+}
+
+__device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)key, d);
-    key = o > key ? o : key;
+    const uint64_t o = __shfl_xor((unsigned long long)x, d);
+    x = o > x ? o : x;
   }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = key;
-  __syncthreads();
-  for (int i = 0; i < NT / 64; ++i) key = red[i] > key ? red[i] : key;
-  Best r;
-  if (key != 0ull) {
-    r.score = __uint_as_float((uint32_t)(key >> 32));
-    r.word = (int)(0xFFFFFFFFu - (uint32_t)key);
-  }
-  return r;
+  return x;
 }
 
-// probability of logit x in a row whose sum is v
-__device__ __forceinline__ float prob(float x, float a, LogSum v) {
-  if (v.m == -kInf) return 0.f;  // (an empty row)
-  return exp2_((x - v.m) * a) / v.S;
-}
-
-template <typename T>
-__global__ __launch_bounds__(kNT) void k_verify_rows(VerifyArgs A) {
-  __shared__ float red[kNT / 64];
-  __shared__ uint64_t red64[kNT / 64];
-  const int tid = threadIdx.x;
-  const int64_t b = blockIdx.x;
-  const T* target = static_cast<const T*>(A.target) + b * A.tb;
-  const T* drafts = static_cast<const T*>(A.drafts) + b * A.db;
-  int len = A.draft;
-  if (A.length != nullptr)
-    len = A.length[b] < 0 ? 0 : A.length[b] < A.draft ? A.length[b] : A.draft;
-  int32_t* out = A.tokens_out + b * (A.draft + 1);
-  float* logp = A.logp != nullptr ? A.logp + b * (A.draft + 1) : nullptr;
-  LogSum pt, qt;
-  const T *tp = target, *dp = nullptr;
-  int n = 0;
-  for (;; ++n) {
-    tp = target + n * A.ti;
-    dp = n < len ? drafts + n * A.di : nullptr;
-    pt = LogSum();
-    qt = LogSum();
-    for (int i = tid; i < A.V; i += kNT) {
-      pt.add(load1(tp, i), A.a);
-      if (dp != nullptr) qt.add(load1(dp, i), A.a);
-    }
-    pt = block_join<kNT>(pt, A.a, red);
-    qt = block_join<kNT>(qt, A.a, red);
-    if (n == len) break;
-    const int x = A.tokens[b * A.draft + n];
-    if (x < 0 || x >= A.V) {
-      if (tid == 0) raise_status(A.status, TKEF_STATUS_INDEX_RANGE);
-      break;
-    }
-    const float zt = load1(tp, x);
-    if (!(A.uniform[b * A.draft + n] * prob(load1(dp, x), A.a, qt) < prob(zt, A.a, pt))) break;
-    if (tid == 0) {
-      out[n] = x;
-      if (logp != nullptr)
-        logp[n] = (zt - pt.m) * A.inv_t - kLn2 * log2_(pt.S);
-    }
-  }
-  Best over, plain;
+// The race over one chunk (blockIdx.x) of the row after the accepted tokens of
+// sequence blockIdx.y: the best word of the residual and, in case that is empty,
+// of the target's own probabilities. The last chunk to end writes the
+// sequence's results and leaves its counters at zero.
+template <typename T, int TPB, int NV>
+__global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch W) {
+  constexpr int N = Span<T>::N, NW = TPB / 64;
+  __shared__ uint64_t red[2][NW];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t b = blockIdx.y;
+  const int places = A.draft + 1;
+  const int len = draft_length(A, b);
+  const uint32_t posted = W.rejected[b];
+  const int n = posted != 0u ? TKEF_VERIFY_MAX_DRAFT + 1 - (int)posted : len;
+  const float4 s = W.sums[b * places + n];
+  const bool drafted = n < len;
+  const T* type = nullptr;
+  const T* tp = static_cast<const T*>(A.target) + b * A.tb + n * A.ti;
+  const T* dp = static_cast<const T*>(A.drafts) + b * A.db + (drafted ? n : 0) * A.di;
   const float* noise = A.noise + b * A.noise_ld;
-  for (int i = tid; i < A.V; i += kNT) {
-    const float pi = prob(load1(tp, i), A.a, pt), e = noise[i];
-    const float r = dp != nullptr ? pi - prob(load1(dp, i), A.a, qt) : pi;
-    if (r > 0.f) over.offer(r / e, i);
-    if (pi > 0.f) plain.offer(pi / e, i);
+  const Span<T> ts(tp, A.V);
+  // p = 2^((x - pm) a) * pi; nothing where the row has no words
+  const float pm = s.x == -kInf ? 0.f : s.x, qm = s.z == -kInf ? 0.f : s.z;
+  const float pi = s.y == 0.f ? 0.f : 1.f / s.y, qi = s.w == 0.f ? 0.f : 1.f / s.w;
+  const int v0 = (int)blockIdx.x * (TPB * NV);
+  uint64_t over = 0ull, own = 0ull;
+  const auto offer = [&](float x, float y, float e, int word) {
+    const float p = exp2_((x - pm) * A.a) * pi;
+    const float r = drafted ? p - exp2_((y - qm) * A.a) * qi : p;
+    const float inv = __builtin_amdgcn_rcpf(e);
+    const float so = r * inv, sp = p * inv;
+    if (r > 0.f && so > 0.f) {
+      const uint64_t key = race_key(so, word);
+      over = key > over ? key : over;
+    }
+    if (p > 0.f && sp > 0.f) {
+      const uint64_t key = race_key(sp, word);
+      own = key > own ? key : own;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + tid;
+    if (v < ts.nvec) {
+      const int w = ts.head + v * N;
+      const uint4 r = load16(ts.vec(v));
+      const uint4 q = drafted ? load16_loose(dp + w) : none_of(type);
+      float x[N], y[N], e[N];
+      unpack(r, x, type);
+      unpack(q, y, type);
+#pragma unroll
+      for (int h = 0; h < N; h += 4) {
+        const uint4 u = load16_loose(noise + w + h);
+        e[h] = __uint_as_float(u.x);
+        e[h + 1] = __uint_as_float(u.y);
+        e[h + 2] = __uint_as_float(u.z);
+        e[h + 3] = __uint_as_float(u.w);
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) offer(x[j], y[j], e[j], w + j);
+    }
   }
-  over = block_best<kNT>(over, red64);
-  plain = block_best<kNT>(plain, red64);
-  const int word = over.word >= 0 ? over.word : plain.word;
-  if (tid == 0) {
-    if (pt.S != pt.S || qt.S != qt.S) raise_status(A.status, TKEF_STATUS_NAN);
+  if (blockIdx.x == 0 && tid < ts.extras) {
+    const int w = ts.extra(tid);
+    offer((float)tp[w], drafted ? (float)dp[w] : -kInf, noise[w], w);
+  }
+  over = wave_max64(over);
+  own = wave_max64(own);
+  if (lane == 0) {
+    red[0][tid >> 6] = over;
+    red[1][tid >> 6] = own;
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  over = wave_max64(red[0][lane < NW ? lane : 0]);
+  own = wave_max64(red[1][lane < NW ? lane : 0]);
+  if (gridDim.x > 1) {
+    uint32_t last = 0u;
+    if (lane == 0) {
+      __hip_atomic_fetch_max(&W.best[2 * b], over, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_fetch_max(&W.best[2 * b + 1], own, __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_AGENT);
+      last = arrive_last(&W.raced[b], gridDim.x) ? 1u : 0u;
+    }
+    if (__builtin_amdgcn_readfirstlane(last) == 0u) return;
+    over = agent_load(&W.best[2 * b]);
+    own = agent_load(&W.best[2 * b + 1]);
+  }
+  const uint64_t key = over != 0ull ? over : own;
+  const int word = key != 0ull ? (int)(0xFFFFFFFFu - (uint32_t)key) : -1;
+  if (lane < places) {  // (at most 64)
+    const int i = lane;
+    const int token = i < n ? A.tokens[b * A.draft + i] : i == n ? word : -1;
+    A.tokens_out[b * places + i] = token;
+    if (A.logp != nullptr) {
+      float lp = 0.f;
+      if (token >= 0) {
+        const float4 at = W.sums[b * places + i];
+        const float x = (float)static_cast<const T*>(A.target)[b * A.tb + i * A.ti + token];
+        lp = (x - at.x) * A.inv_t - kLn2 * log2_(at.y);
+      }
+      A.logp[b * places + i] = lp;
+    }
+    agent_store(&W.arrived[b * places + i], 0u);
+  }
+  if (lane == 0) {
     A.accepted[b] = n;
-    out[n] = word;
-    if (logp != nullptr)
-      logp[n] = word < 0 ? 0.f
-                         : (load1(tp, word) - pt.m) * A.inv_t - kLn2 * log2_(pt.S);
-  }
-  for (int i = n + 1 + tid; i <= A.draft; i += kNT) {
-    out[i] = -1;
-    if (logp != nullptr) logp[i] = 0.f;
+    uint32_t bits = s.y != s.y || (drafted && s.w != s.w) ? TKEF_STATUS_NAN : 0u;
+    if (drafted) {
+      const int x = A.tokens[b * A.draft + n];
+      if (x < 0 || x >= A.V) bits |= TKEF_STATUS_INDEX_RANGE;
+    }
+    raise_status(A.status, bits);
+    agent_store(&W.rejected[b], 0u);
+    agent_store(&W.raced[b], 0u);
+    agent_store(&W.best[2 * b], (uint64_t)0);
+    agent_store(&W.best[2 * b + 1], (uint64_t)0);
   }
 }
 
@@ -1386,10 +1569,54 @@ hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
   });
 }
 
-hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
+// Places are summed in units of 1,024 threads x 4 vectors of each row, or of 256
+// x 4 where those would leave compute units idle.
+namespace {
+constexpr int kUnitVecs = 1024 * 4, kSmallVecs = 256 * 4;
+constexpr int64_t kFewUnits = 256;
+
+int64_t ceil_div(int64_t a, int64_t b) { return a <= 0 ? 1 : (a + b - 1) / b; }
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+}  // namespace
+
+bool verify_fits(int64_t batch, int64_t draft, int64_t V, int32_t dtype) {
+  const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
+  return batch * (draft + 1) * ceil_div(vecs, kUnitVecs) <= (int64_t)1 << 21;
+}
+
+VerifyLayout verify_layout(int64_t batch, int64_t draft, int64_t V, int32_t dtype) {
+  const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
+  const int64_t places = batch * (draft + 1), big = ceil_div(vecs, kUnitVecs);
+  // small units serve batches with fewer than kFewUnits big ones
+  const int64_t small = (places * big < kFewUnits ? places * big : kFewUnits) * 4;
+  const int64_t parts = places * big > small ? places * big : small;
+  VerifyLayout l;
+  l.best = 0;
+  l.rejected = up256((size_t)batch * 16);
+  l.raced = l.rejected + up256((size_t)batch * 4);
+  l.arrived = l.raced + up256((size_t)batch * 4);
+  l.zeroed = l.arrived + up256((size_t)places * 4);
+  l.sums = l.zeroed;
+  l.parts = l.sums + up256((size_t)places * sizeof(float4));
+  l.bytes = l.parts + up256((size_t)parts * sizeof(float4));
+  return l;
+}
+
+hipError_t launch_verify(const VerifyArgs& a, const VerifyScratch& w, hipStream_t s) {
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;
-    k_verify_rows<T><<<dim3((unsigned)a.batch), dim3(kNT), 0, s>>>(a);
+    const int64_t vecs = a.V / Span<T>::N, places = (int64_t)a.batch * (a.draft + 1);
+    const int64_t big = ceil_div(vecs, kUnitVecs);
+    if (places * big >= kFewUnits) {
+      k_verify_sums<T, 1024, 4>
+          <<<dim3((unsigned)(places * big)), 1024, 0, s>>>(a, w, (int)big);
+    } else {
+      const int64_t small = ceil_div(vecs, kSmallVecs);
+      k_verify_sums<T, 256, 4>
+          <<<dim3((unsigned)(places * small)), 256, 0, s>>>(a, w, (int)small);
+    }
+    k_verify_race<T, 256, 4>
+        <<<dim3((unsigned)ceil_div(vecs, kSmallVecs), (unsigned)a.batch), 256, 0, s>>>(a, w);
   });
 }
 

@@ -5,6 +5,7 @@
 #include <new>
 
 #include "tkef.h"
+#include "tkef_internal.h"
 #include "tkef_rows.h"
 
 namespace {
@@ -273,7 +274,9 @@ int tkef_verify_plan_create(int64_t batch, int64_t draft, int64_t vocab, int32_t
   *plan_out = nullptr;
   const int rc = check_sizes(batch, vocab, dtype, temperature);
   if (rc != TKEF_OK) return rc;
-  if (batch > 65536 || draft < 1 || draft > TKEF_VERIFY_MAX_DRAFT) return TKEF_ERANGE;
+  if (batch > TKEF_VERIFY_MAX_BATCH || draft < 1 || draft > TKEF_VERIFY_MAX_DRAFT ||
+      !tkef::verify_fits(batch, draft, vocab, dtype))
+    return TKEF_ERANGE;
   tkef_verify_plan p = new (std::nothrow) tkef_verify_plan_s;
   if (p == nullptr) return TKEF_ENOMEM;
   p->rows = batch;
@@ -281,6 +284,7 @@ int tkef_verify_plan_create(int64_t batch, int64_t draft, int64_t vocab, int32_t
   p->vocab = vocab;
   p->dtype = dtype;
   p->temperature = temperature;
+  p->ws_bytes = tkef::verify_layout(batch, draft, vocab, dtype).bytes;
   *plan_out = p;
   return TKEF_OK;
 }
@@ -295,6 +299,17 @@ int tkef_verify_plan_info(tkef_verify_plan plan, size_t* workspace_bytes) {
   if (plan == nullptr) return TKEF_EINVAL;
   if (workspace_bytes != nullptr) *workspace_bytes = plan->ws_bytes;
   return TKEF_OK;
+}
+
+int tkef_verify_plan_bind(tkef_verify_plan plan, void* ws, size_t ws_bytes,
+                          hipStream_t stream) {
+  if (plan == nullptr) return TKEF_EINVAL;
+  const int rc = check_ws(plan->ws_bytes, ws, ws_bytes);
+  if (rc != TKEF_OK) return rc;
+  const tkef::VerifyLayout l =
+      tkef::verify_layout(plan->rows, plan->draft, plan->vocab, plan->dtype);
+  return done(tkef::launch_fill_u32(static_cast<uint32_t*>(ws), 0u, (int64_t)(l.zeroed / 4),
+                                    stream));
 }
 
 int tkef_verify_execute(tkef_verify_plan plan, const void* target, int64_t target_batch_stride,
@@ -343,7 +358,17 @@ int tkef_verify_execute(tkef_verify_plan plan, const void* target, int64_t targe
   a.tokens_out = tokens_out;
   a.logp = logp_out;
   a.status = status;
-  return done(tkef::launch_verify(a, stream));
+  const tkef::VerifyLayout l =
+      tkef::verify_layout(plan->rows, plan->draft, plan->vocab, plan->dtype);
+  char* base = static_cast<char*>(ws);
+  tkef::VerifyScratch w;
+  w.best = reinterpret_cast<uint64_t*>(base + l.best);
+  w.rejected = reinterpret_cast<uint32_t*>(base + l.rejected);
+  w.raced = reinterpret_cast<uint32_t*>(base + l.raced);
+  w.arrived = reinterpret_cast<uint32_t*>(base + l.arrived);
+  w.sums = reinterpret_cast<float4*>(base + l.sums);
+  w.parts = reinterpret_cast<float4*>(base + l.parts);
+  return done(tkef::launch_verify(a, w, stream));
 }
 
 }  // extern "C"

@@ -25,6 +25,7 @@ DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
 ROWS_MAX_ROWS = ROWS_MAX_VOCAB = 1 << 20
 ROWS_MAX_K = 1024
 VERIFY_MAX_DRAFT = 63
+VERIFY_MAX_BATCH = 32768
 
 _DTYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
 
@@ -71,9 +72,13 @@ class _RowPlan:
             return None
         ws = self._ws.get((stream, dev))
         if ws is None:
-            ws = self._ws[(stream, dev)] = torch.empty(self.ws_bytes, dtype=torch.uint8,
-                                                       device=dev)
+            ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+            self._ready(ws, stream)
+            self._ws[(stream, dev)] = ws
         return ws.data_ptr()
+
+    def _ready(self, ws: torch.Tensor, stream: Optional[int]) -> None:
+        """Readies a new workspace on the stream that will use it."""
 
     def _logits(self, x: torch.Tensor, what: str) -> Tuple[int, int]:
         """(rows, row stride) of a 2-D tensor of the plan's type whose rows are
@@ -314,6 +319,10 @@ class VerifyPlan(_RowPlan):
             self.rows, self.draft, self.vocab, _dtype_code(dtype), self.temperature,
             ctypes.byref(self._h)))
         self._info("tkef_verify_plan_info")
+
+    def _ready(self, ws, stream):
+        _check("tkef_verify_plan_bind", lib().tkef_verify_plan_bind(
+            self._h, ws.data_ptr(), ws.numel(), stream))
 
     def _block(self, x: torch.Tensor, places: int, what: str) -> Tuple[int, int]:
         if x.dim() != 3 or x.dtype != self.dtype or not x.is_cuda:

@@ -426,28 +426,47 @@ __device__ __forceinline__ uint32_t key_step(const __bf16*) { return 1u << 16; }
 //      these TPB * SUB maxima (bisected on order keys by one wave) is at most the
 //      k-th largest word: every selected word is at least that bound, and few
 //      others are (for 64 of 256 shares of 125 words, about 74 in all).
-//   2. One pass over the registers puts the words at or above the bound into
-//      LDS and sums the exponentials of the others.
-//   3. The exact k-th key among those candidates, by bisection again; ties go to
-//      the lower words. A bitmap over the row and its prefix counts give each
-//      selected word its place in ascending order.
-// More candidates than kCap, a NaN (in the sum) or a rest that vanishes beside
-// its bound send the row to top_radix.
+//   2. One pass over the registers sums the exponentials of the words below
+//      the bound; a vector with a word at or above it goes to its wave's part of
+//      LDS instead, whose words the wave then sorts into candidates and others.
+//   3. The k first candidates and their places in ascending order: by counting
+//      for each candidate the better ones, then for each selected word the
+//      selected lower words; above kRank candidates the k-th key by bisection
+//      (ties to the lower words), then a bitmap over the row and its prefix
+//      counts.
+// More vectors or candidates than LDS holds, a NaN (in the sum) or a rest that
+// vanishes beside the last selected word send the row to top_radix.
 template <typename T, int TPB, int NV, int SUB, int STAGE>
 __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, TopStage G) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
-  constexpr int kCap = SUB > 1 ? 8224 : TPB == 256 ? 1024 : 2080;
+  constexpr int kCap = SUB > 1 ? 8224 : TPB == 256 ? 1024 : 2080;  // candidates
+  constexpr int kVecs = SUB > 1 ? 160 : TPB == 256 ? 128 : 80;     // vectors of a wave
+  constexpr int kRank = 256;
   constexpr int kWords = (TPB * NV * N + 28 + 31) / 32;
   constexpr int kPer = (kWords + TPB - 1) / TPB;
   constexpr int kGroups = TPB * SUB;
-  __shared__ uint32_t group[kGroups];
-  __shared__ float cand_x[kCap];
-  __shared__ int32_t cand_i[kCap];
-  __shared__ uint32_t bitmap[kPer * TPB];
-  __shared__ uint16_t before[kPer * TPB];
+  // the bitmap and its prefix counts come after the vectors are done with
+  struct Bits {
+    uint32_t map[kPer * TPB];
+    uint16_t before[kPer * TPB];
+  };
+  struct Vecs {
+    uint4 x[NW][kVecs];
+    int32_t word[NW][kVecs];
+  };
+  union Shared {
+    Vecs v;
+    Bits b;
+    uint32_t group[kGroups];
+    RadixLds radix;
+  };
+  __shared__ Shared S;
+  __shared__ __align__(16) uint64_t cand[kCap];  // order key, complement of the word
+  __shared__ __align__(16) int32_t chosen[kRank];
+  __shared__ float others[kRank];
   __shared__ float red[NW];
-  __shared__ RadixLds radix;
-  __shared__ uint32_t ncand, bound_key, thr_key, thr_count;
+  __shared__ uint32_t scan[NW];
+  __shared__ uint32_t ncand, full, bound_key, thr_key, thr_count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
   const int chunk = STAGE == kChunk ? (int)blockIdx.y : 0;
@@ -467,9 +486,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
   const int xi = s.extra(tid < s.extras ? tid : 0);
   const bool has_ex = tid < s.extras && xi >= e0 && xi < e1;
   const float ex = has_ex ? (float)s.p[xi] : -kInf;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) bitmap[i * TPB + tid] = 0u;
-  if (tid == 0) ncand = 0u;
+  if (tid == 0) ncand = full = 0u;
   // 1. the bound
 #pragma unroll
   for (int q = 0; q < SUB; ++q) {
@@ -480,7 +497,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
       unpack(r[i], x, type);
       m = max_of(m, x);
     }
-    group[q * TPB + tid] = order_key(m);
+    S.group[q * TPB + tid] = order_key(m);
   }
   __syncthreads();
   if (wave == 0) {
@@ -488,7 +505,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
     uint32_t lo = 0xFFFFFFFFu, hi = 0u;
 #pragma unroll
     for (int i = 0; i < kGroups / 64; ++i) {
-      g[i] = group[i * 64 + lane];
+      g[i] = S.group[i * 64 + lane];
       lo = g[i] < lo ? g[i] : lo;
       hi = g[i] > hi ? g[i] : hi;
     }
@@ -522,134 +539,190 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
   // 2. candidates, and the sum of the others
   const float ref = bound == -kInf ? 0.f : bound;
   float sum = 0.f;
-  const auto offer = [&](float x, int32_t i) {
-    const uint32_t at = atomicAdd(&ncand, 1u);
-    if (at < (uint32_t)kCap) {
-      cand_x[at] = x;
-      cand_i[at] = i;
-    }
-  };
-  if (has_ex) {
-    if (ex >= bound)
-      offer(ex, xi);
-    else
-      sum = exp2_((ex - ref) * A.a);
-  }
+  int held = 0;  // vectors in this wave's part
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int v = v0 + i * TPB + tid;
     float x[N];
     renew(r[i]);
     unpack(r[i], x, type);
-    if (max_of(-kInf, x) >= bound && v < s.nvec) {
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-        if (x[n] >= bound) {
-          offer(x[n], s.head + v * N + n);
-          x[n] = -kInf;
-        }
+    const bool above = max_of(-kInf, x) >= bound && v < s.nvec;
+    const uint64_t who = __ballot(above);
+    if (above) {
+      const int at = held + (int)__builtin_amdgcn_mbcnt_hi(
+                                (uint32_t)(who >> 32),
+                                __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+      if (at < kVecs) {
+        S.v.x[wave][at] = r[i];
+        S.v.word[wave][at] = s.head + v * N;
+      }
     }
+    held += (int)__popcll(who);
     float e = 0.f;
 #pragma unroll
     for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * A.a);
-    sum += e;
+    sum += above ? 0.f : e;
   }
+  if (held > kVecs) {
+    held = 0;
+    if (lane == 0) full = 1u;
+  }
+  // the wave's words: those at or above the bound are candidates
+  const auto sort_out = [&](bool valid, float x, int32_t word) {
+    const bool take = valid && x >= bound;
+    const uint64_t who = __ballot(take);
+    if (who != 0ull) {
+      uint32_t at = 0u;
+      if (lane == 0) at = atomicAdd(&ncand, (uint32_t)__popcll(who));
+      at = __builtin_amdgcn_readfirstlane(at) +
+           __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32),
+                                     __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+      if (take && at < (uint32_t)kCap)
+        cand[at] = ((uint64_t)order_key(x) << 32) | (0xFFFFFFFFu - (uint32_t)word);
+    }
+    if (valid && !take) sum += exp2_((x - ref) * A.a);
+  };
+  for (int i = 0; i < held * N; i += 64) {
+    const int e = i + lane;
+    const bool valid = e < held * N;
+    const int at = valid ? e / N : 0;
+    const float x = (float)reinterpret_cast<const T*>(&S.v.x[wave][at])[e % N];
+    sort_out(valid, x, S.v.word[wave][at] + e % N);
+  }
+  if (wave == 0) sort_out(has_ex, ex, xi);
   sum = wave_sum(sum);
   if (lane == 0) red[wave] = sum;
   __syncthreads();
   const int C = (int)ncand;
   sum = wave_sum(lane < NW ? red[lane] : 0.f);
-  bool hard = C > kCap || sum != sum;  // (the same for the whole workgroup)
-  if (!hard) {
-  // 3. the k-th key of the candidates
-  if (wave == 0) {
-    uint32_t lo = bound_key, hi = lo, n_lo = (uint32_t)C;
-    for (int i = lane; i < C; i += 64) {
-      const uint32_t key = order_key(cand_x[i]);
-      hi = key > hi ? key : hi;
+  bool hard = C > kCap || full != 0u || sum != sum;  // (the same for the whole workgroup)
+  const bool more = k < e1 - e0;
+  const auto word_of = [](uint64_t c) { return (int32_t)(0xFFFFFFFFu - (uint32_t)c); };
+  if (!hard && C <= kRank && C <= TPB) {
+    // 3. by counting: candidate tid, its rank, its place among the selected words
+    const uint64_t mine = tid < C ? cand[tid] : 0ull;
+    int rank = 0;
+    if (wave * 64 < C)
+      for (int j = 0; j < C; ++j) rank += cand[j] > mine ? 1 : 0;
+    const int32_t word = word_of(mine);
+    if (tid < C) {
+      if (rank < k)
+        chosen[rank] = word;
+      else
+        others[rank - k] = key_value((uint32_t)(mine >> 32));
+      if (rank == k - 1) thr_key = (uint32_t)(mine >> 32);
     }
+    __syncthreads();
+    const float at_thr = key_value(thr_key), base = at_thr == -kInf ? 0.f : at_thr;
+    float left = 0.f;
+    for (int j = lane; j < C - k; j += 64) left += exp2_((others[j] - base) * A.a);
+    left = wave_sum(left);
+    // the rest relative to the threshold
+    const float rest = sum * rescale(bound, base, A.a) + left;
+    hard = more && !(rest > 0x1p-60f);
+    if (!hard) {
+      if (wave * 64 < C) {
+        int place = 0;
+        for (int j = 0; j < k; ++j) place += chosen[j] < word ? 1 : 0;
+        if (tid < C && rank < k)
+          put_pair<STAGE>(A, G, row, chunk, (uint32_t)place, word, load1(s.p, word));
+      }
+      if constexpr (STAGE == kChunk)
+        for (int j = k + tid; j < A.k; j += TPB)
+          put_pair<STAGE>(A, G, row, chunk, (uint32_t)j, e1 - 1, -kInf);
+      if (tid == 0) put_rest<STAGE>(A, G, row, chunk, more ? base : -kInf, more ? rest : 0.f);
+    }
+  } else if (!hard) {
+    // 3. the k-th key of the candidates, the bitmap of the selected words
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-      const uint32_t b = __shfl_xor(hi, d);
-      hi = b > hi ? b : hi;
-    }
-    hi = __builtin_amdgcn_readfirstlane(hi) + 1u;
-    // n_lo >= k candidates have keys >= lo, fewer than k have keys >= hi
-    while (n_lo > (uint32_t)k && hi - lo > 1u) {
-      const uint32_t mid = lo + (hi - lo) / 2u;
-      uint32_t c = 0u;
-      for (int i = 0; i < C; i += 64)
-        c += (uint32_t)__popcll(
-            __ballot(i + lane < C && order_key(cand_x[i + lane < C ? i + lane : 0]) >= mid));
-      if (c >= (uint32_t)k) {
-        lo = mid;
-        n_lo = c;
-      } else {
-        hi = mid;
+    for (int i = 0; i < kPer; ++i) S.b.map[i * TPB + tid] = 0u;
+    if (wave == 0) {
+      uint32_t lo = bound_key, hi = lo, n_lo = (uint32_t)C;
+      for (int i = lane; i < C; i += 64) {
+        const uint32_t key = (uint32_t)(cand[i] >> 32);
+        hi = key > hi ? key : hi;
+      }
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) {
+        const uint32_t b = __shfl_xor(hi, d);
+        hi = b > hi ? b : hi;
+      }
+      hi = __builtin_amdgcn_readfirstlane(hi) + 1u;
+      // n_lo >= k candidates have keys >= lo, fewer than k have keys >= hi
+      while (n_lo > (uint32_t)k && hi - lo > 1u) {
+        const uint32_t mid = lo + (hi - lo) / 2u;
+        uint32_t c = 0u;
+        for (int i = 0; i < C; i += 64)
+          c += (uint32_t)__popcll(
+              __ballot(i + lane < C && (uint32_t)(cand[i + lane < C ? i + lane : 0] >> 32) >= mid));
+        if (c >= (uint32_t)k) {
+          lo = mid;
+          n_lo = c;
+        } else {
+          hi = mid;
+        }
+      }
+      if (lane == 0) {
+        thr_key = lo;
+        thr_count = n_lo;
       }
     }
-    if (lane == 0) {
-      thr_key = lo;
-      thr_count = n_lo;
+    __syncthreads();
+    // all n_lo candidates at or above the threshold, or (ties at it) the ones
+    // above it and the lowest words of those at it
+    const uint32_t thr = thr_key, surplus = thr_count - (uint32_t)k;
+    const float at_thr = key_value(thr), base = at_thr == -kInf ? 0.f : at_thr;
+    float left = 0.f;
+    for (int i = tid; i < C; i += TPB) {
+      const uint64_t mine = cand[i];
+      const int32_t w = word_of(mine);
+      const uint32_t key = (uint32_t)(mine >> 32);
+      bool take = key >= thr;
+      if (surplus != 0u && key == thr) {
+        uint32_t higher = 0u;  // ties at higher words
+        for (int j = 0; j < C; ++j)
+          higher += (uint32_t)(cand[j] >> 32) == thr && cand[j] < mine ? 1u : 0u;
+        take = higher >= surplus;
+      }
+      if (take)
+        atomicOr(&S.b.map[(w - e0) >> 5], 1u << ((w - e0) & 31));
+      else
+        left += exp2_((key_value(key) - base) * A.a);
+    }
+    left = wave_sum(left);
+    if (lane == 0) red[wave] = left;
+    __syncthreads();
+    // prefix counts of the bitmap's words
+    uint32_t count = 0u, total;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) count += (uint32_t)__popc(S.b.map[tid * kPer + i]);
+    count = block_scan<TPB>(count, scan, &total);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      S.b.before[tid * kPer + i] = (uint16_t)count;
+      count += (uint32_t)__popc(S.b.map[tid * kPer + i]);
+    }
+    left = wave_sum(lane < NW ? red[lane] : 0.f);
+    const float rest = sum * rescale(bound, base, A.a) + left;
+    hard = more && !(rest > 0x1p-60f);
+    __syncthreads();
+    if (!hard) {
+      for (int i = tid; i < C; i += TPB) {
+        const int32_t word = word_of(cand[i]), w = word - e0;
+        const uint32_t bits = S.b.map[w >> 5], bit = 1u << (w & 31);
+        if (bits & bit)
+          put_pair<STAGE>(A, G, row, chunk,
+                          S.b.before[w >> 5] + (uint32_t)__popc(bits & (bit - 1u)), word,
+                          load1(s.p, word));
+      }
+      if constexpr (STAGE == kChunk)
+        for (int j = k + tid; j < A.k; j += TPB)
+          put_pair<STAGE>(A, G, row, chunk, (uint32_t)j, e1 - 1, -kInf);
+      if (tid == 0) put_rest<STAGE>(A, G, row, chunk, more ? base : -kInf, more ? rest : 0.f);
     }
   }
   __syncthreads();
-  // all n_lo candidates at or above the threshold, or (ties at it) the ones
-  // above it and the lowest words of those at it
-  const uint32_t thr = thr_key, surplus = thr_count - (uint32_t)k;
-  const float at_thr = key_value(thr), base = at_thr == -kInf ? 0.f : at_thr;
-  float left = 0.f;
-  for (int i = tid; i < C; i += TPB) {
-    const float x = cand_x[i];
-    const int32_t w = cand_i[i];
-    const uint32_t key = order_key(x);
-    bool take = key >= thr;
-    if (surplus != 0u && key == thr) {
-      uint32_t higher = 0u;  // ties at higher words
-      for (int j = 0; j < C; ++j)
-        higher += order_key(cand_x[j]) == thr && cand_i[j] > w ? 1u : 0u;
-      take = higher >= surplus;
-    }
-    if (take)
-      atomicOr(&bitmap[(w - e0) >> 5], 1u << ((w - e0) & 31));
-    else
-      left += exp2_((x - base) * A.a);
-  }
-  left = wave_sum(left);
-  __syncthreads();  // (red is read above)
-  if (lane == 0) red[wave] = left;
-  // prefix counts of the bitmap's words
-  uint32_t mine = 0u, total;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) mine += (uint32_t)__popc(bitmap[tid * kPer + i]);
-  mine = block_scan<TPB>(mine, radix.red, &total);
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    before[tid * kPer + i] = (uint16_t)mine;
-    mine += (uint32_t)__popc(bitmap[tid * kPer + i]);
-  }
-  left = wave_sum(lane < NW ? red[lane] : 0.f);
-  // the rest relative to the threshold
-  const float rest = sum * rescale(bound, base, A.a) + left;
-  const bool more = k < e1 - e0;
-  hard = more && !(rest > 0x1p-60f);
-  if (!hard) {
-    __syncthreads();
-    for (int i = tid; i < C; i += TPB) {
-      const int32_t w = cand_i[i] - e0;
-      const uint32_t word = bitmap[w >> 5], bit = 1u << (w & 31);
-      if (word & bit)
-        put_pair<STAGE>(A, G, row, chunk,
-                        before[w >> 5] + (uint32_t)__popc(word & (bit - 1u)), cand_i[i],
-                        cand_x[i]);
-    }
-    if constexpr (STAGE == kChunk)
-      for (int j = k + tid; j < A.k; j += TPB)
-        put_pair<STAGE>(A, G, row, chunk, (uint32_t)j, e1 - 1, -kInf);
-    if (tid == 0) put_rest<STAGE>(A, G, row, chunk, more ? base : -kInf, more ? rest : 0.f);
-  }
-  }
-  if (hard) top_radix<T, TPB, STAGE>(A, G, radix, s.p, e0, e1, row, chunk);
+  if (hard) top_radix<T, TPB, STAGE>(A, G, S.radix, s.p, e0, e1, row, chunk);
 }
 
 // ----------------------------------------------------------------------------

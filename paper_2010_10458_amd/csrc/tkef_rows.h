@@ -82,7 +82,7 @@ struct VerifyScratch {
   uint32_t* raced;      // per sequence: chunks of the race that have ended
   uint32_t* arrived;    // per sequence and place: chunks of the sums that have ended
   float4* sums;         // per sequence and place: target (m, S), draft (m, S)
-  float4* parts;        // per sequence, place and chunk: the same of a chunk
+  float2* parts;        // per sequence, place and chunk: the same of a chunk, as two pairs
 };
 hipError_t launch_verify(const VerifyArgs& a, const VerifyScratch& w, hipStream_t s);
 

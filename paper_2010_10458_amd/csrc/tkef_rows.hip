@@ -232,11 +232,69 @@ __device__ __forceinline__ void renew(uint4& r) {
   asm("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w));
 }
 
+__device__ __forceinline__ int renew(int i) {
+  asm("" : "+v"(i));
+  return i;
+}
+
+// Largest of three without the canonicalizing instructions that fmaxf brings
+// for each operand. A quiet NaN is passed over, a signalling one may win: the
+// sums over the same words carry either.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 template <int N>
 __device__ __forceinline__ float max_of(float m, const float (&x)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; i += 2) m = fmaxf(m, fmaxf(x[i], x[i + 1]));
+  for (int i = 0; i < N; i += 2) m = max3(m, x[i], x[i + 1]);
   return m;
+}
+// the same of a packed vector
+template <typename T>
+__device__ __forceinline__ float max_packed(float m, uint4 r, const T* type) {
+  float x[Span<T>::N];
+  unpack(r, x, type);
+  return max_of(m, x);
+}
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ float max_packed(float m, uint4 r, const _Float16*) {
+  const half2_ h = __builtin_bit_cast(half2_, pk_max(pk_max(r.x, r.y), pk_max(r.z, r.w)));
+  return max3(m, (float)h.x, (float)h.y);
+}
+
+// Vectors v0 + i * TPB + tid of a row; -inf in the places of those it has not.
+// Every load is issued at an address inside the row, so the loads need no
+// execution masks; only the slot that the row ends in is patched.
+template <typename T, int TPB, int NV>
+__device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int v0) {
+  const T* type = nullptr;
+  const int last = s.nvec - 1;
+  if (v0 > last) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) r[i] = none_of(type);
+    return;
+  }
+  const char* base = reinterpret_cast<const char*>(s.p + s.head);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = v0 + i * TPB + (int)threadIdx.x;
+    r[i] = load16(base + (uint32_t)(v < last ? v : last) * 16u);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (v0 + (i + 1) * TPB > s.nvec) {  // (the same for all threads)
+      const bool in = v0 + i * TPB + (int)threadIdx.x < s.nvec;
+      r[i].x = in ? r[i].x : none_of(type).x;
+      r[i].y = in ? r[i].y : none_of(type).y;
+      r[i].z = in ? r[i].z : none_of(type).z;
+      r[i].w = in ? r[i].w : none_of(type).w;
+    }
 }
 
 // Wave reductions over DPP row shifts: lane 15 of each row of 16 lanes ends
@@ -437,11 +495,11 @@ __device__ __forceinline__ uint32_t key_step(const __bf16*) { return 1u << 16; }
 // More vectors or candidates than LDS holds, a NaN (in the sum) or a rest that
 // vanishes beside the last selected word send the row to top_radix.
 template <typename T, int TPB, int NV, int SUB, int STAGE>
-__global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, TopStage G) {
+__global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, TopStage G) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
   constexpr int kCap = SUB > 1 ? 8224 : TPB == 256 ? 1024 : 2080;  // candidates
   constexpr int kVecs = SUB > 1 ? 160 : TPB == 256 ? 128 : 80;     // vectors of a wave
-  constexpr int kRank = 256;
+  constexpr int kRank = TPB == 256 ? 256 : 1024;
   constexpr int kWords = (TPB * NV * N + 28 + 31) / 32;
   constexpr int kPer = (kWords + TPB - 1) / TPB;
   constexpr int kGroups = TPB * SUB;
@@ -478,11 +536,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
   const int e1 = last ? A.V : s.head + (v0 + TPB * NV) * N;
   const int k = A.k < e1 - e0 ? A.k : e1 - e0;
   uint4 r[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
-    r[i] = v < s.nvec ? load16(s.vec(v)) : none_of(type);
-  }
+  load_slots<T, TPB, NV>(r, s, v0);
   const int xi = s.extra(tid < s.extras ? tid : 0);
   const bool has_ex = tid < s.extras && xi >= e0 && xi < e1;
   const float ex = has_ex ? (float)s.p[xi] : -kInf;
@@ -493,9 +547,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
     float m = q == 0 ? ex : -kInf;
 #pragma unroll
     for (int i = q; i < NV; i += SUB) {
-      float x[N];
-      unpack(r[i], x, type);
-      m = max_of(m, x);
+      m = max_packed(m, r[i], type);
     }
     S.group[q * TPB + tid] = order_key(m);
   }
@@ -540,9 +592,10 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
   const float ref = bound == -kInf ? 0.f : bound;
   float sum = 0.f;
   int held = 0;  // vectors in this wave's part
+  const int tid2 = renew(tid);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
+    const int v = v0 + i * TPB + tid2;
     float x[N];
     renew(r[i]);
     unpack(r[i], x, type);
@@ -562,6 +615,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
 #pragma unroll
     for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * A.a);
     sum += above ? 0.f : e;
+    asm volatile("" : "+v"(sum));  // (here, not after the last vector from kept registers)
   }
   if (held > kVecs) {
     held = 0;
@@ -598,11 +652,12 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
   bool hard = C > kCap || full != 0u || sum != sum;  // (the same for the whole workgroup)
   const bool more = k < e1 - e0;
   const auto word_of = [](uint64_t c) { return (int32_t)(0xFFFFFFFFu - (uint32_t)c); };
-  if (!hard && C <= kRank && C <= TPB) {
+  if (!hard && C <= kRank) {
     // 3. by counting: candidate tid, its rank, its place among the selected words
     const uint64_t mine = tid < C ? cand[tid] : 0ull;
     int rank = 0;
     if (wave * 64 < C)
+#pragma unroll 4
       for (int j = 0; j < C; ++j) rank += cand[j] > mine ? 1 : 0;
     const int32_t word = word_of(mine);
     if (tid < C) {
@@ -623,6 +678,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 4 : 1) void k_top_row(TopArgs A, 
     if (!hard) {
       if (wave * 64 < C) {
         int place = 0;
+#pragma unroll 4
         for (int j = 0; j < k; ++j) place += chosen[j] < word ? 1 : 0;
         if (tid < C && rank < k)
           put_pair<STAGE>(A, G, row, chunk, (uint32_t)place, word, load1(s.p, word));
@@ -938,11 +994,7 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
   const bool edges = MODE != kPart || blockIdx.y == 0;
   const T* type = nullptr;
   uint4 r[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
-    r[i] = v < s.nvec ? load16(s.vec(v)) : none_of(type);
-  }
+  load_slots<T, TPB, NV>(r, s, v0);
   float ex = edges && tid < s.extras ? (float)s.p[s.extra(tid)] : -kInf;
   for (int i = tid; i < TPB * NV / 16; i += TPB)
     reinterpret_cast<uint4*>(mark)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -1001,9 +1053,7 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
   for (int i = 0; i < NV; ++i) {
     const uint32_t b = mark[tid * NV + i];
     if (b != 0u) r[i] = strike(r[i], b, type);
-    float x[N];
-    unpack(r[i], x, type);
-    m = max_of(m, x);
+    m = max_packed(m, r[i], type);
   }
   const float ref = m == -kInf ? 0.f : m;
   float sum = exp2_((ex - ref) * A.a);
@@ -1040,9 +1090,10 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
     if constexpr (MODE == kStep) {
       const GradScale g = grad_scale(sums, A, w * A.temperature);
       T* grad = static_cast<T*>(A.grad) + row * A.gld;
+      const int tid2 = renew(tid);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int v = i * TPB + tid;
+        const int v = i * TPB + tid2;
         float x[N];
         renew(r[i]);
         unpack(r[i], x, type);
@@ -1117,11 +1168,7 @@ __global__ __launch_bounds__(TPB) void k_distill_grad(DistillArgs A, const Part*
   const bool edges = blockIdx.y == 0;
   const T* type = nullptr;
   uint4 r[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
-    r[i] = v < s.nvec ? load16(s.vec(v)) : none_of(type);
-  }
+  load_slots<T, TPB, NV>(r, s, v0);
   const float ex = edges && tid < s.extras ? (float)s.p[s.extra(tid)] : -kInf;
   // the list: this chunk's words with their logits, and the teacher's sum
   LogSum teach;
@@ -1165,9 +1212,10 @@ __global__ __launch_bounds__(TPB) void k_distill_grad(DistillArgs A, const Part*
   }
   const float up = w * A.temperature * (A.dloss != nullptr ? A.dloss[row] : 1.f);
   const GradScale g = grad_scale(sums, A, up);
+  const int tid2 = renew(tid);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
+    const int v = v0 + i * TPB + tid2;
     float x[N];
     unpack(r[i], x, type);
 #pragma unroll
@@ -1200,11 +1248,29 @@ __device__ __forceinline__ void agent_store(V* p, V v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Counts an arrival at a counter of `of` workgroups; true for the last one,
-// which then sees what the others stored (agent scope) before theirs.
+// Counts an arrival at a counter of `of` workgroups; true for the last one.
+// What the workgroups tell each other goes through agent-scope atomics alone,
+// which act where all dies see them: the calling lane's own have ended there
+// when its counter of outstanding accesses is zero, so the last arrival's
+// atomic loads find all of them. (An acquire-release arrival would also write
+// back and drop the die's L2, for every workgroup.)
 __device__ __forceinline__ bool arrive_last(uint32_t* ticket, uint32_t of) {
-  return __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
-         of - 1u;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  const uint32_t before =
+      __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("" ::: "memory");
+  return before == of - 1u;
+}
+
+__device__ __forceinline__ void agent_put(float2* p, float a, float b) {
+  (void)__hip_atomic_exchange(
+      reinterpret_cast<unsigned long long*>(p),
+      ((unsigned long long)__float_as_uint(b) << 32) | __float_as_uint(a), __ATOMIC_RELAXED,
+      __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 agent_get(const float2* p) {
+  const unsigned long long u = agent_load(reinterpret_cast<const unsigned long long*>(p));
+  return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
 }
 
 __device__ __forceinline__ int draft_length(const VerifyArgs& A, int64_t b) {
@@ -1225,11 +1291,7 @@ __device__ __forceinline__ LogSum regs_sum(const uint4 (&r)[NV], float ex, float
   LogSum v;
   v.m = ex;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    float x[N];
-    unpack(r[i], x, type);
-    v.m = max_of(v.m, x);
-  }
+  for (int i = 0; i < NV; ++i) v.m = max_packed(v.m, r[i], type);
   const float ref = v.m == -kInf ? 0.f : v.m;
   v.S = exp2_((ex - ref) * a);
 #pragma unroll
@@ -1271,22 +1333,13 @@ __global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch
     if (posted > (uint32_t)(TKEF_VERIFY_MAX_DRAFT + 1 - place)) return;
   }
   const bool drafted = place < len;
-  const T* type = nullptr;
   const T* tp = static_cast<const T*>(A.target) + b * A.tb + place * A.ti;
   const T* dp = static_cast<const T*>(A.drafts) + b * A.db + (drafted ? place : 0) * A.di;
   const Span<T> ts(tp, A.V), ds(dp, A.V);
   const int v0 = (int)chunk * (TPB * NV);
   uint4 r[NV], q[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
-    r[i] = v < ts.nvec ? load16(ts.vec(v)) : none_of(type);
-  }
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
-    q[i] = drafted && v < ds.nvec ? load16(ds.vec(v)) : none_of(type);
-  }
+  load_slots<T, TPB, NV>(r, ts, v0);
+  if (drafted) load_slots<T, TPB, NV>(q, ds, v0);
   const float rx = chunk == 0u && tid < ts.extras ? (float)tp[ts.extra(tid)] : -kInf;
   const float qx = drafted && chunk == 0u && tid < ds.extras ? (float)dp[ds.extra(tid)] : -kInf;
   LogSum p = regs_sum<T, NV>(r, rx, A.a), d;
@@ -1302,25 +1355,22 @@ __global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch
     float m0 = wave_max(s.x), m1 = wave_max(s.z);
     const float s0 = wave_sum(join_sum(s.x, s.y, m0, A.a));
     const float s1 = wave_sum(join_sum(s.z, s.w, m1, A.a));
-    float* mine = reinterpret_cast<float*>(W.parts + at * chunks + chunk);
+    float2* mine = W.parts + 2 * (at * chunks + chunk);
     uint32_t last = 0u;
     if (lane == 0) {
-      agent_store(mine, m0);
-      agent_store(mine + 1, s0);
-      agent_store(mine + 2, m1);
-      agent_store(mine + 3, s1);
+      agent_put(mine, m0, s0);
+      agent_put(mine + 1, m1, s1);
       last = arrive_last(&W.arrived[at], (uint32_t)chunks) ? 1u : 0u;
     }
     if (__builtin_amdgcn_readfirstlane(last) == 0u) return;
     s = make_float4(-kInf, 0.f, -kInf, 0.f);
     for (int c = lane; c < chunks; c += 64) {
-      const float* o = reinterpret_cast<const float*>(W.parts + at * chunks + c);
-      const float om = agent_load(o), os = agent_load(o + 1);
-      const float dm = agent_load(o + 2), dS = agent_load(o + 3);
-      m0 = fmaxf(s.x, om);
-      m1 = fmaxf(s.z, dm);
-      s.y = join_sum(s.x, s.y, m0, A.a) + join_sum(om, os, m0, A.a);
-      s.w = join_sum(s.z, s.w, m1, A.a) + join_sum(dm, dS, m1, A.a);
+      const float2 o = agent_get(W.parts + 2 * (at * chunks + c));
+      const float2 e = agent_get(W.parts + 2 * (at * chunks + c) + 1);
+      m0 = fmaxf(s.x, o.x);
+      m1 = fmaxf(s.z, e.x);
+      s.y = join_sum(s.x, s.y, m0, A.a) + join_sum(o.x, o.y, m0, A.a);
+      s.w = join_sum(s.z, s.w, m1, A.a) + join_sum(e.x, e.y, m1, A.a);
       s.x = m0;
       s.z = m1;
     }
@@ -1357,7 +1407,8 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
 
 // The race over one chunk (blockIdx.x) of the row after the accepted tokens of
 // sequence blockIdx.y: the best word of the residual and, in case that is empty,
-// of the target's own probabilities. The last chunk to end writes the
+// of the target's own probabilities. The noise does not depend on where the
+// drafts ended and is asked for first. The last chunk to end writes the
 // sequence's results and leaves its counters at zero.
 template <typename T, int TPB, int NV>
 __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch W) {
@@ -1366,61 +1417,70 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t b = blockIdx.y;
   const int places = A.draft + 1;
+  // vectors of N words from the row's start (any alignment), the last of them cut
+  const float* noise = A.noise + b * A.noise_ld;
+  const int nvec = A.V / N, v0 = (int)blockIdx.x * (TPB * NV) + tid;
+  uint4 e[NV][N / 4];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (v0 + i * TPB < nvec) {
+#pragma unroll
+      for (int h = 0; h < N / 4; ++h)
+        e[i][h] = load16_loose(noise + (int64_t)(v0 + i * TPB) * N + 4 * h);
+    }
   const int len = draft_length(A, b);
   const uint32_t posted = W.rejected[b];
   const int n = posted != 0u ? TKEF_VERIFY_MAX_DRAFT + 1 - (int)posted : len;
-  const float4 s = W.sums[b * places + n];
   const bool drafted = n < len;
   const T* type = nullptr;
   const T* tp = static_cast<const T*>(A.target) + b * A.tb + n * A.ti;
   const T* dp = static_cast<const T*>(A.drafts) + b * A.db + (drafted ? n : 0) * A.di;
-  const float* noise = A.noise + b * A.noise_ld;
-  const Span<T> ts(tp, A.V);
+  uint4 r[NV], q[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (v0 + i * TPB < nvec) {
+      r[i] = load16_loose(tp + (int64_t)(v0 + i * TPB) * N);
+      if (drafted) q[i] = load16_loose(dp + (int64_t)(v0 + i * TPB) * N);
+    }
+  const float4 s = W.sums[b * places + n];
   // p = 2^((x - pm) a) * pi; nothing where the row has no words
   const float pm = s.x == -kInf ? 0.f : s.x, qm = s.z == -kInf ? 0.f : s.z;
   const float pi = s.y == 0.f ? 0.f : 1.f / s.y, qi = s.w == 0.f ? 0.f : 1.f / s.w;
-  const int v0 = (int)blockIdx.x * (TPB * NV);
-  uint64_t over = 0ull, own = 0ull;
-  const auto offer = [&](float x, float y, float e, int word) {
+  // (a thread meets its words in ascending order: a tie keeps the first)
+  float over_s = 0.f, own_s = 0.f;
+  int over_w = 0, own_w = 0;
+  const auto offer = [&](float x, float y, float noise_of, int word) {
     const float p = exp2_((x - pm) * A.a) * pi;
     const float r = drafted ? p - exp2_((y - qm) * A.a) * qi : p;
-    const float inv = __builtin_amdgcn_rcpf(e);
-    const float so = r * inv, sp = p * inv;
-    if (r > 0.f && so > 0.f) {
-      const uint64_t key = race_key(so, word);
-      over = key > over ? key : over;
-    }
-    if (p > 0.f && sp > 0.f) {
-      const uint64_t key = race_key(sp, word);
-      own = key > own ? key : own;
-    }
+    const float inv = __builtin_amdgcn_rcpf(noise_of);
+    const float so = r > 0.f ? r * inv : 0.f, sp = p > 0.f ? p * inv : 0.f;
+    over_w = so > over_s ? word : over_w;
+    over_s = so > over_s ? so : over_s;
+    own_w = sp > own_s ? word : own_w;
+    own_s = sp > own_s ? sp : own_s;
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid;
-    if (v < ts.nvec) {
-      const int w = ts.head + v * N;
-      const uint4 r = load16(ts.vec(v));
-      const uint4 q = drafted ? load16_loose(dp + w) : none_of(type);
-      float x[N], y[N], e[N];
-      unpack(r, x, type);
-      unpack(q, y, type);
+    const int v = v0 + i * TPB;
+    if (v < nvec) {
+      float x[N], y[N];
+      unpack(r[i], x, type);
+      unpack(drafted ? q[i] : none_of(type), y, type);
 #pragma unroll
-      for (int h = 0; h < N; h += 4) {
-        const uint4 u = load16_loose(noise + w + h);
-        e[h] = __uint_as_float(u.x);
-        e[h + 1] = __uint_as_float(u.y);
-        e[h + 2] = __uint_as_float(u.z);
-        e[h + 3] = __uint_as_float(u.w);
+      for (int j = 0; j < N; ++j) {
+        const uint4 u = e[i][j / 4];
+        const uint32_t w = j % 4 == 0 ? u.x : j % 4 == 1 ? u.y : j % 4 == 2 ? u.z : u.w;
+        offer(x[j], y[j], __uint_as_float(w), v * N + j);
       }
-#pragma unroll
-      for (int j = 0; j < N; ++j) offer(x[j], y[j], e[j], w + j);
     }
   }
-  if (blockIdx.x == 0 && tid < ts.extras) {
-    const int w = ts.extra(tid);
+  const int w = nvec * N + tid;
+  if (blockIdx.x == 0 && w < A.V) {
+    // a word after the vectors, by a thread that has met lower words alone
     offer((float)tp[w], drafted ? (float)dp[w] : -kInf, noise[w], w);
   }
+  uint64_t over = over_s > 0.f ? race_key(over_s, over_w) : 0ull;
+  uint64_t own = own_s > 0.f ? race_key(own_s, own_w) : 0ull;
   over = wave_max64(over);
   own = wave_max64(own);
   if (lane == 0) {
@@ -1671,7 +1731,7 @@ VerifyLayout verify_layout(int64_t batch, int64_t draft, int64_t V, int32_t dtyp
   l.zeroed = l.arrived + up256((size_t)places * 4);
   l.sums = l.zeroed;
   l.parts = l.sums + up256((size_t)places * sizeof(float4));
-  l.bytes = l.parts + up256((size_t)parts * sizeof(float4));
+  l.bytes = l.parts + up256((size_t)parts * 2 * sizeof(float2));
   return l;
 }
 

@@ -367,7 +367,7 @@ int tkef_verify_execute(tkef_verify_plan plan, const void* target, int64_t targe
   w.raced = reinterpret_cast<uint32_t*>(base + l.raced);
   w.arrived = reinterpret_cast<uint32_t*>(base + l.arrived);
   w.sums = reinterpret_cast<float4*>(base + l.sums);
-  w.parts = reinterpret_cast<float4*>(base + l.parts);
+  w.parts = reinterpret_cast<float2*>(base + l.parts);
   return done(tkef::launch_verify(a, w, stream));
 }
 

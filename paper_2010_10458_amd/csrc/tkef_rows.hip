@@ -6,6 +6,8 @@
 // its largest logit: each term is 2^((x - m) a). The difference is taken
 // before the product, so logits at the lowest value of their type (a common
 // mask) neither overflow nor lose their order.
+#include <cmath>
+
 #include <hip/hip_runtime.h>
 
 #include "tkef.h"
@@ -268,11 +270,12 @@ __device__ __forceinline__ float max_packed(float m, uint4 r, const _Float16*) {
   return max3(m, (float)h.x, (float)h.y);
 }
 
-// Vectors v0 + i * TPB + tid of a row; -inf in the places of those it has not.
+// Vectors v0 + i * step + tid of a row; -inf in the places of those it has not.
 // Every load is issued at an address inside the row, so the loads need no
 // execution masks; only the slot that the row ends in is patched.
 template <typename T, int TPB, int NV>
-__device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int v0) {
+__device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int v0,
+                                           int step = TPB) {
   const T* type = nullptr;
   const int last = s.nvec - 1;
   if (v0 > last) {
@@ -283,13 +286,13 @@ __device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int
   const char* base = reinterpret_cast<const char*>(s.p + s.head);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + (int)threadIdx.x;
+    const int v = v0 + i * step + (int)threadIdx.x;
     r[i] = load16(base + (uint32_t)(v < last ? v : last) * 16u);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (v0 + (i + 1) * TPB > s.nvec) {  // (the same for all threads)
-      const bool in = v0 + i * TPB + (int)threadIdx.x < s.nvec;
+    if (v0 + i * step + TPB > s.nvec) {  // (the same for all threads)
+      const bool in = v0 + i * step + (int)threadIdx.x < s.nvec;
       r[i].x = in ? r[i].x : none_of(type).x;
       r[i].y = in ? r[i].y : none_of(type).y;
       r[i].z = in ? r[i].z : none_of(type).z;
@@ -329,61 +332,41 @@ __device__ __forceinline__ float wave_sum(float x) {
   return (lane_value(x, 15) + lane_value(x, 31)) + (lane_value(x, 47) + lane_value(x, 63));
 }
 
+// fmaxf passes over a NaN; the sums carry it
+__device__ __forceinline__ float join_sum(float m, float s, float top, float a) {
+  return s * rescale(m, top, a);
+}
+
+__device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const uint64_t o = __shfl_xor((unsigned long long)x, d);
+    x = o > x ? o : x;
+  }
+  return x;
+}
+
 // ----------------------------------------------------------------------------
 // top logits
 
 constexpr uint32_t kNaNBits = 0x7FC00000u;
 
-// What a selection writes to. A whole row's results are the caller's; a row
-// too long for one workgroup is selected in chunks, each writing its own list
-// and its rest as a pair, and the lists of a row, one after the other, are
-// then selected from like a row of logits.
-struct TopStage {
-  float* list_val;     // rows x chunks x k
-  int32_t* list_word;
-  float2* rests;       // rows x chunks: (m, S)
-  int32_t chunks;
-};
-enum { kWhole = 0, kChunk = 1, kLists = 2 };
-
-template <int STAGE>
-__device__ __forceinline__ void put_pair(const TopArgs& A, const TopStage& G, int64_t row,
-                                         int chunk, uint32_t pos, int32_t word, float x) {
-  if constexpr (STAGE == kChunk) {
-    const int64_t o = (row * G.chunks + chunk) * A.k + pos;
-    G.list_word[o] = word;
-    G.list_val[o] = x;
-  } else {
-    const int64_t o = row * A.k + pos;
-    A.idx[o] = STAGE == kLists ? G.list_word[row * A.ld + word] : word;
-    if (A.val_format == TKEF_VAL_F16)
-      static_cast<_Float16*>(A.val)[o] = (_Float16)x;
-    else
-      static_cast<float*>(A.val)[o] = x;
-  }
+__device__ __forceinline__ void put_pair(const TopArgs& A, int64_t row, uint32_t pos,
+                                         int32_t word, float x) {
+  const int64_t o = row * A.k + pos;
+  A.idx[o] = word;
+  if (A.val_format == TKEF_VAL_F16)
+    static_cast<_Float16*>(A.val)[o] = (_Float16)x;
+  else
+    static_cast<float*>(A.val)[o] = x;
 }
 
-// The rest of a selection: S * 2^(m a), by one thread.
-template <int STAGE>
-__device__ __forceinline__ void put_rest(const TopArgs& A, const TopStage& G, int64_t row,
-                                         int chunk, float m, float S) {
-  if constexpr (STAGE == kChunk) {
-    G.rests[row * G.chunks + chunk] = make_float2(m, S);
-  } else {
-    if (A.tail == nullptr) return;
-    bool nan = S != S;
-    if constexpr (STAGE == kLists) {
-      for (int c = 0; c < G.chunks; ++c) {
-        const float2 r = G.rests[row * G.chunks + c];
-        const float top = fmaxf(m, r.x);
-        if (top != kInf) S = S * rescale(m, top, A.a) + r.y * rescale(r.x, top, A.a);
-        m = top;
-        nan |= r.y != r.y;
-      }
-    }
-    A.tail[row] = nan ? __uint_as_float(kNaNBits)
-                      : m == kInf ? kInf : S > 0.f ? m * A.inv_t + kLn2 * log2_(S) : -kInf;
-  }
+// The rest of a selection, S * 2^(m a), by one thread.
+__device__ __forceinline__ void put_rest(const TopArgs& A, int64_t row, float m, float S) {
+  if (A.tail == nullptr) return;
+  A.tail[row] = S != S ? __uint_as_float(kNaNBits)
+                : m == kInf ? kInf
+                : S > 0.f ? m * A.inv_t + kLn2 * log2_(S) : -kInf;
 }
 
 struct RadixLds {
@@ -393,23 +376,20 @@ struct RadixLds {
   uint32_t pick[2];
 };
 
-// Selection among words [e0, e1) of a row that takes any values: radix select
-// of the k-th largest order key over four 8-bit digits, then the ordered
-// compaction and the rest's sum. Seven passes over the words; the kernel below
-// comes here with rows whose words nearly all tie (constant rows, rows with few
-// words left unmasked), rows with NaN, and rows whose rest lies more than 2^-60
-// below their k-th word.
-template <typename T, int NT, int STAGE>
-__device__ __forceinline__ void top_radix(const TopArgs& A, const TopStage& G, RadixLds& L,
-                                       const T* p, int e0, int e1, int64_t row, int chunk) {
-  const int tid = threadIdx.x;
-  uint32_t prefix = 0u;
-  uint32_t need = (uint32_t)(A.k < e1 - e0 ? A.k : e1 - e0);
-  const uint32_t taken = need;
+// Selection from a row of any values: radix select of the k-th largest order
+// key over four 8-bit digits, then the ordered compaction and the rest's sum.
+// Seven passes over the row; the kernels below come here with rows whose words
+// nearly all tie (constant rows, rows with few words left unmasked), rows with
+// NaN, and rows whose rest lies more than 2^-60 below their k-th word.
+template <typename T, int NT>
+__device__ __forceinline__ void top_radix(const TopArgs& A, RadixLds& L, const T* p,
+                                          int64_t row) {
+  const int tid = threadIdx.x, V = A.V;
+  uint32_t prefix = 0u, need = (uint32_t)A.k;
   for (int shift = 24; shift >= 0; shift -= 8) {
     if (tid < 256) L.hist[tid] = 0u;
     __syncthreads();
-    for (int i = e0 + tid; i < e1; i += NT) {
+    for (int i = tid; i < V; i += NT) {
       const uint32_t key = order_key(load1(p, i));
       if (shift == 24 || (key >> (shift + 8)) == prefix)
         atomicAdd(&L.hist[(key >> shift) & 255u], 1u);
@@ -432,33 +412,30 @@ __device__ __forceinline__ void top_radix(const TopArgs& A, const TopStage& G, R
   uint32_t done_gt = 0u, done_eq = 0u;
   float top = -kInf;
   int nan = 0;
-  for (int base = e0; base < e1; base += NT) {
+  for (int base = 0; base < V; base += NT) {
     const int i = base + tid;
-    const float x = i < e1 ? load1(p, i) : 0.f;
-    const uint32_t key = i < e1 ? order_key(x) : 0u;
-    const bool gt = i < e1 && key > kth, eq = i < e1 && key == kth;
+    const float x = i < V ? load1(p, i) : 0.f;
+    const uint32_t key = i < V ? order_key(x) : 0u;
+    const bool gt = i < V && key > kth, eq = i < V && key == kth;
     uint32_t total;
     // (both counts in one scan: at most 1,024 of each in a round)
     const uint32_t before =
         block_scan<NT>((gt ? 1u : 0u) | (eq ? 1u << 16 : 0u), L.red, &total);
     const uint32_t r_gt = done_gt + (before & 0xFFFFu), r_eq = done_eq + (before >> 16);
     if (gt || (eq && r_eq < quota))
-      put_pair<STAGE>(A, G, row, chunk, r_gt + (r_eq < quota ? r_eq : quota), i, x);
-    else if (i < e1)
+      put_pair(A, row, r_gt + (r_eq < quota ? r_eq : quota), i, x);
+    else if (i < V)
       top = x > top ? x : top;
-    nan |= i < e1 && x != x;
+    nan |= i < V && x != x;
     done_gt += total & 0xFFFFu;
     done_eq += total >> 16;
   }
-  if constexpr (STAGE == kChunk)
-    for (uint32_t j = taken + tid; j < (uint32_t)A.k; j += NT)
-      put_pair<STAGE>(A, G, row, chunk, j, e1 - 1, -kInf);
   nan = __syncthreads_or(nan);
   if (nan && tid == 0) raise_status(A.status, TKEF_STATUS_NAN);
   top = block_reduce<NT>(top, L.fred, MaxOp());
   const float m = top == -kInf ? 0.f : top;
   float sum = 0.f;
-  for (int i = e0 + tid; i < e1; i += NT) {
+  for (int i = tid; i < V; i += NT) {
     const float x = load1(p, i);
     if (order_key(x) < kth) sum += exp2_((x - m) * A.a);
   }
@@ -469,17 +446,200 @@ __device__ __forceinline__ void top_radix(const TopArgs& A, const TopStage& G, R
     if (done_eq > quota && tie > -kInf)
       sum += (float)(done_eq - quota) * exp2_((tie - m) * A.a);
     if (top == kInf) sum = 1.f;
-    put_rest<STAGE>(A, G, row, chunk, nan ? 0.f : top, nan ? __uint_as_float(kNaNBits) : sum);
+    put_rest(A, row, top, nan ? __uint_as_float(kNaNBits) : sum);
   }
 }
 
-// Smallest difference of two order keys of a type's values.
-__device__ __forceinline__ uint32_t key_step(const float*) { return 1u; }
-__device__ __forceinline__ uint32_t key_step(const _Float16*) { return 1u << 13; }
-__device__ __forceinline__ uint32_t key_step(const __bf16*) { return 1u << 16; }
+// A candidate: the distinct upper bits of its order key, then the complement of
+// its word, so that a larger candidate is selected first.
+constexpr int kWordBits = 20;
+static_assert(TKEF_ROWS_MAX_VOCAB <= 1 << kWordBits, "words of a candidate");
+__device__ __forceinline__ constexpr int key_shift(const float*) { return 0; }
+__device__ __forceinline__ constexpr int key_shift(const _Float16*) { return 13; }
+__device__ __forceinline__ constexpr int key_shift(const __bf16*) { return 16; }
 
-// One workgroup selects from a row (or a chunk of one) that it holds in
-// registers, NV vectors a thread.
+template <typename T>
+__device__ __forceinline__ uint64_t candidate(uint32_t key, int32_t word) {
+  const T* type = nullptr;
+  return ((uint64_t)(key >> key_shift(type)) << kWordBits) |
+         (uint32_t)((1 << kWordBits) - 1 - word);
+}
+__device__ __forceinline__ int32_t word_of(uint64_t c) {
+  return (1 << kWordBits) - 1 - (int32_t)((uint32_t)c & ((1u << kWordBits) - 1u));
+}
+template <typename T>
+__device__ __forceinline__ float value_of(uint64_t c) {
+  const T* type = nullptr;
+  uint32_t key = (uint32_t)(c >> kWordBits) << key_shift(type);
+  if (!(key >> 31)) key |= (1u << key_shift(type)) - 1u;  // (a negative value's key is inverted)
+  return key_value(key);
+}
+
+// the least candidate at or above an order key
+template <typename T>
+__device__ __forceinline__ uint64_t floor_of(uint32_t key) {
+  const T* type = nullptr;
+  return (uint64_t)(key >> key_shift(type)) << kWordBits;
+}
+
+// Rank among candidates by counting where there is one a thread at most.
+template <int TPB>
+constexpr int rank_limit() {
+  return TPB == 256 ? 256 : 512;
+}
+
+template <int TPB, int KMAX>
+struct FinishLds {
+  int32_t chosen[KMAX + 4];  // (and up to three fillers)
+  uint64_t thr, top[TPB / 64];
+  float others[rank_limit<TPB>()];
+  uint32_t count[2][TPB / 64];
+  float red[TPB / 64];
+  uint32_t ntaken;
+};
+
+// The k first of C candidates (LDS, all >= least, then a 0), their places in ascending order of words,
+// and the rest: S * 2^(m a) and the candidates not taken. Up to rank_limit
+// candidates a thread counts the better ones of its own; beyond that the k-th
+// candidate is bisected, a candidate's word being part of it, so that ties end
+// at the lower words. A selected word's place is the number of selected lower
+// words. False, with nothing written, where candidates below `lowest` would be
+// needed or the rest vanishes beside the last selected word. The same for all
+// threads.
+template <typename T, int TPB, int CAP, int KMAX>
+__device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const T* p,
+                                           const uint64_t* cand, int C, uint64_t least,
+                                           uint64_t lowest, float m, float S,
+                                           FinishLds<TPB, KMAX>& L) {
+  constexpr int NW = TPB / 64, CPT = (CAP + TPB - 1) / TPB;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = A.k;
+  if (C < k) return false;
+  const bool more = k < A.V;
+  uint64_t c[CPT];
+  const bool counted = C <= rank_limit<TPB>();
+  uint64_t thr;
+  float left = 0.f;
+  if (tid < 4) L.chosen[k + tid] = INT32_MAX;
+  if (counted) {
+    c[0] = tid < C ? cand[tid] : 0ull;
+    int rank = 0;
+    if (wave * 64 < C) {
+      for (int j = 0; j < C; j += 2) {  // (cand[C] is 0)
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&cand[j]);
+        rank += (o.x > c[0] ? 1 : 0) + (o.y > c[0] ? 1 : 0);
+      }
+    }
+    if (tid < C) {
+      if (rank < k)
+        L.chosen[rank] = word_of(c[0]);
+      else
+        L.others[rank - k] = value_of<T>(c[0]);
+      if (rank == k - 1) L.thr = c[0];
+    }
+    __syncthreads();
+    thr = L.thr;
+  } else {
+    uint64_t hi = 0ull;
+#pragma unroll
+    for (int q = 0; q < CPT; ++q) {
+      c[q] = 0ull;
+      if (q * TPB < C) {
+        c[q] = q * TPB + tid < C ? cand[q * TPB + tid] : 0ull;
+        hi = c[q] > hi ? c[q] : hi;
+      }
+    }
+    hi = wave_max64(hi);
+    if (lane == 0) L.top[wave] = hi;
+    if (tid == 0) L.ntaken = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) hi = L.top[w] > hi ? L.top[w] : hi;
+    ++hi;
+    // n_lo >= k candidates are >= lo, fewer than k are >= hi
+    uint64_t lo = least;
+    uint32_t n_lo = (uint32_t)C;
+    for (int turn = 0; n_lo > (uint32_t)k && hi - lo > 1ull; turn ^= 1) {
+      const uint64_t mid = lo + (hi - lo) / 2ull;
+      uint32_t n = 0u;
+#pragma unroll
+      for (int q = 0; q < CPT; ++q)
+        if (q * TPB < C) n += (uint32_t)__popcll(__ballot(c[q] >= mid));
+      if (lane == 0) L.count[turn][wave] = n;
+      __syncthreads();
+      n = 0u;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) n += L.count[turn][w];
+      if (n >= (uint32_t)k) {
+        lo = mid;
+        n_lo = n;
+      } else {
+        hi = mid;
+      }
+    }
+    thr = lo;
+  }
+  if (thr < lowest) return false;
+  const float at_thr = value_of<T>(thr), base = at_thr == -kInf ? 0.f : at_thr;
+  if (counted) {
+    for (int j = lane; j < C - k; j += 64) left += exp2_((L.others[j] - base) * A.a);
+    left = wave_sum(left);
+  } else {
+#pragma unroll
+    for (int q = 0; q < CPT; ++q) {
+      if (q * TPB >= C) continue;
+      const bool take = c[q] >= thr;
+      const uint64_t who = __ballot(take);
+      if (who != 0ull) {
+        uint32_t at = 0u;
+        if (lane == 0) at = atomicAdd(&L.ntaken, (uint32_t)__popcll(who));
+        at = __builtin_amdgcn_readfirstlane(at) +
+             __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32),
+                                       __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+        if (take) L.chosen[at] = word_of(c[q]);
+      }
+      if (!take && c[q] != 0ull) left += exp2_((value_of<T>(c[q]) - base) * A.a);
+    }
+    left = wave_sum(left);
+    if (lane == 0) L.red[wave] = left;
+    __syncthreads();
+    left = wave_sum(lane < NW ? L.red[lane] : 0.f);
+  }
+  // the rest relative to the last selected word
+  const float rest = S * rescale(m, base, A.a) + left;
+  if (more && !(rest > 0x1p-60f)) return false;
+  for (int j = tid; j < k; j += TPB) {
+    const int32_t word = L.chosen[j];
+    int place = 0;
+    for (int i = 0; i < k; i += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(&L.chosen[i]);
+      place += (o.x < word ? 1 : 0) + (o.y < word ? 1 : 0) + (o.z < word ? 1 : 0) +
+               (o.w < word ? 1 : 0);
+    }
+    put_pair(A, row, (uint32_t)place, word, load1(p, word));
+  }
+  if (tid == 0) put_rest(A, row, more ? base : -kInf, more ? rest : 0.f);
+  return true;
+}
+
+// Parts of a row that is too long for one workgroup's registers. A part
+// holds every `parts`-th piece of TPB vectors of the row, so that words that
+// lie together (frequent ones often do) spread over all parts, and hands on its
+// words at or above a bound that about `want` of them reach: enough for
+// its share of the k first. The words of the k first that it might hold back are
+// below its bound, which the merge checks against the k-th.
+struct PartHead {
+  float bound, sum;    // the words below: sum * 2^(bound a)
+  uint32_t key, count; // the bound's order key; candidates, kFullPart: too many, or NaN
+};
+constexpr uint32_t kFullPart = 0xFFFFFFFFu;
+struct TopParts {
+  PartHead* heads;  // rows x parts
+  uint64_t* lists;  // rows x parts x room
+  int32_t parts, room, want;
+};
+
+// One workgroup takes a row, or a part of one, into registers, NV vectors a
+// thread.
 //   1. Each thread's maximum over each of its SUB shares. The k-th largest of
 //      these TPB * SUB maxima (bisected on order keys by one wave) is at most the
 //      k-th largest word: every selected word is at least that bound, and few
@@ -487,60 +647,44 @@ __device__ __forceinline__ uint32_t key_step(const __bf16*) { return 1u << 16; }
 //   2. One pass over the registers sums the exponentials of the words below
 //      the bound; a vector with a word at or above it goes to its wave's part of
 //      LDS instead, whose words the wave then sorts into candidates and others.
-//   3. The k first candidates and their places in ascending order: by counting
-//      for each candidate the better ones, then for each selected word the
-//      selected lower words; above kRank candidates the k-th key by bisection
-//      (ties to the lower words), then a bitmap over the row and its prefix
-//      counts.
-// More vectors or candidates than LDS holds, a NaN (in the sum) or a rest that
-// vanishes beside the last selected word send the row to top_radix.
-template <typename T, int TPB, int NV, int SUB, int STAGE>
-__global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, TopStage G) {
+//   3. top_finish, or a part's list.
+// More vectors or candidates than LDS holds or a NaN (in the sum) send the row
+// to top_radix.
+template <typename T, int TPB, int NV, int SUB, bool PART>
+__global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, TopParts P) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
-  constexpr int kCap = SUB > 1 ? 8224 : TPB == 256 ? 1024 : 2080;  // candidates
-  constexpr int kVecs = SUB > 1 ? 160 : TPB == 256 ? 128 : 80;     // vectors of a wave
-  constexpr int kRank = TPB == 256 ? 256 : 1024;
-  constexpr int kWords = (TPB * NV * N + 28 + 31) / 32;
-  constexpr int kPer = (kWords + TPB - 1) / TPB;
+  constexpr int kKMax = PART ? 1 : SUB > 1 ? TKEF_ROWS_MAX_K : TPB / 4;
+  constexpr int kCap = PART ? 1 : SUB > 1 ? 8224 : TPB == 256 ? 1024 : 2080;  // candidates
+  constexpr int kVecs = SUB > 1 ? (TPB == 256 ? 320 : 160) : TPB == 256 ? 128 : 80;  // of a wave
   constexpr int kGroups = TPB * SUB;
-  // the bitmap and its prefix counts come after the vectors are done with
-  struct Bits {
-    uint32_t map[kPer * TPB];
-    uint16_t before[kPer * TPB];
-  };
   struct Vecs {
     uint4 x[NW][kVecs];
     int32_t word[NW][kVecs];
   };
   union Shared {
-    Vecs v;
-    Bits b;
     uint32_t group[kGroups];
+    Vecs v;
+    FinishLds<TPB, kKMax> finish;
     RadixLds radix;
   };
   __shared__ Shared S;
-  __shared__ __align__(16) uint64_t cand[kCap];  // order key, complement of the word
-  __shared__ __align__(16) int32_t chosen[kRank];
-  __shared__ float others[kRank];
+  __shared__ __align__(16) uint64_t cand[kCap + 2];
   __shared__ float red[NW];
-  __shared__ uint32_t scan[NW];
-  __shared__ uint32_t ncand, full, bound_key, thr_key, thr_count;
+  __shared__ uint32_t wave_count[NW];
+  __shared__ uint32_t full, bound_key;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
-  const int chunk = STAGE == kChunk ? (int)blockIdx.y : 0;
+  const int part = PART ? (int)blockIdx.y : 0, parts = PART ? P.parts : 1;
   const T* type = nullptr;
   const Span<T> s(static_cast<const T*>(A.z) + row * A.ld, A.V);
-  const int v0 = chunk * (TPB * NV);
-  const bool first = chunk == 0, last = STAGE != kChunk || chunk == G.chunks - 1;
-  const int e0 = first ? 0 : s.head + v0 * N;
-  const int e1 = last ? A.V : s.head + (v0 + TPB * NV) * N;
-  const int k = A.k < e1 - e0 ? A.k : e1 - e0;
+  const int v0 = part * TPB, step = parts * TPB;
+  const int k = PART ? P.want : A.k;
   uint4 r[NV];
-  load_slots<T, TPB, NV>(r, s, v0);
+  load_slots<T, TPB, NV>(r, s, v0, step);
   const int xi = s.extra(tid < s.extras ? tid : 0);
-  const bool has_ex = tid < s.extras && xi >= e0 && xi < e1;
+  const bool has_ex = part == 0 && tid < s.extras;
   const float ex = has_ex ? (float)s.p[xi] : -kInf;
-  if (tid == 0) ncand = full = 0u;
+  if (tid == 0) full = 0u;
   // 1. the bound
 #pragma unroll
   for (int q = 0; q < SUB; ++q) {
@@ -570,8 +714,8 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi) + 1u;
     // at least k maxima have keys >= lo, fewer than k have keys >= hi
-    const uint32_t step = key_step(type), enough = (uint32_t)k + ((uint32_t)k >> 3) + 1u;
-    while (hi - lo > step) {
+    const uint32_t least = 1u << key_shift(type), enough = (uint32_t)k + ((uint32_t)k >> 3) + 1u;
+    while (hi - lo > least) {
       const uint32_t mid = lo + (hi - lo) / 2u;
       uint32_t c = 0u;
 #pragma unroll
@@ -587,7 +731,8 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     if (lane == 0) bound_key = lo;
   }
   __syncthreads();
-  const float bound = key_value(bound_key);
+  const uint32_t at_bound = bound_key;
+  const float bound = key_value(at_bound);
   // 2. candidates, and the sum of the others
   const float ref = bound == -kInf ? 0.f : bound;
   float sum = 0.f;
@@ -595,7 +740,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
   const int tid2 = renew(tid);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * TPB + tid2;
+    const int v = v0 + i * step + tid2;
     float x[N];
     renew(r[i]);
     unpack(r[i], x, type);
@@ -621,164 +766,124 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     held = 0;
     if (lane == 0) full = 1u;
   }
-  // the wave's words: those at or above the bound are candidates
-  const auto sort_out = [&](bool valid, float x, int32_t word) {
-    const bool take = valid && x >= bound;
-    const uint64_t who = __ballot(take);
-    if (who != 0ull) {
-      uint32_t at = 0u;
-      if (lane == 0) at = atomicAdd(&ncand, (uint32_t)__popcll(who));
-      at = __builtin_amdgcn_readfirstlane(at) +
-           __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32),
-                                     __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
-      if (take && at < (uint32_t)kCap)
-        cand[at] = ((uint64_t)order_key(x) << 32) | (0xFFFFFFFFu - (uint32_t)word);
+  // The wave's words at or above the bound are candidates: `each` gets them with
+  // a number that counts them in a fixed order.
+  const auto wave_words = [&](auto each) {
+    int seen = 0;
+    const auto one = [&](bool valid, float x, int32_t word) {
+      const bool take = valid && x >= bound;
+      const uint64_t who = __ballot(take);
+      each(valid, take, x, word,
+           seen + (int)__builtin_amdgcn_mbcnt_hi(
+                      (uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u)));
+      seen += (int)__popcll(who);
+    };
+    for (int i = 0; i < held * N; i += 64) {
+      const int e = i + lane;
+      const bool valid = e < held * N;
+      const int at = valid ? e / N : 0;
+      const float x = (float)reinterpret_cast<const T*>(&S.v.x[wave][at])[e % N];
+      one(valid, x, S.v.word[wave][at] + e % N);
     }
-    if (valid && !take) sum += exp2_((x - ref) * A.a);
+    if (wave == 0) one(has_ex, ex, xi);
+    return seen;
   };
-  for (int i = 0; i < held * N; i += 64) {
-    const int e = i + lane;
-    const bool valid = e < held * N;
-    const int at = valid ? e / N : 0;
-    const float x = (float)reinterpret_cast<const T*>(&S.v.x[wave][at])[e % N];
-    sort_out(valid, x, S.v.word[wave][at] + e % N);
-  }
-  if (wave == 0) sort_out(has_ex, ex, xi);
+  const int found = wave_words([&](bool valid, bool take, float x, int32_t, int) {
+    if (valid && !take) sum += exp2_((x - ref) * A.a);
+  });
   sum = wave_sum(sum);
-  if (lane == 0) red[wave] = sum;
+  if (lane == 0) {
+    red[wave] = sum;
+    wave_count[wave] = (uint32_t)found;
+  }
   __syncthreads();
-  const int C = (int)ncand;
+  int C = 0, mine = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    mine += w < wave ? (int)wave_count[w] : 0;
+    C += (int)wave_count[w];
+  }
   sum = wave_sum(lane < NW ? red[lane] : 0.f);
-  bool hard = C > kCap || full != 0u || sum != sum;  // (the same for the whole workgroup)
-  const bool more = k < e1 - e0;
-  const auto word_of = [](uint64_t c) { return (int32_t)(0xFFFFFFFFu - (uint32_t)c); };
-  if (!hard && C <= kRank) {
-    // 3. by counting: candidate tid, its rank, its place among the selected words
-    const uint64_t mine = tid < C ? cand[tid] : 0ull;
-    int rank = 0;
-    if (wave * 64 < C)
-#pragma unroll 4
-      for (int j = 0; j < C; ++j) rank += cand[j] > mine ? 1 : 0;
-    const int32_t word = word_of(mine);
-    if (tid < C) {
-      if (rank < k)
-        chosen[rank] = word;
-      else
-        others[rank - k] = key_value((uint32_t)(mine >> 32));
-      if (rank == k - 1) thr_key = (uint32_t)(mine >> 32);
+  const bool odd = full != 0u || sum != sum;  // (the same for the whole workgroup)
+  if constexpr (PART) {
+    const int64_t at = row * parts + part;
+    const bool fits = !odd && C <= P.room;
+    if (fits)
+      wave_words([&](bool, bool take, float x, int32_t word, int n) {
+        if (take) P.lists[at * P.room + mine + n] = candidate<T>(order_key(x), word);
+      });
+    if (tid == 0) {
+      PartHead h;
+      h.bound = bound;
+      h.sum = sum;
+      h.key = at_bound;
+      h.count = fits ? (uint32_t)C : kFullPart;
+      P.heads[at] = h;
+    }
+  } else {
+    bool done = false;
+    if (!odd && C <= kCap) {
+      wave_words([&](bool, bool take, float x, int32_t word, int n) {
+        if (take) cand[mine + n] = candidate<T>(order_key(x), word);
+      });
+      if (tid == 0) cand[C] = 0ull;
+      __syncthreads();
+      done = top_finish<T, TPB, kCap, kKMax>(A, row, s.p, cand, C,
+                                               floor_of<T>(at_bound), 0ull, bound, sum, S.finish);
     }
     __syncthreads();
-    const float at_thr = key_value(thr_key), base = at_thr == -kInf ? 0.f : at_thr;
-    float left = 0.f;
-    for (int j = lane; j < C - k; j += 64) left += exp2_((others[j] - base) * A.a);
-    left = wave_sum(left);
-    // the rest relative to the threshold
-    const float rest = sum * rescale(bound, base, A.a) + left;
-    hard = more && !(rest > 0x1p-60f);
-    if (!hard) {
-      if (wave * 64 < C) {
-        int place = 0;
-#pragma unroll 4
-        for (int j = 0; j < k; ++j) place += chosen[j] < word ? 1 : 0;
-        if (tid < C && rank < k)
-          put_pair<STAGE>(A, G, row, chunk, (uint32_t)place, word, load1(s.p, word));
-      }
-      if constexpr (STAGE == kChunk)
-        for (int j = k + tid; j < A.k; j += TPB)
-          put_pair<STAGE>(A, G, row, chunk, (uint32_t)j, e1 - 1, -kInf);
-      if (tid == 0) put_rest<STAGE>(A, G, row, chunk, more ? base : -kInf, more ? rest : 0.f);
-    }
-  } else if (!hard) {
-    // 3. the k-th key of the candidates, the bitmap of the selected words
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) S.b.map[i * TPB + tid] = 0u;
-    if (wave == 0) {
-      uint32_t lo = bound_key, hi = lo, n_lo = (uint32_t)C;
-      for (int i = lane; i < C; i += 64) {
-        const uint32_t key = (uint32_t)(cand[i] >> 32);
-        hi = key > hi ? key : hi;
-      }
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) {
-        const uint32_t b = __shfl_xor(hi, d);
-        hi = b > hi ? b : hi;
-      }
-      hi = __builtin_amdgcn_readfirstlane(hi) + 1u;
-      // n_lo >= k candidates have keys >= lo, fewer than k have keys >= hi
-      while (n_lo > (uint32_t)k && hi - lo > 1u) {
-        const uint32_t mid = lo + (hi - lo) / 2u;
-        uint32_t c = 0u;
-        for (int i = 0; i < C; i += 64)
-          c += (uint32_t)__popcll(
-              __ballot(i + lane < C && (uint32_t)(cand[i + lane < C ? i + lane : 0] >> 32) >= mid));
-        if (c >= (uint32_t)k) {
-          lo = mid;
-          n_lo = c;
-        } else {
-          hi = mid;
-        }
-      }
-      if (lane == 0) {
-        thr_key = lo;
-        thr_count = n_lo;
-      }
-    }
+    if (!done) top_radix<T, TPB>(A, S.radix, s.p, row);
+  }
+}
+
+// The k first of a row from its parts' lists.
+template <typename T, int TPB, int CAP>
+__global__ __launch_bounds__(TPB) void k_top_merge(TopArgs A, TopParts P) {
+  __shared__ __align__(16) uint64_t cand[CAP + 2];
+  __shared__ uint32_t from[64];
+  union Shared {
+    FinishLds<TPB, TKEF_ROWS_MAX_K> finish;
+    RadixLds radix;
+  };
+  __shared__ Shared S;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t row = blockIdx.x;
+  const T* p = static_cast<const T*>(A.z) + row * A.ld;
+  // (every wave reads the heads; at most 64 of them)
+  PartHead h = {-kInf, 0.f, 0u, 0u};
+  if (lane < P.parts) h = P.heads[row * P.parts + lane];
+  const bool odd = __ballot(h.count == kFullPart) != 0ull;
+  bool done = false;
+  if (!odd) {
+    const uint32_t inc = wave_incl(h.count);
+    if (tid < 64) from[lane] = inc - h.count;
+    const int C = __builtin_amdgcn_readlane((int)inc, 63);
+    const float m = wave_max(h.bound);
+    const float sum = wave_sum(join_sum(h.bound, h.sum, m, A.a));
+    // what a part held back lies below its bound; the least that does not
+    const T* type = nullptr;
+    const uint64_t lowest =
+        wave_max64(lane < P.parts && h.key != 0u
+                       ? (((uint64_t)((h.key - 1u) >> key_shift(type)) + 1ull) << kWordBits)
+                       : 0ull);
+    const uint64_t least = ~wave_max64(lane < P.parts ? ~floor_of<T>(h.key) : 0ull);
     __syncthreads();
-    // all n_lo candidates at or above the threshold, or (ties at it) the ones
-    // above it and the lowest words of those at it
-    const uint32_t thr = thr_key, surplus = thr_count - (uint32_t)k;
-    const float at_thr = key_value(thr), base = at_thr == -kInf ? 0.f : at_thr;
-    float left = 0.f;
-    for (int i = tid; i < C; i += TPB) {
-      const uint64_t mine = cand[i];
-      const int32_t w = word_of(mine);
-      const uint32_t key = (uint32_t)(mine >> 32);
-      bool take = key >= thr;
-      if (surplus != 0u && key == thr) {
-        uint32_t higher = 0u;  // ties at higher words
-        for (int j = 0; j < C; ++j)
-          higher += (uint32_t)(cand[j] >> 32) == thr && cand[j] < mine ? 1u : 0u;
-        take = higher >= surplus;
+    if (C <= CAP) {
+      const int64_t lists = row * P.parts * P.room;
+      for (int i = tid; i < P.parts * P.room; i += TPB) {
+        const int part = i / P.room, n = i - part * P.room;
+        const uint32_t at = from[part];
+        const uint32_t end = part + 1 < P.parts ? from[part + 1] : (uint32_t)C;
+        if (at + (uint32_t)n < end) cand[at + n] = P.lists[lists + i];
       }
-      if (take)
-        atomicOr(&S.b.map[(w - e0) >> 5], 1u << ((w - e0) & 31));
-      else
-        left += exp2_((key_value(key) - base) * A.a);
-    }
-    left = wave_sum(left);
-    if (lane == 0) red[wave] = left;
-    __syncthreads();
-    // prefix counts of the bitmap's words
-    uint32_t count = 0u, total;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) count += (uint32_t)__popc(S.b.map[tid * kPer + i]);
-    count = block_scan<TPB>(count, scan, &total);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      S.b.before[tid * kPer + i] = (uint16_t)count;
-      count += (uint32_t)__popc(S.b.map[tid * kPer + i]);
-    }
-    left = wave_sum(lane < NW ? red[lane] : 0.f);
-    const float rest = sum * rescale(bound, base, A.a) + left;
-    hard = more && !(rest > 0x1p-60f);
-    __syncthreads();
-    if (!hard) {
-      for (int i = tid; i < C; i += TPB) {
-        const int32_t word = word_of(cand[i]), w = word - e0;
-        const uint32_t bits = S.b.map[w >> 5], bit = 1u << (w & 31);
-        if (bits & bit)
-          put_pair<STAGE>(A, G, row, chunk,
-                          S.b.before[w >> 5] + (uint32_t)__popc(bits & (bit - 1u)), word,
-                          load1(s.p, word));
-      }
-      if constexpr (STAGE == kChunk)
-        for (int j = k + tid; j < A.k; j += TPB)
-          put_pair<STAGE>(A, G, row, chunk, (uint32_t)j, e1 - 1, -kInf);
-      if (tid == 0) put_rest<STAGE>(A, G, row, chunk, more ? base : -kInf, more ? rest : 0.f);
+      if (tid == 0) cand[C] = 0ull;
+      __syncthreads();
+      done = top_finish<T, TPB, CAP, TKEF_ROWS_MAX_K>(A, row, p, cand, C, least, lowest,
+                                                      m, sum, S.finish);
     }
   }
   __syncthreads();
-  if (hard) top_radix<T, TPB, STAGE>(A, G, S.radix, s.p, e0, e1, row, chunk);
+  if (!done) top_radix<T, TPB>(A, S.radix, p, row);
 }
 
 // ----------------------------------------------------------------------------
@@ -860,11 +965,6 @@ struct Part {
   float rm, rs, zm, zs, tm, ts, cross, pad;
 };
 static_assert(sizeof(Part) == kPartBytes, "workspace layout");
-
-// fmaxf passes over a NaN; the sums carry it
-__device__ __forceinline__ float join_sum(float m, float s, float top, float a) {
-  return s * rescale(m, top, a);
-}
 
 __device__ __forceinline__ Part wave_join(Part p, float a) {
   Part r;
@@ -1396,15 +1496,6 @@ __device__ __forceinline__ uint64_t race_key(float score, int word) {
   return ((uint64_t)__float_as_uint(score) << 32) | (0xFFFFFFFFu - (uint32_t)word);
 }
 
-__device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)x, d);
-    x = o > x ? o : x;
-  }
-  return x;
-}
-
 // The race over one chunk (blockIdx.x) of the row after the accepted tokens of
 // sequence blockIdx.y: the best word of the residual and, in case that is empty,
 // of the target's own probabilities. The noise does not depend on where the
@@ -1558,73 +1649,65 @@ struct Pointee<T*> {
 // Registers hold a row of up to 16 vectors for each of 1,024 threads.
 constexpr int kRowVecs = 1024 * 16;
 constexpr int kChunkVecs = 256 * 8;
-// the longest row's lists fit the kernel that selects from them
-static_assert((TKEF_ROWS_MAX_VOCAB / 4 + kRowVecs - 1) / kRowVecs * TKEF_ROWS_MAX_K / 4 <= 1024 * 4,
-              "lists of a row's chunks");
-
-int top_chunks(int64_t V, int32_t dtype) {
-  const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
-  return vecs <= kRowVecs ? 1 : (int)((vecs + kRowVecs - 1) / kRowVecs);
-}
-
-size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype) {
-  const int chunks = top_chunks(V, dtype);
-  if (chunks == 1) return 0;
-  return (size_t)rows * (size_t)chunks * (sizeof(float2) + (size_t)k * 8);
-}
 
 namespace {
 
-template <typename T>
-void launch_top_whole(const TopArgs& a, hipStream_t s) {
-  const int vecs = a.V / Span<T>::N;
-  const dim3 grid((unsigned)a.rows);
-  const TopStage g{};
-  if (a.k <= 64 && vecs <= 256 * 16) {
-    if (vecs <= 256 * 4)
-      k_top_row<T, 256, 4, 1, kWhole><<<grid, 256, 0, s>>>(a, g);
-    else
-      k_top_row<T, 256, 16, 1, kWhole><<<grid, 256, 0, s>>>(a, g);
-  } else if (a.k <= 256) {
-    if (vecs <= 1024 * 4)
-      k_top_row<T, 1024, 4, 1, kWhole><<<grid, 1024, 0, s>>>(a, g);
-    else if (vecs <= 1024 * 8)
-      k_top_row<T, 1024, 8, 1, kWhole><<<grid, 1024, 0, s>>>(a, g);
-    else
-      k_top_row<T, 1024, 16, 1, kWhole><<<grid, 1024, 0, s>>>(a, g);
-  } else if (vecs <= 1024 * 4) {
-    k_top_row<T, 1024, 4, 4, kWhole><<<grid, 1024, 0, s>>>(a, g);
-  } else {
-    k_top_row<T, 1024, 16, 4, kWhole><<<grid, 1024, 0, s>>>(a, g);
-  }
+int64_t ceil_div(int64_t a, int64_t b) { return a <= 0 ? 1 : (a + b - 1) / b; }
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// A row's selection: whole in one workgroup up to kPartVecs vectors, else in
+// parts of that many.
+constexpr int kPartVecs = 256 * 16;
+constexpr int kMergeSmall = 2080, kMergeLarge = 9216;
+
+TopParts top_parts(int64_t V, int64_t k, int32_t dtype) {
+  TopParts p{};
+  p.parts = (int32_t)ceil_div(V / (dtype == TKEF_DTYPE_F32 ? 4 : 8), kPartVecs);
+  if (p.parts == 1) return p;
+  // a part's share of the k first and four standard deviations of it
+  const double share = (double)k / p.parts;
+  int64_t want = (int64_t)(share + 4.0 * std::sqrt(share)) + 8;
+  p.want = (int32_t)(want < k ? want : k);
+  p.room = 2 * p.want + 64;
+  return p;
 }
 
 }  // namespace
 
+size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype) {
+  const TopParts p = top_parts(V, k, dtype);
+  if (p.parts == 1) return 0;
+  return up256((size_t)rows * (size_t)p.parts * sizeof(PartHead)) +
+         (size_t)rows * (size_t)p.parts * (size_t)p.room * 8;
+}
+
 hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
-  const int chunks = top_chunks(a.V, a.dtype);
+  TopParts p = top_parts(a.V, a.k, a.dtype);
+  const dim3 rows((unsigned)a.rows), split((unsigned)a.rows, (unsigned)p.parts);
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;
-    if (chunks == 1) {
-      launch_top_whole<T>(a, s);
-      return;
-    }
-    TopStage g{};
-    g.chunks = chunks;
-    g.rests = static_cast<float2*>(ws);
-    g.list_val = reinterpret_cast<float*>(g.rests + a.rows * chunks);
-    g.list_word = reinterpret_cast<int32_t*>(g.list_val + a.rows * chunks * a.k);
-    const dim3 grid((unsigned)a.rows, (unsigned)chunks);
-    TopArgs lists = a;
-    lists.z = g.list_val;
-    lists.ld = (int64_t)chunks * a.k;
-    lists.V = chunks * a.k;
-    if (a.k <= 256) {
-      k_top_row<T, 1024, 16, 1, kChunk><<<grid, 1024, 0, s>>>(a, g);
-      k_top_row<float, 1024, 4, 1, kLists><<<dim3((unsigned)a.rows), 1024, 0, s>>>(lists, g);
+    const int vecs = a.V / Span<T>::N;
+    if (p.parts > 1) {
+      p.heads = static_cast<PartHead*>(ws);
+      p.lists = reinterpret_cast<uint64_t*>(
+          static_cast<char*>(ws) + up256((size_t)a.rows * (size_t)p.parts * sizeof(PartHead)));
+      if (p.want <= 64)
+        k_top_row<T, 256, 16, 1, true><<<split, 256, 0, s>>>(a, p);
+      else
+        k_top_row<T, 256, 16, 4, true><<<split, 256, 0, s>>>(a, p);
+      if (p.parts * p.room <= kMergeSmall)
+        k_top_merge<T, 256, kMergeSmall><<<rows, 256, 0, s>>>(a, p);
+      else
+        k_top_merge<T, 1024, kMergeLarge><<<rows, 1024, 0, s>>>(a, p);
+    } else if (a.k <= 64) {
+      if (vecs <= 256 * 4)
+        k_top_row<T, 256, 4, 1, false><<<rows, 256, 0, s>>>(a, p);
+      else
+        k_top_row<T, 256, 16, 1, false><<<rows, 256, 0, s>>>(a, p);
+    } else if (a.k <= 256) {
+      k_top_row<T, 1024, 4, 1, false><<<rows, 1024, 0, s>>>(a, p);
     } else {
-      k_top_row<T, 1024, 16, 4, kChunk><<<grid, 1024, 0, s>>>(a, g);
-      k_top_row<float, 1024, 4, 4, kLists><<<dim3((unsigned)a.rows), 1024, 0, s>>>(lists, g);
+      k_top_row<T, 1024, 4, 4, false><<<rows, 1024, 0, s>>>(a, p);
     }
   });
 }
@@ -1707,9 +1790,6 @@ hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
 namespace {
 constexpr int kUnitVecs = 1024 * 4, kSmallVecs = 256 * 4;
 constexpr int64_t kFewUnits = 256;
-
-int64_t ceil_div(int64_t a, int64_t b) { return a <= 0 ? 1 : (a + b - 1) / b; }
-size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 }  // namespace
 
 bool verify_fits(int64_t batch, int64_t draft, int64_t V, int32_t dtype) {

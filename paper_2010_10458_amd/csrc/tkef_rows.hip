@@ -1416,18 +1416,18 @@ __device__ __forceinline__ LogSum regs_sum(const uint4 (&r)[NV], float ex, float
 // joins the place's sums and decides about its token; a rejection is posted, and
 // workgroups of later places that start after it leave at once, so a large
 // batch reads little beyond each sequence's first rejection. Nothing waits.
-template <typename T, int TPB, int NV>
+template <typename T, int TPB, int NV, bool CHECK>
 __global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch W, int chunks) {
   constexpr int NW = TPB / 64;
   __shared__ float4 red[NW];
-  __shared__ uint32_t posted;
+  __shared__ uint32_t posted;  // (CHECK)
   const int tid = threadIdx.x, lane = tid & 63;
   const uint32_t unit = blockIdx.x, chunk = unit % (uint32_t)chunks;
   const int64_t b = (unit / (uint32_t)chunks) % (uint32_t)A.batch;
   const int place = (int)(unit / (uint32_t)chunks / (uint32_t)A.batch);
   const int len = draft_length(A, b);
   if (place > len) return;
-  if (place > 0) {
+  if (CHECK && place > 0) {
     if (tid == 0) posted = agent_load(&W.rejected[b]);
     __syncthreads();
     if (posted > (uint32_t)(TKEF_VERIFY_MAX_DRAFT + 1 - place)) return;
@@ -1570,6 +1570,15 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
     // a word after the vectors, by a thread that has met lower words alone
     offer((float)tp[w], drafted ? (float)dp[w] : -kInf, noise[w], w);
   }
+  if (blockIdx.x == 0 && tid < n) {  // the accepted drafts
+    const int token = A.tokens[b * A.draft + tid];
+    A.tokens_out[b * places + tid] = token;
+    if (A.logp != nullptr) {
+      const float4 at = W.sums[b * places + tid];
+      const float x = (float)static_cast<const T*>(A.target)[b * A.tb + tid * A.ti + token];
+      A.logp[b * places + tid] = (x - at.x) * A.inv_t - kLn2 * log2_(at.y);
+    }
+  }
   uint64_t over = over_s > 0.f ? race_key(over_s, over_w) : 0ull;
   uint64_t own = own_s > 0.f ? race_key(own_s, own_w) : 0ull;
   over = wave_max64(over);
@@ -1597,19 +1606,14 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
   const uint64_t key = over != 0ull ? over : own;
   const int word = key != 0ull ? (int)(0xFFFFFFFFu - (uint32_t)key) : -1;
   if (lane < places) {  // (at most 64)
-    const int i = lane;
-    const int token = i < n ? A.tokens[b * A.draft + i] : i == n ? word : -1;
-    A.tokens_out[b * places + i] = token;
-    if (A.logp != nullptr) {
-      float lp = 0.f;
-      if (token >= 0) {
-        const float4 at = W.sums[b * places + i];
-        const float x = (float)static_cast<const T*>(A.target)[b * A.tb + i * A.ti + token];
-        lp = (x - at.x) * A.inv_t - kLn2 * log2_(at.y);
-      }
-      A.logp[b * places + i] = lp;
+    if (lane >= n) {
+      const int token = lane == n ? word : -1;
+      A.tokens_out[b * places + lane] = token;
+      if (A.logp != nullptr)
+        A.logp[b * places + lane] =
+            token < 0 ? 0.f : ((float)tp[token] - s.x) * A.inv_t - kLn2 * log2_(s.y);
     }
-    agent_store(&W.arrived[b * places + i], 0u);
+    agent_store(&W.arrived[b * places + lane], 0u);
   }
   if (lane == 0) {
     A.accepted[b] = n;
@@ -1789,7 +1793,7 @@ hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
 // x 4 where those would leave compute units idle.
 namespace {
 constexpr int kUnitVecs = 1024 * 4, kSmallVecs = 256 * 4;
-constexpr int64_t kFewUnits = 256;
+constexpr int64_t kFewUnits = 512;
 }  // namespace
 
 bool verify_fits(int64_t batch, int64_t draft, int64_t V, int32_t dtype) {
@@ -1801,7 +1805,7 @@ VerifyLayout verify_layout(int64_t batch, int64_t draft, int64_t V, int32_t dtyp
   const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
   const int64_t places = batch * (draft + 1), big = ceil_div(vecs, kUnitVecs);
   // small units serve batches with fewer than kFewUnits big ones
-  const int64_t small = (places * big < kFewUnits ? places * big : kFewUnits) * 4;
+  const int64_t small = (places * big < kFewUnits ? places * big : kFewUnits) * 16;
   const int64_t parts = places * big > small ? places * big : small;
   VerifyLayout l;
   l.best = 0;
@@ -1820,16 +1824,24 @@ hipError_t launch_verify(const VerifyArgs& a, const VerifyScratch& w, hipStream_
     using T = typename Pointee<decltype(t)>::type;
     const int64_t vecs = a.V / Span<T>::N, places = (int64_t)a.batch * (a.draft + 1);
     const int64_t big = ceil_div(vecs, kUnitVecs);
-    if (places * big >= kFewUnits) {
-      k_verify_sums<T, 1024, 4>
+    if (places * big > kFewUnits) {
+      k_verify_sums<T, 1024, 4, true>
           <<<dim3((unsigned)(places * big)), 1024, 0, s>>>(a, w, (int)big);
-    } else {
+    } else if (places * big > 32) {
       const int64_t small = ceil_div(vecs, kSmallVecs);
-      k_verify_sums<T, 256, 4>
+      k_verify_sums<T, 256, 4, false>
           <<<dim3((unsigned)(places * small)), 256, 0, s>>>(a, w, (int)small);
+    } else {
+      const int64_t tiny = ceil_div(vecs, 256);
+      k_verify_sums<T, 256, 1, false>
+          <<<dim3((unsigned)(places * tiny)), 256, 0, s>>>(a, w, (int)tiny);
     }
-    k_verify_race<T, 256, 4>
-        <<<dim3((unsigned)ceil_div(vecs, kSmallVecs), (unsigned)a.batch), 256, 0, s>>>(a, w);
+    if (a.batch * ceil_div(vecs, 256 * 4) <= 128)
+      k_verify_race<T, 256, 1>
+          <<<dim3((unsigned)ceil_div(vecs, 256), (unsigned)a.batch), 256, 0, s>>>(a, w);
+    else
+      k_verify_race<T, 256, 4>
+          <<<dim3((unsigned)ceil_div(vecs, 256 * 4), (unsigned)a.batch), 256, 0, s>>>(a, w);
   });
 }
 

@@ -482,15 +482,16 @@ __device__ __forceinline__ uint64_t floor_of(uint32_t key) {
   return (uint64_t)(key >> key_shift(type)) << kWordBits;
 }
 
-// Rank among candidates by counting where there is one a thread at most.
+// Ranks by counting up to this many candidates, by bisection above: counting costs
+// a comparison for each pair, bisection some twelve rounds with a barrier each.
 template <int TPB>
 constexpr int rank_limit() {
-  return TPB == 256 ? 256 : 512;
+  return TPB == 256 ? 128 : 256;
 }
 
 template <int TPB, int KMAX>
 struct FinishLds {
-  int32_t chosen[KMAX + 4];  // (and up to three fillers)
+  int32_t chosen[KMAX + 16];  // (and fillers up to a multiple of 16)
   uint64_t thr, top[TPB / 64];
   float others[rank_limit<TPB>()];
   uint32_t count[2][TPB / 64];
@@ -498,7 +499,7 @@ struct FinishLds {
   uint32_t ntaken;
 };
 
-// The k first of C candidates (LDS, all >= least, then a 0), their places in ascending order of words,
+// The k first of C candidates (LDS, all >= least, then eight zeros), their places in ascending order of words,
 // and the rest: S * 2^(m a) and the candidates not taken. Up to rank_limit
 // candidates a thread counts the better ones of its own; beyond that the k-th
 // candidate is bisected, a candidate's word being part of it, so that ties end
@@ -519,14 +520,18 @@ __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const 
   const bool counted = C <= rank_limit<TPB>();
   uint64_t thr;
   float left = 0.f;
-  if (tid < 4) L.chosen[k + tid] = INT32_MAX;
+  if (tid < 16) L.chosen[k + tid] = INT32_MAX;
   if (counted) {
     c[0] = tid < C ? cand[tid] : 0ull;
     int rank = 0;
     if (wave * 64 < C) {
-      for (int j = 0; j < C; j += 2) {  // (cand[C] is 0)
-        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&cand[j]);
-        rank += (o.x > c[0] ? 1 : 0) + (o.y > c[0] ? 1 : 0);
+      for (int j = 0; j < C; j += 8) {  // (zeros follow; all reads before the first use)
+        ulonglong2 o[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          o[u] = *reinterpret_cast<const ulonglong2*>(&cand[j + 2 * u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) rank += (o[u].x > c[0] ? 1 : 0) + (o[u].y > c[0] ? 1 : 0);
       }
     }
     if (tid < C) {
@@ -610,10 +615,14 @@ __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const 
   for (int j = tid; j < k; j += TPB) {
     const int32_t word = L.chosen[j];
     int place = 0;
-    for (int i = 0; i < k; i += 4) {
-      const int4 o = *reinterpret_cast<const int4*>(&L.chosen[i]);
-      place += (o.x < word ? 1 : 0) + (o.y < word ? 1 : 0) + (o.z < word ? 1 : 0) +
-               (o.w < word ? 1 : 0);
+    for (int i = 0; i < k; i += 16) {
+      int4 o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] = *reinterpret_cast<const int4*>(&L.chosen[i + 4 * u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        place += (o[u].x < word ? 1 : 0) + (o[u].y < word ? 1 : 0) + (o[u].z < word ? 1 : 0) +
+                 (o[u].w < word ? 1 : 0);
     }
     put_pair(A, row, (uint32_t)place, word, load1(p, word));
   }
@@ -653,9 +662,9 @@ struct TopParts {
 template <typename T, int TPB, int NV, int SUB, bool PART>
 __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, TopParts P) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
-  constexpr int kKMax = PART ? 1 : SUB > 1 ? TKEF_ROWS_MAX_K : TPB / 4;
-  constexpr int kCap = PART ? 1 : SUB > 1 ? 8224 : TPB == 256 ? 1024 : 2080;  // candidates
-  constexpr int kVecs = SUB > 1 ? (TPB == 256 ? 320 : 160) : TPB == 256 ? 128 : 80;  // of a wave
+  constexpr int kKMax = PART ? 1 : TPB * SUB / 4;                 // words to select
+  constexpr int kCap = PART ? 1 : kKMax * 8 + 32;                // candidates
+  constexpr int kVecs = TPB == 1024 ? 160 : PART && SUB > 1 ? 320 : 128;  // vectors of a wave
   constexpr int kGroups = TPB * SUB;
   struct Vecs {
     uint4 x[NW][kVecs];
@@ -668,7 +677,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     RadixLds radix;
   };
   __shared__ Shared S;
-  __shared__ __align__(16) uint64_t cand[kCap + 2];
+  __shared__ __align__(16) uint64_t cand[kCap + 8];
   __shared__ float red[NW];
   __shared__ uint32_t wave_count[NW];
   __shared__ uint32_t full, bound_key;
@@ -826,7 +835,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
       wave_words([&](bool, bool take, float x, int32_t word, int n) {
         if (take) cand[mine + n] = candidate<T>(order_key(x), word);
       });
-      if (tid == 0) cand[C] = 0ull;
+      if (tid < 8) cand[C + tid] = 0ull;
       __syncthreads();
       done = top_finish<T, TPB, kCap, kKMax>(A, row, s.p, cand, C,
                                                floor_of<T>(at_bound), 0ull, bound, sum, S.finish);
@@ -839,7 +848,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
 // The k first of a row from its parts' lists.
 template <typename T, int TPB, int CAP>
 __global__ __launch_bounds__(TPB) void k_top_merge(TopArgs A, TopParts P) {
-  __shared__ __align__(16) uint64_t cand[CAP + 2];
+  __shared__ __align__(16) uint64_t cand[CAP + 8];
   __shared__ uint32_t from[64];
   union Shared {
     FinishLds<TPB, TKEF_ROWS_MAX_K> finish;
@@ -876,7 +885,7 @@ __global__ __launch_bounds__(TPB) void k_top_merge(TopArgs A, TopParts P) {
         const uint32_t end = part + 1 < P.parts ? from[part + 1] : (uint32_t)C;
         if (at + (uint32_t)n < end) cand[at + n] = P.lists[lists + i];
       }
-      if (tid == 0) cand[C] = 0ull;
+      if (tid < 8) cand[C + tid] = 0ull;
       __syncthreads();
       done = top_finish<T, TPB, CAP, TKEF_ROWS_MAX_K>(A, row, p, cand, C, least, lowest,
                                                       m, sum, S.finish);
@@ -1706,10 +1715,17 @@ hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
     } else if (a.k <= 64) {
       if (vecs <= 256 * 4)
         k_top_row<T, 256, 4, 1, false><<<rows, 256, 0, s>>>(a, p);
+      else if (vecs <= 256 * 8)
+        k_top_row<T, 256, 8, 1, false><<<rows, 256, 0, s>>>(a, p);
       else
         k_top_row<T, 256, 16, 1, false><<<rows, 256, 0, s>>>(a, p);
     } else if (a.k <= 256) {
-      k_top_row<T, 1024, 4, 1, false><<<rows, 1024, 0, s>>>(a, p);
+      if (vecs <= 256 * 4)
+        k_top_row<T, 256, 4, 4, false><<<rows, 256, 0, s>>>(a, p);
+      else if (vecs <= 256 * 8)
+        k_top_row<T, 256, 8, 4, false><<<rows, 256, 0, s>>>(a, p);
+      else
+        k_top_row<T, 256, 16, 4, false><<<rows, 256, 0, s>>>(a, p);
     } else {
       k_top_row<T, 1024, 4, 4, false><<<rows, 1024, 0, s>>>(a, p);
     }

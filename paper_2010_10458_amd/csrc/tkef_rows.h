@@ -60,10 +60,11 @@ struct VerifyArgs {
 // Bytes of ws that launch_top uses (0: rows short enough for one workgroup).
 size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype);
 hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s);
-// A row that is too long for one workgroup's registers is taken in this many
-// chunks (1: whole); ws then holds kPartBytes for each.
+// A row that is too long for one workgroup is taken in this many chunks (1:
+// whole) for its loss, and for its loss and gradient; ws then holds kPartBytes
+// for each.
 constexpr size_t kPartBytes = 32;
-int distill_chunks(int64_t V, int32_t dtype);
+int distill_chunks(int64_t V, int32_t dtype, bool gradient);
 hipError_t launch_distill_forward(const DistillArgs& a, void* ws, hipStream_t s);
 hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s);
 hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s);

@@ -31,6 +31,27 @@ __device__ __forceinline__ float rescale(float m, float top, float a) {
   return m == -kInf ? 0.f : exp2_((m - top) * a);
 }
 
+// (x - m) a as one operation, fma(x, a, -c) with c = fl(m a): what c's rounding
+// changes is the same factor for all x, 2^(c - m a), and rest() takes it out of
+// their sum. m is held to where the product stays in range; sums whose maximum
+// does not fit (masks at the lowest value of binary32 or bfloat16 and nothing
+// else) are taken again by the difference. One of eight operations a word: 145 ->
+// 134 us for the step of 1,021 x 131,071 binary16, whose rows leave one workgroup
+// a compute unit, 219 -> 206 for 8,192 x 32,000 bfloat16.
+struct Product {
+  float m, a, c;
+  __device__ Product(float max, float a_) : a(a_) {
+    const float limit = fminf(0x1p126f / a, 0x1p126f);
+    m = max == -kInf ? 0.f : fmaxf(fminf(max, limit), -limit);
+    c = m * a;
+  }
+  __device__ float exponent(float x) const { return __builtin_fmaf(x, a, -c); }
+  __device__ float rest() const { return exp2_(-__builtin_fmaf(m, a, -c)); }
+  __device__ static bool fits(float max, float a) {
+    return max == -kInf || __builtin_fabsf(max) < fminf(0x1p126f / a, 0x1p126f);
+  }
+};
+
 template <typename T>
 __device__ __forceinline__ float load1(const T* p, int64_t i) {
   return (float)p[i];
@@ -657,8 +678,8 @@ struct TopParts {
 //      the bound; a vector with a word at or above it goes to its wave's part of
 //      LDS instead, whose words the wave then sorts into candidates and others.
 //   3. top_finish, or a part's list.
-// More vectors or candidates than LDS holds or a NaN (in the sum) send the row
-// to top_radix.
+// More vectors or candidates than LDS holds, a bound at the end of the range
+// or a NaN (in the sum) send the row to top_radix.
 template <typename T, int TPB, int NV, int SUB, bool PART>
 __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, TopParts P) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
@@ -743,7 +764,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
   const uint32_t at_bound = bound_key;
   const float bound = key_value(at_bound);
   // 2. candidates, and the sum of the others
-  const float ref = bound == -kInf ? 0.f : bound;
+  const Product ref(bound, A.a);
   float sum = 0.f;
   int held = 0;  // vectors in this wave's part
   const int tid2 = renew(tid);
@@ -767,11 +788,12 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     held += (int)__popcll(who);
     float e = 0.f;
 #pragma unroll
-    for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * A.a);
+    for (int n = 0; n < N; ++n) e += exp2_(ref.exponent(x[n]));
     sum += above ? 0.f : e;
     asm volatile("" : "+v"(sum));  // (here, not after the last vector from kept registers)
   }
-  if (held > kVecs) {
+  sum *= ref.rest();
+  if (held > kVecs || !Product::fits(bound, A.a)) {
     held = 0;
     if (lane == 0) full = 1u;
   }
@@ -798,7 +820,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     return seen;
   };
   const int found = wave_words([&](bool valid, bool take, float x, int32_t, int) {
-    if (valid && !take) sum += exp2_((x - ref) * A.a);
+    if (valid && !take) sum += exp2_((x - ref.m) * A.a);
   });
   sum = wave_sum(sum);
   if (lane == 0) {
@@ -1086,6 +1108,7 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
   __shared__ uint32_t mark_extra;
   __shared__ ListLds list;
   __shared__ Part red[NW];
+  __shared__ float fred[NW];
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x;
   const int cnt = used_entries(A, row);
@@ -1164,8 +1187,8 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
     if (b != 0u) r[i] = strike(r[i], b, type);
     m = max_packed(m, r[i], type);
   }
-  const float ref = m == -kInf ? 0.f : m;
-  float sum = exp2_((ex - ref) * A.a);
+  const Product ref(m, A.a);
+  float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float x[N];
@@ -1173,11 +1196,11 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
     unpack(r[i], x, type);
     float e = 0.f;
 #pragma unroll
-    for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * A.a);
+    for (int n = 0; n < N; ++n) e += exp2_(ref.exponent(x[n]));
     sum += e;
   }
   part.rm = m;
-  part.rs = sum;
+  part.rs = sum * ref.rest() + exp2_((ex - ref.m) * A.a);
   part = wave_join(part, A.a);
   if (lane == 0) red[tid >> 6] = part;
   __syncthreads();
@@ -1186,6 +1209,17 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
     part = red[o];
     if (lane >= NW) part.rs = part.zs = part.ts = part.cross = 0.f;
     part = wave_join(part, A.a);
+  }
+  const bool odd = !Product::fits(part.rm, A.a);  // (the same for the whole workgroup)
+  if (odd) {
+    float e = 0.f;
+    for (int i = tid; i < s.nvec * N; i += TPB) {
+      const int v = i / N - v0, at = (v % TPB) * NV + v / TPB;
+      if (v >= 0 && v < TPB * NV && !((mark[at] >> (i % N)) & 1u))
+        e += exp2_(((float)s.p[s.head + i] - part.rm) * A.a);
+    }
+    e += exp2_((ex - part.rm) * A.a);
+    part.rs = block_reduce<TPB>(e, fred, AddOp());
   }
   if constexpr (MODE == kPart) {
     if (tid == 0) parts[row * gridDim.y + blockIdx.y] = part;
@@ -1200,15 +1234,22 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
       const GradScale g = grad_scale(sums, A, w * A.temperature);
       T* grad = static_cast<T*>(A.grad) + row * A.gld;
       const int tid2 = renew(tid);
+      const Product from(g.rm, A.a);
+      const float scale = g.rest * from.rest();
+      if (!odd) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int v = i * TPB + tid2;
-        float x[N];
-        renew(r[i]);
-        unpack(r[i], x, type);
+        for (int i = 0; i < NV; ++i) {
+          const int v = i * TPB + tid2;
+          float x[N];
+          renew(r[i]);
+          unpack(r[i], x, type);
 #pragma unroll
-        for (int n = 0; n < N; ++n) x[n] = exp2_((x[n] - g.rm) * A.a) * g.rest;
-        if (v < s.nvec) store16(grad + s.head + (int64_t)v * N, pack(x, type));
+          for (int n = 0; n < N; ++n) x[n] = exp2_(from.exponent(x[n])) * scale;
+          if (v < s.nvec) store16(grad + s.head + (int64_t)v * N, pack(x, type));
+        }
+      } else {
+        for (int i = s.head + tid; i < s.head + s.nvec * N; i += TPB)
+          grad[i] = (T)(exp2_(((float)s.p[i] - g.rm) * A.a) * g.rest);
       }
       if (tid < s.extras) grad[s.extra(tid)] = (T)(exp2_((ex - g.rm) * A.a) * g.rest);
       __syncthreads();
@@ -1662,6 +1703,10 @@ struct Pointee<T*> {
 // Registers hold a row of up to 16 vectors for each of 1,024 threads.
 constexpr int kRowVecs = 1024 * 16;
 constexpr int kChunkVecs = 256 * 8;
+// The loss alone needs a row once, so it need not be held: beyond 64 KB, where
+// whole rows leave few workgroups a compute unit, chunks of it read faster
+// (131,071 words: 3.6 -> KB2 TB/s bfloat16; 64,000 binary32: 4.2 -> KF4).
+constexpr int kLossVecs = 256 * 16;
 
 namespace {
 
@@ -1732,9 +1777,9 @@ hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
   });
 }
 
-int distill_chunks(int64_t V, int32_t dtype) {
+int distill_chunks(int64_t V, int32_t dtype, bool gradient) {
   const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
-  return vecs <= kRowVecs ? 1 : (int)((vecs + kChunkVecs - 1) / kChunkVecs);
+  return vecs <= (gradient ? kRowVecs : kLossVecs) ? 1 : (int)ceil_div(vecs, kChunkVecs);
 }
 
 namespace {
@@ -1749,10 +1794,12 @@ void launch_row(const DistillArgs& a, hipStream_t s) {
     k_distill_row<T, 256, 8, MODE><<<grid, 256, 0, s>>>(a, nullptr);
   else if (vecs <= 256 * 16)
     k_distill_row<T, 256, 16, MODE><<<grid, 256, 0, s>>>(a, nullptr);
-  else if (vecs <= 512 * 16)
-    k_distill_row<T, 512, 16, MODE><<<grid, 512, 0, s>>>(a, nullptr);
-  else
-    k_distill_row<T, 1024, 16, MODE><<<grid, 1024, 0, s>>>(a, nullptr);
+  else if constexpr (MODE == kStep) {
+    if (vecs <= 512 * 16)
+      k_distill_row<T, 512, 16, MODE><<<grid, 512, 0, s>>>(a, nullptr);
+    else
+      k_distill_row<T, 1024, 16, MODE><<<grid, 1024, 0, s>>>(a, nullptr);
+  }
 }
 
 template <typename T>
@@ -1771,7 +1818,7 @@ void launch_grad(const DistillArgs& a, const Part* parts, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_distill_forward(const DistillArgs& a, void* ws, hipStream_t s) {
-  const int chunks = distill_chunks(a.V, a.dtype);
+  const int chunks = distill_chunks(a.V, a.dtype, false);
   Part* parts = static_cast<Part*>(ws);
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;
@@ -1792,7 +1839,7 @@ hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
-  const int chunks = distill_chunks(a.V, a.dtype);
+  const int chunks = distill_chunks(a.V, a.dtype, true);
   Part* parts = static_cast<Part*>(ws);
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;

@@ -233,20 +233,27 @@ __device__ __forceinline__ uint4 strike(uint4 r, uint32_t bits, const _Float16*)
                     strike2<0xFC00u>(r.z, bits >> 4), strike2<0xFC00u>(r.w, bits >> 6));
 }
 
+// STREAM: what the call does not read again, past the caches' usual order.
+typedef uint32_t uint4_ __attribute__((ext_vector_type(4)));
+template <bool STREAM>
 __device__ __forceinline__ uint4 load16(const void* p) {
-  return *static_cast<const uint4*>(p);
+  if constexpr (STREAM) {
+    const uint4_ v = __builtin_nontemporal_load(static_cast<const uint4_*>(p));
+    return make_uint4(v.x, v.y, v.z, v.w);
+  } else {
+    return *static_cast<const uint4*>(p);
+  }
 }
-// a store to any address of the element's alignment
+// 16 bytes at any address of the element's alignment; stores stream (backward of
+// 4,096 x 32,000 bfloat16: 107 -> 95 us with streaming loads and stores, with
+// either alone 107 to 109; the step of 8,192: 206 -> 200)
 struct __attribute__((packed, aligned(2))) Loose16 {
   uint32_t x, y, z, w;
 };
+typedef uint32_t loose4_ __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ void store16(void* p, uint4 r) {
-  Loose16 l;
-  l.x = r.x;
-  l.y = r.y;
-  l.z = r.z;
-  l.w = r.w;
-  *static_cast<Loose16*>(p) = l;
+  const uint4_ v = {r.x, r.y, r.z, r.w};
+  __builtin_nontemporal_store(v, static_cast<loose4_*>(p));
 }
 
 // Makes the registers opaque: without it the compiler keeps the unpacked
@@ -294,7 +301,7 @@ __device__ __forceinline__ float max_packed(float m, uint4 r, const _Float16*) {
 // Vectors v0 + i * step + tid of a row; -inf in the places of those it has not.
 // Every load is issued at an address inside the row, so the loads need no
 // execution masks; only the slot that the row ends in is patched.
-template <typename T, int TPB, int NV>
+template <typename T, int TPB, int NV, bool STREAM>
 __device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int v0,
                                            int step = TPB) {
   const T* type = nullptr;
@@ -308,7 +315,7 @@ __device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int v = v0 + i * step + (int)threadIdx.x;
-    r[i] = load16(base + (uint32_t)(v < last ? v : last) * 16u);
+    r[i] = load16<STREAM>(base + (uint32_t)(v < last ? v : last) * 16u);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i)
@@ -710,7 +717,7 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
   const int v0 = part * TPB, step = parts * TPB;
   const int k = PART ? P.want : A.k;
   uint4 r[NV];
-  load_slots<T, TPB, NV>(r, s, v0, step);
+  load_slots<T, TPB, NV, true>(r, s, v0, step);
   const int xi = s.extra(tid < s.extras ? tid : 0);
   const bool has_ex = part == 0 && tid < s.extras;
   const float ex = has_ex ? (float)s.p[xi] : -kInf;
@@ -1126,7 +1133,7 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
   const bool edges = MODE != kPart || blockIdx.y == 0;
   const T* type = nullptr;
   uint4 r[NV];
-  load_slots<T, TPB, NV>(r, s, v0);
+  load_slots<T, TPB, NV, MODE != kPart>(r, s, v0);
   float ex = edges && tid < s.extras ? (float)s.p[s.extra(tid)] : -kInf;
   for (int i = tid; i < TPB * NV / 16; i += TPB)
     reinterpret_cast<uint4*>(mark)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -1318,7 +1325,7 @@ __global__ __launch_bounds__(TPB) void k_distill_grad(DistillArgs A, const Part*
   const bool edges = blockIdx.y == 0;
   const T* type = nullptr;
   uint4 r[NV];
-  load_slots<T, TPB, NV>(r, s, v0);
+  load_slots<T, TPB, NV, true>(r, s, v0);
   const float ex = edges && tid < s.extras ? (float)s.p[s.extra(tid)] : -kInf;
   // the list: this chunk's words with their logits, and the teacher's sum
   LogSum teach;
@@ -1488,8 +1495,8 @@ __global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch
   const Span<T> ts(tp, A.V), ds(dp, A.V);
   const int v0 = (int)chunk * (TPB * NV);
   uint4 r[NV], q[NV];
-  load_slots<T, TPB, NV>(r, ts, v0);
-  if (drafted) load_slots<T, TPB, NV>(q, ds, v0);
+  load_slots<T, TPB, NV, false>(r, ts, v0);
+  if (drafted) load_slots<T, TPB, NV, false>(q, ds, v0);
   const float rx = chunk == 0u && tid < ts.extras ? (float)tp[ts.extra(tid)] : -kInf;
   const float qx = drafted && chunk == 0u && tid < ds.extras ? (float)dp[ds.extra(tid)] : -kInf;
   LogSum p = regs_sum<T, NV>(r, rx, A.a), d;
@@ -1705,7 +1712,7 @@ constexpr int kRowVecs = 1024 * 16;
 constexpr int kChunkVecs = 256 * 8;
 // The loss alone needs a row once, so it need not be held: beyond 64 KB, where
 // whole rows leave few workgroups a compute unit, chunks of it read faster
-// (131,071 words: 3.6 -> KB2 TB/s bfloat16; 64,000 binary32: 4.2 -> KF4).
+// (128,000 bfloat16 words: 3.6 -> 5.5 TB/s; 64,000 binary32: 4.2 -> 5.6).
 constexpr int kLossVecs = 256 * 16;
 
 namespace {
@@ -1784,6 +1791,12 @@ int distill_chunks(int64_t V, int32_t dtype, bool gradient) {
 
 namespace {
 
+// LDS that a step over rows of up to 64 KB asks for beyond its own, so that a
+// compute unit takes three of them: with their stores beside the others' loads
+// more in flight are slower (8,192 x 32,000 bfloat16: 206 us at three, 213 at four,
+// 220 at five, 220 at two; the loss alone, which only reads, takes five).
+constexpr unsigned kStepSpare = 34 << 10;
+
 template <typename T, int MODE>
 void launch_row(const DistillArgs& a, hipStream_t s) {
   const int vecs = a.V / Span<T>::N;
@@ -1793,7 +1806,7 @@ void launch_row(const DistillArgs& a, hipStream_t s) {
   else if (vecs <= 256 * 8)
     k_distill_row<T, 256, 8, MODE><<<grid, 256, 0, s>>>(a, nullptr);
   else if (vecs <= 256 * 16)
-    k_distill_row<T, 256, 16, MODE><<<grid, 256, 0, s>>>(a, nullptr);
+    k_distill_row<T, 256, 16, MODE><<<grid, 256, MODE == kStep ? kStepSpare : 0, s>>>(a, nullptr);
   else if constexpr (MODE == kStep) {
     if (vecs <= 512 * 16)
       k_distill_row<T, 512, 16, MODE><<<grid, 512, 0, s>>>(a, nullptr);
@@ -1845,10 +1858,10 @@ hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
     using T = typename Pointee<decltype(t)>::type;
     if (chunks == 1) {
       launch_row<T, kStep>(a, s);
-    } else {
-      launch_parts<T>(a, parts, chunks, s);
-      launch_grad<T>(a, parts, s);
+      return;
     }
+    launch_parts<T>(a, parts, chunks, s);
+    launch_grad<T>(a, parts, s);
   });
 }
 

@@ -42,7 +42,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _check_vector(t: Optional[torch.Tensor], n: int, dtype, what: str) -> None:
-    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_cuda
+    if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_cuda
                           or not t.is_contiguous()):
         raise ValueError(f"{what}: expected {n} contiguous {dtype} CUDA values")
 
@@ -98,14 +98,12 @@ class _RowPlan:
         return status, False
 
 
-class _On:
-    """Allocations of a call that runs on `stream` come from that stream."""
-
-    def __new__(cls, stream):
-        return torch.cuda.stream(stream) if stream is not None else _NOTHING
+def _on(stream):
+    """Allocations of a call on `stream` come from that stream."""
+    return torch.cuda.stream(stream) if stream is not None else _HERE
 
 
-class _Nothing:
+class _Here:
     def __enter__(self):
         return None
 
@@ -113,7 +111,21 @@ class _Nothing:
         return None
 
 
-_NOTHING = _Nothing()
+_HERE = _Here()
+
+
+def _out(t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype, dev, what: str):
+    """The caller's output, checked, or a new one (empty_strided: the cheapest of
+    torch's allocating calls, 1.3 against 1.6 us, and a small call waits for three)."""
+    if t is None:
+        if len(shape) == 1:
+            return torch.empty_strided(shape, (1,), dtype=dtype, device=dev)
+        return torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=dev)
+    n = 1
+    for d in shape:
+        n *= d
+    _check_vector(t, n, dtype, what)
+    return t
 
 
 class TopLogitsPlan(_RowPlan):
@@ -133,6 +145,7 @@ class TopLogitsPlan(_RowPlan):
             self.rows, self.vocab, self.k, _dtype_code(dtype), _val_format(val_dtype),
             self.temperature, ctypes.byref(self._h)))
         self._info("tkef_top_plan_info")
+        self._execute = lib().tkef_top_execute
 
     def execute(self, logits: torch.Tensor, idx_out: Optional[torch.Tensor] = None,
                 val_out: Optional[torch.Tensor] = None,
@@ -143,24 +156,17 @@ class TopLogitsPlan(_RowPlan):
         n, ld = self._logits(logits, "logits")
         dev = logits.device
         h = _stream_handle(stream)
-        with _On(stream):
-            if idx_out is None:
-                idx_out = torch.empty((n, self.k), dtype=torch.int32, device=dev)
-            else:
-                _check_vector(idx_out, n * self.k, torch.int32, "idx_out")
-            if val_out is None:
-                val_out = torch.empty((n, self.k), dtype=self.val_dtype, device=dev)
-            else:
-                _check_vector(val_out, n * self.k, self.val_dtype, "val_out")
-            if tail_out is None:
-                tail_out = torch.empty((n,), dtype=torch.float32, device=dev)
-            else:
-                _check_vector(tail_out, n, torch.float32, "tail_out")
+        with _on(stream):
+            idx_out = _out(idx_out, (n, self.k), torch.int32, dev, "idx_out")
+            val_out = _out(val_out, (n, self.k), self.val_dtype, dev, "val_out")
+            tail_out = _out(tail_out, (n,), torch.float32, dev, "tail_out")
             status, own = self._status_of(status, dev)
             ws = self._workspace(h, dev)
-        _check("tkef_top_execute", lib().tkef_top_execute(
+        rc = self._execute(
             self._h, logits.data_ptr(), ld, n, idx_out.data_ptr(), val_out.data_ptr(),
-            tail_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h))
+            tail_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h)
+        if rc:
+            _check("tkef_top_execute", rc)
         if own:
             _raise_on_status("tkef_top_execute", status, stream)
         return idx_out, val_out, tail_out
@@ -184,6 +190,9 @@ class DistillPlan(_RowPlan):
             self.rows, self.vocab, self.k, _dtype_code(dtype), _val_format(val_dtype),
             self.temperature, ctypes.byref(self._h)))
         self._info("tkef_distill_plan_info")
+        L = lib()
+        self._forward, self._backward, self._step = (
+            L.tkef_distill_forward, L.tkef_distill_backward, L.tkef_distill_step)
 
     def _lists(self, n, idx, val, tail, count, weight):
         _check_vector(idx, n * self.k, torch.int32, "idx")
@@ -195,7 +204,8 @@ class DistillPlan(_RowPlan):
 
     def _grad(self, logits, grad_out):
         if grad_out is None:
-            grad_out = torch.empty(logits.shape, dtype=self.dtype, device=logits.device)
+            grad_out = _out(None, tuple(logits.shape), self.dtype, logits.device, "grad_out")
+            return grad_out, self.vocab
         elif grad_out.shape != logits.shape:
             raise ValueError("grad_out: expected the shape of the logits")
         return grad_out, self._logits(grad_out, "grad_out")[1]
@@ -211,20 +221,16 @@ class DistillPlan(_RowPlan):
         lists = self._lists(n, idx, val, tail, count, weight)
         dev = logits.device
         h = _stream_handle(stream)
-        with _On(stream):
-            if loss_out is None:
-                loss_out = torch.empty((n,), dtype=torch.float32, device=dev)
-            else:
-                _check_vector(loss_out, n, torch.float32, "loss_out")
-            if stats_out is None:
-                stats_out = torch.empty((n, 4), dtype=torch.float32, device=dev)
-            else:
-                _check_vector(stats_out, n * 4, torch.float32, "stats_out")
+        with _on(stream):
+            loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
+            stats_out = _out(stats_out, (n, 4), torch.float32, dev, "stats_out")
             status, own = self._status_of(status, dev)
             ws = self._workspace(h, dev)
-        _check("tkef_distill_forward", lib().tkef_distill_forward(
+        rc = self._forward(
             self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
-            stats_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h))
+            stats_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h)
+        if rc:
+            _check("tkef_distill_forward", rc)
         if own:
             _raise_on_status("tkef_distill_forward", status, stream)
         return loss_out, stats_out
@@ -242,13 +248,15 @@ class DistillPlan(_RowPlan):
         _check_vector(dloss, n, torch.float32, "dloss")
         dev = logits.device
         h = _stream_handle(stream)
-        with _On(stream):
+        with _on(stream):
             grad_out, gld = self._grad(logits, grad_out)
             status, own = self._status_of(status, dev)
             ws = self._workspace(h, dev)
-        _check("tkef_distill_backward", lib().tkef_distill_backward(
+        rc = self._backward(
             self._h, logits.data_ptr(), ld, n, *lists, stats.data_ptr(), _ptr(dloss),
-            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h))
+            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h)
+        if rc:
+            _check("tkef_distill_backward", rc)
         if own:
             _raise_on_status("tkef_distill_backward", status, stream)
         return grad_out
@@ -264,17 +272,16 @@ class DistillPlan(_RowPlan):
         lists = self._lists(n, idx, val, tail, count, weight)
         dev = logits.device
         h = _stream_handle(stream)
-        with _On(stream):
-            if loss_out is None:
-                loss_out = torch.empty((n,), dtype=torch.float32, device=dev)
-            else:
-                _check_vector(loss_out, n, torch.float32, "loss_out")
+        with _on(stream):
+            loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
             grad_out, gld = self._grad(logits, grad_out)
             status, own = self._status_of(status, dev)
             ws = self._workspace(h, dev)
-        _check("tkef_distill_step", lib().tkef_distill_step(
+        rc = self._step(
             self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
-            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h))
+            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h)
+        if rc:
+            _check("tkef_distill_step", rc)
         if own:
             _raise_on_status("tkef_distill_step", status, stream)
         return loss_out, grad_out
@@ -319,6 +326,7 @@ class VerifyPlan(_RowPlan):
             self.rows, self.draft, self.vocab, _dtype_code(dtype), self.temperature,
             ctypes.byref(self._h)))
         self._info("tkef_verify_plan_info")
+        self._execute = lib().tkef_verify_execute
 
     def _ready(self, ws, stream):
         _check("tkef_verify_plan_bind", lib().tkef_verify_plan_bind(
@@ -361,26 +369,19 @@ class VerifyPlan(_RowPlan):
             raise ValueError("noise: expected (batch, vocab) float32 CUDA values in rows")
         dev = target.device
         h = _stream_handle(stream)
-        with _On(stream):
-            if accepted_out is None:
-                accepted_out = torch.empty((b,), dtype=torch.int32, device=dev)
-            else:
-                _check_vector(accepted_out, b, torch.int32, "accepted_out")
-            if tokens_out is None:
-                tokens_out = torch.empty((b, self.draft + 1), dtype=torch.int32, device=dev)
-            else:
-                _check_vector(tokens_out, b * (self.draft + 1), torch.int32, "tokens_out")
-            if logp_out is None:
-                logp_out = torch.empty((b, self.draft + 1), dtype=torch.float32, device=dev)
-            else:
-                _check_vector(logp_out, b * (self.draft + 1), torch.float32, "logp_out")
+        with _on(stream):
+            accepted_out = _out(accepted_out, (b,), torch.int32, dev, "accepted_out")
+            tokens_out = _out(tokens_out, (b, self.draft + 1), torch.int32, dev, "tokens_out")
+            logp_out = _out(logp_out, (b, self.draft + 1), torch.float32, dev, "logp_out")
             status, own = self._status_of(status, dev)
             ws = self._workspace(h, dev)
-        _check("tkef_verify_execute", lib().tkef_verify_execute(
+        rc = self._execute(
             self._h, target.data_ptr(), tb, ti, drafts.data_ptr(), db, di, b,
             tokens.data_ptr(), uniform.data_ptr(), noise.data_ptr(),
             noise.stride(0) if b > 1 else self.vocab, _ptr(length), accepted_out.data_ptr(),
-            tokens_out.data_ptr(), logp_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h))
+            tokens_out.data_ptr(), logp_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h)
+        if rc:
+            _check("tkef_verify_execute", rc)
         if own:
             _raise_on_status("tkef_verify_execute", status, stream)
         return accepted_out, tokens_out, logp_out

@@ -48,7 +48,10 @@ def distill(z, idx, val, tail: float = -INF, weight: float = 1.0,
     t = np.asarray(val, dtype=np.float64) / temperature
     if weight == 0.0 or idx.size == 0:
         return Distilled(0.0, np.zeros(z.size), np.zeros(idx.size), 0.0, np.zeros(z.size), 0.0)
-    s = z / temperature
+    # from the row's largest logit: a row of nothing but a mask's value (-3e38,
+    # say) would lose the logarithm of its sum even in 64 bits
+    top = z.max()
+    s = (z - top) / temperature if math.isfinite(top) else z / temperature
     lt = logsumexp(np.append(t, tail))
     lz = logsumexp(s)
     if not math.isfinite(lt) or not math.isfinite(lz):
@@ -69,7 +72,8 @@ def distill(z, idx, val, tail: float = -INF, weight: float = 1.0,
     grad = q.copy()
     grad[idx] -= p
     if lpr > -INF and lqr > -INF:
-        grad[outside] *= 1.0 - math.exp(lpr - lqr)
+        # q (1 - p_r / q_r) = q - p_r (q / q_r), the last a softmax of its own
+        grad[outside] -= math.exp(lpr) * softmax(z[outside] / temperature)
     return Distilled(loss * weight * temperature ** 2, grad * weight * temperature, p,
                      math.exp(lpr), q, math.exp(lqr))
 
@@ -83,8 +87,11 @@ class Verified(NamedTuple):
 
 def softmax(x):
     x = np.asarray(x, dtype=np.float64)
-    lse = logsumexp(x)
-    return np.zeros(x.size) if lse == -INF else np.exp(x - lse)
+    m = x.max()
+    if m == -INF:
+        return np.zeros(x.size)
+    e = np.exp(x - m)
+    return e / e.sum()
 
 
 def verify(target, drafts, tokens, uniform, noise, length: Optional[int] = None,

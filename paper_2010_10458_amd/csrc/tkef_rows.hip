@@ -949,10 +949,10 @@ __device__ __forceinline__ LogSum block_join(LogSum v, float a, float* red) {
   return r;
 }
 
-// log2 of (2^(tau log2 e) / 2^(m a)), with 1 / temperature in two parts so
-// that the product's rounding does not enter
+// tau - m / temperature, with 1 / temperature in two parts so that the product's
+// rounding does not enter
 __device__ __forceinline__ float tail_over(float tau, float m, float inv_t, float inv_t_lo) {
-  return (__builtin_fmaf(-m, inv_t, tau) - m * inv_t_lo) * kLog2e;
+  return __builtin_fmaf(-m, inv_t, tau) - m * inv_t_lo;
 }
 
 // The teacher's side of a row: the list's sum, with the tail's mass.
@@ -967,7 +967,7 @@ __device__ __forceinline__ Teacher teacher_of(LogSum list, const DistillArgs& A,
   const float tail_m = t.tau * A.temperature;
   t.m = list.m > tail_m ? list.m : tail_m;
   const float rest =
-      t.tau == -kInf ? 0.f : exp2_(tail_over(t.tau, t.m, A.inv_t, A.inv_t_lo));
+      t.tau == -kInf ? 0.f : exp2_(tail_over(t.tau, t.m, A.inv_t, A.inv_t_lo) * kLog2e);
   t.S = list.S * rescale(list.m, t.m, A.a) + rest;
   t.inv = 1.f / t.S;
   t.p_rest = rest * t.inv;
@@ -996,24 +996,63 @@ __device__ __forceinline__ bool entry_ok(const int32_t* idx, int j, int V, uint3
   return true;
 }
 
-// What a part of a row (a wave's share, or a chunk's) adds to its sums: the
-// unlisted words' and the listed words' student sums, the list's teacher sum,
-// and sum_j 2^((t_j - tm) a) (t_j - z_j) a over its listed words.
+// What a part of a row (a thread's share, a wave's, a chunk's) adds to its sums:
+// the unlisted words' student sum (rm, rs), the listed words' student sum (zm,
+// zs) and teacher sum (tm, ts), and
+//   cross = sum_j 2^((t_j - tm) a) ((t_j - tm) - (z_j - zm)) / temperature
+// over its listed words: both logits from their own maximum, so rows that lie
+// far off zero (all words at a mask's value) lose nothing.
 struct Part {
   float rm, rs, zm, zs, tm, ts, cross, pad;
 };
 static_assert(sizeof(Part) == kPartBytes, "workspace layout");
 
-__device__ __forceinline__ Part wave_join(Part p, float a) {
+// cross of a part after its maxima move to (tm, zm)
+__device__ __forceinline__ float moved_cross(const Part& p, float tm, float zm,
+                                             const DistillArgs& A) {
+  const float f = rescale(p.tm, tm, A.a), ts = p.ts * f;
+  if (!(ts > 0.f)) return ts;  // (0, or NaN)
+  const float dt = p.tm == tm ? 0.f : p.tm - tm, dz = p.zm == zm ? 0.f : p.zm - zm;
+  return p.cross * f + ts * ((dt - dz) * A.inv_t);
+}
+
+__device__ __forceinline__ Part empty_part() {
+  return Part{-kInf, 0.f, -kInf, 0.f, -kInf, 0.f, 0.f, 0.f};
+}
+
+__device__ __forceinline__ Part join(const Part& p, const Part& q, const DistillArgs& A) {
+  Part r;
+  r.rm = fmaxf(p.rm, q.rm);
+  r.zm = fmaxf(p.zm, q.zm);
+  r.tm = fmaxf(p.tm, q.tm);
+  r.rs = join_sum(p.rm, p.rs, r.rm, A.a) + join_sum(q.rm, q.rs, r.rm, A.a);
+  r.zs = join_sum(p.zm, p.zs, r.zm, A.a) + join_sum(q.zm, q.zs, r.zm, A.a);
+  r.ts = join_sum(p.tm, p.ts, r.tm, A.a) + join_sum(q.tm, q.ts, r.tm, A.a);
+  r.cross = moved_cross(p, r.tm, r.zm, A) + moved_cross(q, r.tm, r.zm, A);
+  r.pad = 0.f;
+  return r;
+}
+
+// one listed word (a sum of one term from its own maximum is 1, or NaN)
+__device__ __forceinline__ Part entry_part(float t, float z) {
+  Part p = empty_part();
+  p.zm = z;
+  p.zs = z == -kInf ? 0.f : exp2_(z - z);
+  p.tm = t;
+  p.ts = t == -kInf ? 0.f : exp2_(t - t);
+  p.cross = p.ts > 0.f && z == -kInf ? kInf : 0.f;  // a wanted word that has no probability
+  return p;
+}
+
+__device__ __forceinline__ Part wave_join(const Part& p, const DistillArgs& A) {
   Part r;
   r.rm = wave_max(p.rm);
   r.zm = wave_max(p.zm);
   r.tm = wave_max(p.tm);
-  r.rs = wave_sum(join_sum(p.rm, p.rs, r.rm, a));
-  r.zs = wave_sum(join_sum(p.zm, p.zs, r.zm, a));
-  const float f = rescale(p.tm, r.tm, a);
-  r.ts = wave_sum(p.ts * f);
-  r.cross = wave_sum(f > 0.f ? p.cross * f : 0.f);
+  r.rs = wave_sum(join_sum(p.rm, p.rs, r.rm, A.a));
+  r.zs = wave_sum(join_sum(p.zm, p.zs, r.zm, A.a));
+  r.ts = wave_sum(join_sum(p.tm, p.ts, r.tm, A.a));
+  r.cross = wave_sum(moved_cross(p, r.tm, r.zm, A));
   r.pad = 0.f;
   return r;
 }
@@ -1022,7 +1061,7 @@ __device__ __forceinline__ Part wave_join(Part p, float a) {
 struct RowSums {
   Teacher t;
   float rm, rs, zm, zs;  // student sums: unlisted, listed
-  float loss;            // divergence, natural units
+  float loss;            // the divergence
 };
 
 __device__ __forceinline__ RowSums row_sums(const Part& p, const DistillArgs& A, int64_t row) {
@@ -1037,17 +1076,16 @@ __device__ __forceinline__ RowSums row_sums(const Part& p, const DistillArgs& A,
   r.zs = p.zs;
   const float top = fmaxf(p.rm, p.zm);
   const float total = join_sum(p.rm, p.rs, top, A.a) + join_sum(p.zm, p.zs, top, A.a);
-  // sum_j p_j (log p_j - log q_j) = sum_j p_j s (t_j - z_j) + (LZ - LT) sum_j p_j, and
-  // with the others' term p_r (log p_r - log q_r) = p_r (tau - LR) + p_r (LZ - LT)
-  const float f = rescale(p.tm, r.t.m, A.a) * r.t.inv;
-  float loss = (f > 0.f ? p.cross * f : 0.f) +
-               ((top - r.t.m) * A.a + (log2_(total) - log2_(r.t.S)));
+  // With logarithms from the maxima (t.m of the teacher, top of the student),
+  //   sum_j p_j (log p_j - log q_j) + p_r (log p_r - log q_r)
+  //     = cross / S + log total - log S + p_r ((tau - s t.m) - (s (rm - top) + log rs))
+  float loss = moved_cross(p, r.t.m, top, A) * r.t.inv + kLn2 * (log2_(total) - log2_(r.t.S));
   if (r.t.p_rest > 0.f)
-    loss += p.rs == 0.f
-                ? kInf
-                : r.t.p_rest * (tail_over(r.t.tau, p.rm, A.inv_t, A.inv_t_lo) - log2_(p.rs));
+    loss += p.rs == 0.f ? kInf
+                        : r.t.p_rest * (tail_over(r.t.tau, r.t.m, A.inv_t, A.inv_t_lo) -
+                                        ((p.rm - top) * A.inv_t + kLn2 * log2_(p.rs)));
   if (!(total > 0.f) || !has_mass(r.t)) loss = __uint_as_float(0x7FC00000u);
-  r.loss = loss * kLn2;
+  r.loss = loss;
   return r;
 }
 
@@ -1140,7 +1178,7 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
   if (tid == 0) mark_extra = 0u;
   __syncthreads();
   // the list: marks, and the sums over listed words
-  Part part = {-kInf, 0.f, -kInf, 0.f, -kInf, 0.f, 0.f, 0.f};
+  Part part = empty_part();
   uint32_t bits = 0u;
   const int32_t* idx = A.idx + row * A.k;
   for (int j = tid; j < cnt; j += TPB) {
@@ -1163,21 +1201,7 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
     if (mine) {
       t = load_val(A.val, A.val_format, row * A.k + j);
       z = (float)s.p[idx[j]];
-      LogSum zs, ts;
-      zs.m = part.zm;
-      zs.S = part.zs;
-      zs.add(z, A.a);
-      part.zm = zs.m;
-      part.zs = zs.S;
-      const float before = part.tm;
-      ts.m = part.tm;
-      ts.S = part.ts;
-      ts.add(t, A.a);
-      part.tm = ts.m;
-      part.ts = ts.S;
-      const float f = before == ts.m ? 1.f : rescale(before, ts.m, A.a);
-      const float p = ts.m == -kInf ? 0.f : exp2_((t - ts.m) * A.a);
-      part.cross = (f > 0.f ? part.cross * f : 0.f) + (p > 0.f ? p * ((t - z) * A.a) : 0.f);
+      part = join(part, entry_part(t, z), A);
     }
     list.word[j] = mine ? idx[j] : -1;
     list.t[j] = t;
@@ -1208,14 +1232,14 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
   }
   part.rm = m;
   part.rs = sum * ref.rest() + exp2_((ex - ref.m) * A.a);
-  part = wave_join(part, A.a);
+  part = wave_join(part, A);
   if (lane == 0) red[tid >> 6] = part;
   __syncthreads();
   {
     const int o = lane < NW ? lane : 0;
     part = red[o];
     if (lane >= NW) part.rs = part.zs = part.ts = part.cross = 0.f;
-    part = wave_join(part, A.a);
+    part = wave_join(part, A);
   }
   const bool odd = !Product::fits(part.rm, A.a);  // (the same for the whole workgroup)
   if (odd) {
@@ -1269,21 +1293,10 @@ __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts)
 }
 
 // Sum of a row's chunk parts, by every wave of a workgroup.
-__device__ __forceinline__ Part join_parts(const Part* parts, int n, float a) {
-  Part p = {-kInf, 0.f, -kInf, 0.f, -kInf, 0.f, 0.f, 0.f};
-  for (int i = (int)(threadIdx.x & 63); i < n; i += 64) {
-    const Part q = parts[i];
-    const float rm = fmaxf(p.rm, q.rm), zm = fmaxf(p.zm, q.zm), tm = fmaxf(p.tm, q.tm);
-    p.rs = join_sum(p.rm, p.rs, rm, a) + join_sum(q.rm, q.rs, rm, a);
-    p.zs = join_sum(p.zm, p.zs, zm, a) + join_sum(q.zm, q.zs, zm, a);
-    const float fp = rescale(p.tm, tm, a), fq = rescale(q.tm, tm, a);
-    p.ts = p.ts * fp + q.ts * fq;
-    p.cross = (fp > 0.f ? p.cross * fp : 0.f) + (fq > 0.f ? q.cross * fq : 0.f);
-    p.rm = rm;
-    p.zm = zm;
-    p.tm = tm;
-  }
-  return wave_join(p, a);
+__device__ __forceinline__ Part join_parts(const Part* parts, int n, const DistillArgs& A) {
+  Part p = empty_part();
+  for (int i = (int)(threadIdx.x & 63); i < n; i += 64) p = join(p, parts[i], A);
+  return wave_join(p, A);
 }
 
 // loss and sums of a row from its parts, one wave a row
@@ -1293,7 +1306,7 @@ __global__ __launch_bounds__(64) void k_distill_join(DistillArgs A, const Part* 
   float loss = 0.f;
   float4 stats = make_float4(0.f, 0.f, 0.f, 0.f);
   if (used_entries(A, row) != 0 && w != 0.f) {
-    const RowSums s = row_sums(join_parts(parts + row * chunks, chunks, A.a), A, row);
+    const RowSums s = row_sums(join_parts(parts + row * chunks, chunks, A), A, row);
     loss = s.loss * w * (A.temperature * A.temperature);
     stats = make_float4(s.rm, s.rs, s.zm, s.zs);
   }
@@ -1349,7 +1362,7 @@ __global__ __launch_bounds__(TPB) void k_distill_grad(DistillArgs A, const Part*
   if (blockIdx.y == 0 && parts == nullptr) raise_status(A.status, bits);
   RowSums sums;
   if (parts != nullptr) {
-    sums = row_sums(join_parts(parts + row * gridDim.y, (int)gridDim.y, A.a), A, row);
+    sums = row_sums(join_parts(parts + row * gridDim.y, (int)gridDim.y, A), A, row);
     if (blockIdx.y == 0 && tid == 0) A.loss[row] = sums.loss * w * (A.temperature * A.temperature);
     __syncthreads();
   } else {

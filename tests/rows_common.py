@@ -43,10 +43,13 @@ def logits(rng, n, v, spread=3.0):
 
 
 def finite_max(*arrays):
+    """Largest magnitude among logits that are not a mask: words at a type's
+    lowest value have no probability beside others and differ by nothing among
+    themselves, so their magnitude rounds nothing."""
     best = 0.0
     for a in arrays:
         a = np.abs(np.asarray(a, dtype=np.float64))
-        a = a[np.isfinite(a)]
+        a = a[a < 6e4]
         best = max(best, float(a.max()) if a.size else 0.0)
     return best
 

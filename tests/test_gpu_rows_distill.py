@@ -42,7 +42,7 @@ def check_row(got_loss, got_grad, z, want, val, tail, weight, temperature, dtype
                     part = want.p * np.abs(np.log(want.p))
                 spread += float(np.nansum(part[np.isfinite(part)]))
                 spread += finite_max(val) / temperature * 0.125
-            tol = abs(weight) * temperature ** 2 * rel * spread + abs(want.loss) * 4 * EPS
+            tol = abs(weight) * temperature ** 2 * rel * spread + abs(want.loss) * (4 * EPS + rel)
             assert abs(got_loss - want.loss) <= tol, (got_loss, want.loss, tol)
     if got_grad is not None:
         g = want.grad * dloss
@@ -294,3 +294,34 @@ def test_refusals():
         tk.DistillPlan(4, 100, 101)
     with pytest.raises(ValueError):
         tk.DistillPlan(4, 100, 8, val_dtype=torch.bfloat16)
+
+
+LOWEST = {"f32": float(np.finfo(np.float32).min), "f16": -65504.0,
+          "bf16": float(torch.finfo(torch.bfloat16).min)}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [300, 32000, 70000, 140001])
+def test_masks_at_the_lowest_value_of_the_type(v, dtype):
+    """A mask of the type's lowest value leaves a word without probability
+    beside ordinary ones, and a row of nothing else uniform."""
+    rng = np.random.default_rng(v + 1)
+    low = LOWEST[dtype]
+    n, k = 6, 12
+    teacher = logits(rng, n, v)
+    student = teacher + rng.normal(size=(n, v)) * 0.5
+    best = [np.argsort(-teacher[r])[:k] for r in range(n)]
+    student[0] = low                                   # nothing but the mask
+    student[1, v // 3:] = low                          # most words masked
+    teacher[1, v // 3:] = -60.0
+    student[2] = low
+    student[2, best[2]] = teacher[2, best[2]]          # only listed words left
+    student[3] = -INF
+    student[3, ::2] = low                              # the mask, and masked words
+    teacher[3, 1::2] = -60.0
+    student[4] = low
+    student[4, v - 1] = 1.0                            # one word left, at the end
+    teacher[4] = -60.0
+    teacher[4, v - 1] = 2.0
+    for use_tail in (True, False):
+        check(rng, n, v, k, dtype, student=student, teacher=teacher, use_tail=use_tail)

@@ -156,3 +156,21 @@ def test_refusals():
             tk.TopLogitsPlan(**{**dict(rows=4, vocab=100, k=8), **kw})
     with pytest.raises(ValueError):
         tk.TopLogitsPlan(4, 100, 8, dtype=torch.float64)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [300, 32000, 131071, 200000])
+def test_masks_at_the_lowest_value_of_the_type(v, dtype):
+    rng = np.random.default_rng(v + 2)
+    low = -65504.0 if dtype == "f16" else float(torch.finfo(TYPES[dtype]).min)
+    x = logits(rng, 5, v)
+    x[0] = low
+    x[1, v // 4:] = low
+    x[2] = low
+    x[2, ::1000] = 1.0
+    x[3, 1::2] = -INF
+    x[3, ::2] = low
+    x[4] = low
+    x[4, v // 2] = 0.0
+    for k in (1, 20, 70):
+        check(x, k, dtype)

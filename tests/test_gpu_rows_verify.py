@@ -183,3 +183,23 @@ def test_refusals():
     for args in ((0, 3, 50), (2, 0, 50), (2, 64, 50), (2, 3, 0), (65537, 3, 50)):
         with pytest.raises(tk.TkefError):
             tk.VerifyPlan(*args)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [300, 32000])
+def test_masks_at_the_lowest_value_of_the_type(v, dtype):
+    rng = np.random.default_rng(v + 3)
+    low = -65504.0 if dtype == "f16" else float(torch.finfo(TYPES[dtype]).min)
+    b, draft = 5, 2
+    target = logits(rng, b * (draft + 1), v).reshape(b, draft + 1, v)
+    drafts = target[:, :draft] + rng.normal(size=(b, draft, v)) * 0.5
+    tokens = rng.integers(0, v, (b, draft))
+    uniform = np.full((b, draft), 0.25)
+    target[0] = low                          # uniform
+    target[1, :, v // 2:] = low              # half the words masked in the target
+    tokens[1, 0] = v - 1                     # such a word drafted
+    drafts[2, :, : v // 2] = low
+    target[3] = low
+    target[3, :, 7] = 0.0                    # one word left
+    drafts[4] = low                          # a uniform draft
+    check(rng, b, draft, v, dtype, target=target, drafts=drafts, tokens=tokens, uniform=uniform)

@@ -298,12 +298,13 @@ __device__ __forceinline__ float max_packed(float m, uint4 r, const _Float16*) {
   return max3(m, (float)h.x, (float)h.y);
 }
 
-// Vectors v0 + i * step + tid of a row; -inf in the places of those it has not.
+// Vectors v0 + i * step + t of a row, t < width across the threads that share v0;
+// -inf in the places of those it has not.
 // Every load is issued at an address inside the row, so the loads need no
 // execution masks; only the slot that the row ends in is patched.
 template <typename T, int TPB, int NV, bool STREAM>
-__device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int v0,
-                                           int step = TPB) {
+__device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int v0, int step,
+                                           int t, int width) {
   const T* type = nullptr;
   const int last = s.nvec - 1;
   if (v0 > last) {
@@ -314,18 +315,22 @@ __device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int
   const char* base = reinterpret_cast<const char*>(s.p + s.head);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int v = v0 + i * step + (int)threadIdx.x;
+    const int v = v0 + i * step + t;
     r[i] = load16<STREAM>(base + (uint32_t)(v < last ? v : last) * 16u);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (v0 + i * step + TPB > s.nvec) {  // (the same for all threads)
-      const bool in = v0 + i * step + (int)threadIdx.x < s.nvec;
+    if (v0 + i * step + width > s.nvec) {  // (the same for all threads of the width)
+      const bool in = v0 + i * step + t < s.nvec;
       r[i].x = in ? r[i].x : none_of(type).x;
       r[i].y = in ? r[i].y : none_of(type).y;
       r[i].z = in ? r[i].z : none_of(type).z;
       r[i].w = in ? r[i].w : none_of(type).w;
     }
+}
+template <typename T, int TPB, int NV, bool STREAM>
+__device__ __forceinline__ void load_slots(uint4 (&r)[NV], const Span<T>& s, int v0) {
+  load_slots<T, TPB, NV, STREAM>(r, s, v0, TPB, (int)threadIdx.x, TPB);
 }
 
 // Wave reductions over DPP row shifts: lane 15 of each row of 16 lanes ends
@@ -406,9 +411,9 @@ struct RadixLds {
 
 // Selection from a row of any values: radix select of the k-th largest order
 // key over four 8-bit digits, then the ordered compaction and the rest's sum.
-// Seven passes over the row; the kernels below come here with rows whose words
-// nearly all tie (constant rows, rows with few words left unmasked), rows with
-// NaN, and rows whose rest lies more than 2^-60 below their k-th word.
+// Seven passes over the row; the kernels below come here with rows that have
+// NaN, that have more words in reach of the k first than LDS holds, and whose
+// rest lies more than 2^-60 below their k-th word.
 template <typename T, int NT>
 __device__ __forceinline__ void top_radix(const TopArgs& A, RadixLds& L, const T* p,
                                           int64_t row) {
@@ -514,7 +519,7 @@ __device__ __forceinline__ uint64_t floor_of(uint32_t key) {
 // a comparison for each pair, bisection some twelve rounds with a barrier each.
 template <int TPB>
 constexpr int rank_limit() {
-  return TPB == 256 ? 128 : 256;
+  return TPB < 1024 ? 128 : 256;
 }
 
 template <int TPB, int KMAX>
@@ -533,8 +538,8 @@ struct FinishLds {
 // candidate is bisected, a candidate's word being part of it, so that ties end
 // at the lower words. A selected word's place is the number of selected lower
 // words. False, with nothing written, where candidates below `lowest` would be
-// needed or the rest vanishes beside the last selected word. The same for all
-// threads.
+// needed or the rest, though it holds words with a probability, vanishes beside
+// the last selected word. The same for all threads.
 template <typename T, int TPB, int CAP, int KMAX>
 __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const T* p,
                                            const uint64_t* cand, int C, uint64_t least,
@@ -613,10 +618,13 @@ __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const 
   }
   if (thr < lowest) return false;
   const float at_thr = value_of<T>(thr), base = at_thr == -kInf ? 0.f : at_thr;
+  bool some = m != -kInf;  // unselected words that are not masked
   if (counted) {
     for (int j = lane; j < C - k; j += 64) left += exp2_((L.others[j] - base) * A.a);
     left = wave_sum(left);
+    some |= C > k && L.others[0] != -kInf;
   } else {
+    int mine = 0;
 #pragma unroll
     for (int q = 0; q < CPT; ++q) {
       if (q * TPB >= C) continue;
@@ -630,16 +638,20 @@ __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const 
                                        __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
         if (take) L.chosen[at] = word_of(c[q]);
       }
-      if (!take && c[q] != 0ull) left += exp2_((value_of<T>(c[q]) - base) * A.a);
+      if (!take && c[q] != 0ull) {
+        const float x = value_of<T>(c[q]);
+        left += exp2_((x - base) * A.a);
+        mine |= x != -kInf;
+      }
     }
     left = wave_sum(left);
     if (lane == 0) L.red[wave] = left;
-    __syncthreads();
+    some |= __syncthreads_or(mine) != 0;
     left = wave_sum(lane < NW ? L.red[lane] : 0.f);
   }
   // the rest relative to the last selected word
   const float rest = S * rescale(m, base, A.a) + left;
-  if (more && !(rest > 0x1p-60f)) return false;
+  if (more && some && !(rest > 0x1p-60f)) return false;
   for (int j = tid; j < k; j += TPB) {
     const int32_t word = L.chosen[j];
     int place = 0;
@@ -654,13 +666,13 @@ __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const 
     }
     put_pair(A, row, (uint32_t)place, word, load1(p, word));
   }
-  if (tid == 0) put_rest(A, row, more ? base : -kInf, more ? rest : 0.f);
+  if (tid == 0) put_rest(A, row, more && some ? base : -kInf, more && some ? rest : 0.f);
   return true;
 }
 
 // Parts of a row that is too long for one workgroup's registers. A part
-// holds every `parts`-th piece of TPB vectors of the row, so that words that
-// lie together (frequent ones often do) spread over all parts, and hands on its
+// holds every `parts`-th piece of 1 KB of the row, so that words that lie
+// together (frequent ones often do) spread over all parts, and hands on its
 // words at or above a bound that about `want` of them reach: enough for
 // its share of the k first. The words of the k first that it might hold back are
 // below its bound, which the merge checks against the k-th.
@@ -668,6 +680,7 @@ struct PartHead {
   float bound, sum;    // the words below: sum * 2^(bound a)
   uint32_t key, count; // the bound's order key; candidates, kFullPart: too many, or NaN
 };
+constexpr int kPiece = 64;  // vectors
 constexpr uint32_t kFullPart = 0xFFFFFFFFu;
 struct TopParts {
   PartHead* heads;  // rows x parts
@@ -685,13 +698,17 @@ struct TopParts {
 //      the bound; a vector with a word at or above it goes to its wave's part of
 //      LDS instead, whose words the wave then sorts into candidates and others.
 //   3. top_finish, or a part's list.
-// More vectors or candidates than LDS holds, a bound at the end of the range
-// or a NaN (in the sum) send the row to top_radix.
+// Where more vectors or words reach the bound than LDS holds, they do so by ties
+// (constant rows; rows with few words left unmasked; coarse values): the words above
+// the least value at the bound are the candidates then, and the lowest words at
+// that value fill up. A bound at the end of the range or a NaN (in the sum), or too
+// many words above the ties, send the row to top_radix.
 template <typename T, int TPB, int NV, int SUB, bool PART>
-__global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, TopParts P) {
+__global__ __launch_bounds__(TPB, TPB != 256 ? 1 : SUB == 1 && NV < 16 ? 8 - NV / 8 : 5) void k_top_row(TopArgs A, TopParts P) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
   constexpr int kKMax = PART ? 1 : TPB * SUB / 4;                 // words to select
-  constexpr int kCap = PART ? 1 : kKMax * 8 + 32;                // candidates
+  // (sorted rows bring whole vectors, an eighth more of them than words to select)
+  constexpr int kCap = PART ? 1 : (kKMax + kKMax / 8 + 2) * 8;   // candidates
   constexpr int kVecs = TPB == 1024 ? 160 : PART && SUB > 1 ? 320 : 128;  // vectors of a wave
   constexpr int kGroups = TPB * SUB;
   struct Vecs {
@@ -707,17 +724,21 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
   __shared__ Shared S;
   __shared__ __align__(16) uint64_t cand[kCap + 8];
   __shared__ float red[NW];
-  __shared__ uint32_t wave_count[NW];
+  __shared__ uint32_t wave_count[NW], scan[NW];
   __shared__ uint32_t full, bound_key;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x;
   const int part = PART ? (int)blockIdx.y : 0, parts = PART ? P.parts : 1;
   const T* type = nullptr;
   const Span<T> s(static_cast<const T*>(A.z) + row * A.ld, A.V);
-  const int v0 = part * TPB, step = parts * TPB;
+  // vector t of slot i, ascending in (i, t): i * step + t, in a part the t / 64-th
+  // of each `parts` pieces
+  const int step = parts * TPB;
+  const int v0 = PART ? (__builtin_amdgcn_readfirstlane(wave) * parts + part) * kPiece : 0;
   const int k = PART ? P.want : A.k;
   uint4 r[NV];
-  load_slots<T, TPB, NV, true>(r, s, v0, step);
+  const int own = PART ? lane : tid;
+  load_slots<T, TPB, NV, true>(r, s, v0, step, own, PART ? kPiece : TPB);
   const int xi = s.extra(tid < s.extras ? tid : 0);
   const bool has_ex = part == 0 && tid < s.extras;
   const float ex = has_ex ? (float)s.p[xi] : -kInf;
@@ -768,13 +789,14 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     if (lane == 0) bound_key = lo;
   }
   __syncthreads();
-  const uint32_t at_bound = bound_key;
-  const float bound = key_value(at_bound);
+  uint32_t at_bound = bound_key;
+  float bound = key_value(at_bound);
+  bool ties = false;  // the candidates are the words above the bound
   // 2. candidates, and the sum of the others
   const Product ref(bound, A.a);
   float sum = 0.f;
   int held = 0;  // vectors in this wave's part
-  const int tid2 = renew(tid);
+  const int tid2 = renew(own);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int v = v0 + i * step + tid2;
@@ -800,16 +822,16 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     asm volatile("" : "+v"(sum));  // (here, not after the last vector from kept registers)
   }
   sum *= ref.rest();
-  if (held > kVecs || !Product::fits(bound, A.a)) {
+  if (held > kVecs) {
     held = 0;
     if (lane == 0) full = 1u;
   }
-  // The wave's words at or above the bound are candidates: `each` gets them with
+  // The wave's words that reach the bound are candidates: `each` gets them with
   // a number that counts them in a fixed order.
   const auto wave_words = [&](auto each) {
     int seen = 0;
     const auto one = [&](bool valid, float x, int32_t word) {
-      const bool take = valid && x >= bound;
+      const bool take = valid && (ties ? x > bound : x >= bound);
       const uint64_t who = __ballot(take);
       each(valid, take, x, word,
            seen + (int)__builtin_amdgcn_mbcnt_hi(
@@ -826,48 +848,167 @@ __global__ __launch_bounds__(TPB, TPB == 256 ? 5 : 1) void k_top_row(TopArgs A, 
     if (wave == 0) one(has_ex, ex, xi);
     return seen;
   };
-  const int found = wave_words([&](bool valid, bool take, float x, int32_t, int) {
-    if (valid && !take) sum += exp2_((x - ref.m) * A.a);
-  });
-  sum = wave_sum(sum);
-  if (lane == 0) {
-    red[wave] = sum;
-    wave_count[wave] = (uint32_t)found;
-  }
-  __syncthreads();
-  int C = 0, mine = 0;
+  int C, mine;
+  // candidates and sum of the workgroup, from each wave's
+  const auto add_up = [&](int found) {
+    sum = wave_sum(sum);
+    if (lane == 0) {
+      red[wave] = sum;
+      wave_count[wave] = (uint32_t)found;
+    }
+    __syncthreads();
+    C = mine = 0;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    mine += w < wave ? (int)wave_count[w] : 0;
-    C += (int)wave_count[w];
+    for (int w = 0; w < NW; ++w) {
+      mine += w < wave ? (int)wave_count[w] : 0;
+      C += (int)wave_count[w];
+    }
+    sum = wave_sum(lane < NW ? red[lane] : 0.f);
+  };
+  add_up(wave_words([&](bool valid, bool take, float x, int32_t, int) {
+    if (valid && !take) sum += exp2_((x - ref.m) * A.a);
+  }));
+  // (the same for the whole workgroup, as all that is decided from here on)
+  const bool odd = sum != sum || !(Product::fits(bound, A.a));
+  const int room = PART ? P.room - A.k : kCap;
+  bool many = full != 0u || C > room;
+  int wanted = 0;  // of the words at the bound, with ties
+  if (many && !odd) {
+    // the least value that reaches the bound, and how many words do
+    // (read again: registers held for this rare case would spill in all others)
+    load_slots<T, TPB, NV, false>(r, s, v0, step, own, PART ? kPiece : TPB);
+    float least = kInf;
+    int reach = 0;
+    const int tid3 = renew(own);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float x[N];
+      renew(r[i]);
+      unpack(r[i], x, type);
+      const bool in = v0 + i * step + tid3 < s.nvec;
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const bool at = in && x[n] >= bound;
+        least = at ? fminf(least, x[n]) : least;
+        reach += at ? 1 : 0;
+      }
+    }
+    if (has_ex && ex >= bound) {
+      least = fminf(least, ex);
+      ++reach;
+    }
+    least = -wave_max(-least);
+    for (int d = 32; d > 0; d >>= 1) reach += __shfl_xor(reach, d);
+    __syncthreads();
+    if (lane == 0) {
+      red[wave] = least;
+      wave_count[wave] = (uint32_t)reach;
+    }
+    if (tid == 0) full = 0u;
+    __syncthreads();
+    bound = kInf;
+    reach = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      bound = fminf(bound, red[w]);
+      reach += (int)wave_count[w];
+    }
+    at_bound = order_key(bound);
+    ties = true;
+    // the words above it, and the sum of those below
+    sum = 0.f;
+    held = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = v0 + i * step + tid3;
+      float x[N];
+      renew(r[i]);
+      unpack(r[i], x, type);
+      const bool above = max_of(-kInf, x) > bound;
+      const uint64_t who = __ballot(above);
+      if (above) {
+        const int at = held + (int)__builtin_amdgcn_mbcnt_hi(
+                                  (uint32_t)(who >> 32),
+                                  __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+        if (at < kVecs) {
+          S.v.x[wave][at] = r[i];
+          S.v.word[wave][at] = s.head + v * N;
+        }
+      }
+      held += (int)__popcll(who);
+      float e = 0.f;
+#pragma unroll
+      for (int n = 0; n < N; ++n) e += x[n] < bound ? exp2_((x[n] - bound) * A.a) : 0.f;
+      sum += above ? 0.f : e;
+      asm volatile("" : "+v"(sum));
+    }
+    if (held > kVecs) {
+      held = 0;
+      if (lane == 0) full = 1u;
+    }
+    __syncthreads();  // (red and wave_count are read above)
+    add_up(wave_words([&](bool valid, bool, float x, int32_t, int) {
+      if (valid && x < bound) sum += exp2_((x - bound) * A.a);
+    }));
+    many = full != 0u || C > room;
+    // A row needs as many words at the bound as are missing of its k, a part
+    // never more than k.
+    const int at_it = reach - C, most = PART ? A.k : C < A.k ? A.k - C : 0;
+    wanted = at_it < most ? at_it : most;
+    if (bound != -kInf) sum += (float)(at_it - wanted);
   }
-  sum = wave_sum(lane < NW ? red[lane] : 0.f);
-  const bool odd = full != 0u || sum != sum;  // (the same for the whole workgroup)
+  // the lowest `wanted` words at the bound: `put` gets each with its number
+  const auto fill = [&](auto put) {
+    int done = 0;
+    const auto round = [&](bool valid, int32_t word) {
+      const bool tie = valid && load1(s.p, word) == bound;
+      uint32_t total;
+      const int at = done + (int)block_scan<TPB>(tie, scan, &total);
+      if (tie && at < wanted) put(at, word);
+      done += (int)total;
+    };
+    if (part == 0 && wanted > 0) round(tid < s.head, tid);
+    for (int i = 0; i < NV && done < wanted; ++i)
+      for (int e = tid; e < TPB * N + tid && done < wanted; e += TPB) {
+        const int t = e / N;
+        const int v = i * step + (PART ? (t / kPiece * parts + part) * kPiece + t % kPiece : t);
+        round(v < s.nvec, s.head + v * N + e % N);
+      }
+    if (part == 0 && done < wanted) {
+      const int32_t word = s.head + s.nvec * N + tid;
+      round(word < A.V, word);
+    }
+  };
   if constexpr (PART) {
     const int64_t at = row * parts + part;
-    const bool fits = !odd && C <= P.room;
-    if (fits)
+    const bool fits = !odd && !many;
+    if (fits) {
+      uint64_t* list = P.lists + at * P.room;
       wave_words([&](bool, bool take, float x, int32_t word, int n) {
-        if (take) P.lists[at * P.room + mine + n] = candidate<T>(order_key(x), word);
+        if (take) list[mine + n] = candidate<T>(order_key(x), word);
       });
+      fill([&](int n, int32_t word) { list[C + n] = candidate<T>(at_bound, word); });
+    }
     if (tid == 0) {
       PartHead h;
       h.bound = bound;
       h.sum = sum;
       h.key = at_bound;
-      h.count = fits ? (uint32_t)C : kFullPart;
+      h.count = fits ? (uint32_t)(C + wanted) : kFullPart;
       P.heads[at] = h;
     }
   } else {
     bool done = false;
-    if (!odd && C <= kCap) {
+    if (!odd && !many) {
       wave_words([&](bool, bool take, float x, int32_t word, int n) {
         if (take) cand[mine + n] = candidate<T>(order_key(x), word);
       });
+      fill([&](int n, int32_t word) { cand[C + n] = candidate<T>(at_bound, word); });
+      C += wanted;
       if (tid < 8) cand[C + tid] = 0ull;
       __syncthreads();
-      done = top_finish<T, TPB, kCap, kKMax>(A, row, s.p, cand, C,
-                                               floor_of<T>(at_bound), 0ull, bound, sum, S.finish);
+      done = top_finish<T, TPB, kCap, kKMax>(A, row, s.p, cand, C, floor_of<T>(at_bound), 0ull,
+                                             bound, sum, S.finish);
     }
     __syncthreads();
     if (!done) top_radix<T, TPB>(A, S.radix, s.p, row);
@@ -1736,17 +1877,18 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 // A row's selection: whole in one workgroup up to kPartVecs vectors, else in
 // parts of that many.
 constexpr int kPartVecs = 256 * 16;
-constexpr int kMergeSmall = 2080, kMergeLarge = 9216;
+constexpr int kMergeSmall = 2560, kMergeLarge = 9216;
 
 TopParts top_parts(int64_t V, int64_t k, int32_t dtype) {
   TopParts p{};
-  p.parts = (int32_t)ceil_div(V / (dtype == TKEF_DTYPE_F32 ? 4 : 8), kPartVecs);
+  const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
+  p.parts = vecs <= 512 * 16 && k <= 128 ? 1 : (int32_t)ceil_div(vecs, kPartVecs);
   if (p.parts == 1) return p;
   // a part's share of the k first and four standard deviations of it
   const double share = (double)k / p.parts;
   int64_t want = (int64_t)(share + 4.0 * std::sqrt(share)) + 8;
   p.want = (int32_t)(want < k ? want : k);
-  p.room = 2 * p.want + 64;
+  p.room = (int32_t)((p.want + p.want / 8 + 2) * 8 + k);
   return p;
 }
 
@@ -1773,10 +1915,12 @@ hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
         k_top_row<T, 256, 16, 1, true><<<split, 256, 0, s>>>(a, p);
       else
         k_top_row<T, 256, 16, 4, true><<<split, 256, 0, s>>>(a, p);
-      if (p.parts * p.room <= kMergeSmall)
+      if (p.parts * (2 * p.want + 64) <= kMergeSmall)
         k_top_merge<T, 256, kMergeSmall><<<rows, 256, 0, s>>>(a, p);
       else
         k_top_merge<T, 1024, kMergeLarge><<<rows, 1024, 0, s>>>(a, p);
+    } else if (vecs > kPartVecs) {
+      k_top_row<T, 512, 16, 1, false><<<rows, 512, 0, s>>>(a, p);
     } else if (a.k <= 64) {
       if (vecs <= 256 * 4)
         k_top_row<T, 256, 4, 1, false><<<rows, 256, 0, s>>>(a, p);

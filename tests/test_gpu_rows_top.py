@@ -174,3 +174,27 @@ def test_masks_at_the_lowest_value_of_the_type(v, dtype):
     x[4, v // 2] = 0.0
     for k in (1, 20, 70):
         check(x, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [3000, 32000, 40001, 131071])
+def test_clustered_and_tied_rows(v, dtype):
+    """The k first together in one place, beside ties that reach past what a
+    workgroup keeps, and with fewer ordinary words than k."""
+    rng = np.random.default_rng(v + 4)
+    n = 9
+    x = rng.normal(size=(n, v))
+    x[0, 1000:] = -INF                                  # the first words only
+    x[1, : v - 700] -= 50.0                             # the last words far ahead
+    x[2] = np.round(x[2])                               # few values
+    x[3] = np.round(x[3] * 2)
+    x[4] = 1.0
+    x[4, rng.integers(0, v, 30)] = 2.0                  # 30 above a constant
+    x[5] = 1.0
+    x[5, v // 2: v // 2 + 500] = 3.0                    # a run of ties above a constant
+    x[6] = -INF
+    x[6, rng.permutation(v)[:55]] = rng.normal(size=55)
+    x[7] = np.sort(x[7])[::-1]
+    x[8] = np.repeat(rng.normal(size=(v + 63) // 64), 64)[:v]   # blocks of equal words
+    for k in (1, 55, 64, 128, 200, 256, 700):
+        check(x, k, dtype, pad=k % 3, shift=k % 5)

@@ -33,22 +33,24 @@ __device__ __forceinline__ float rescale(float m, float top, float a) {
 
 // (x - m) a as one operation, fma(x, a, -c) with c = fl(m a): what c's rounding
 // changes is the same factor for all x, 2^(c - m a), and rest() takes it out of
-// their sum. m is held to where the product stays in range; sums whose maximum
-// does not fit (masks at the lowest value of binary32 or bfloat16 and nothing
-// else) are taken again by the difference. One of eight operations a word: 145 ->
+// their sum. m is held to where c's rounding is at most 2^5, so that neither that
+// factor nor the terms leave the range: a sum whose own maximum lies below (masks
+// at -1e10 or the type's lowest value, beside ordinary words) is 0 then, which is
+// right beside them, and one whose row has no other words is taken again by the
+// difference. One of eight operations a word: 145 ->
 // 134 us for the step of 1,021 x 131,071 binary16, whose rows leave one workgroup
 // a compute unit, 219 -> 206 for 8,192 x 32,000 bfloat16.
 struct Product {
   float m, a, c;
   __device__ Product(float max, float a_) : a(a_) {
-    const float limit = fminf(0x1p126f / a, 0x1p126f);
+    const float limit = 0x1p30f / a;
     m = max == -kInf ? 0.f : fmaxf(fminf(max, limit), -limit);
     c = m * a;
   }
   __device__ float exponent(float x) const { return __builtin_fmaf(x, a, -c); }
   __device__ float rest() const { return exp2_(-__builtin_fmaf(m, a, -c)); }
   __device__ static bool fits(float max, float a) {
-    return max == -kInf || __builtin_fabsf(max) < fminf(0x1p126f / a, 0x1p126f);
+    return max == -kInf || __builtin_fabsf(max) < 0x1p30f / a;
   }
 };
 
@@ -688,6 +690,14 @@ struct TopParts {
   int32_t parts, room, want;
 };
 
+// Workgroups of 256 a compute unit for which registers are allotted. Parts of 16
+// vectors: 4 (64 us in five's 96 registers, which hold some in memory, 54 in four's;
+// 509 x 131,071 binary32).
+template <int TPB, int NV, int SUB, bool PART>
+constexpr int top_workgroups() {
+  return TPB != 256 ? 1 : PART ? 4 : SUB == 1 && NV < 16 ? 8 - NV / 8 : 5;
+}
+
 // One workgroup takes a row, or a part of one, into registers, NV vectors a
 // thread.
 //   1. Each thread's maximum over each of its SUB shares. The k-th largest of
@@ -701,10 +711,11 @@ struct TopParts {
 // Where more vectors or words reach the bound than LDS holds, they do so by ties
 // (constant rows; rows with few words left unmasked; coarse values): the words above
 // the least value at the bound are the candidates then, and the lowest words at
-// that value fill up. A bound at the end of the range or a NaN (in the sum), or too
-// many words above the ties, send the row to top_radix.
+// that value fill up; so too where the bound lies beyond what Product takes. A NaN
+// (in the sum), or too many words above the ties, send the row to top_radix.
 template <typename T, int TPB, int NV, int SUB, bool PART>
-__global__ __launch_bounds__(TPB, TPB != 256 ? 1 : SUB == 1 && NV < 16 ? 8 - NV / 8 : 5) void k_top_row(TopArgs A, TopParts P) {
+__global__ __launch_bounds__(TPB, top_workgroups<TPB, NV, SUB, PART>()) void k_top_row(
+    TopArgs A, TopParts P) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
   constexpr int kKMax = PART ? 1 : TPB * SUB / 4;                 // words to select
   // (sorted rows bring whole vectors, an eighth more of them than words to select)
@@ -869,9 +880,9 @@ __global__ __launch_bounds__(TPB, TPB != 256 ? 1 : SUB == 1 && NV < 16 ? 8 - NV 
     if (valid && !take) sum += exp2_((x - ref.m) * A.a);
   }));
   // (the same for the whole workgroup, as all that is decided from here on)
-  const bool odd = sum != sum || !(Product::fits(bound, A.a));
+  bool odd = sum != sum;
   const int room = PART ? P.room - A.k : kCap;
-  bool many = full != 0u || C > room;
+  bool many = full != 0u || C > room || !Product::fits(bound, A.a);
   int wanted = 0;  // of the words at the bound, with ties
   if (many && !odd) {
     // the least value that reaches the bound, and how many words do
@@ -938,7 +949,7 @@ __global__ __launch_bounds__(TPB, TPB != 256 ? 1 : SUB == 1 && NV < 16 ? 8 - NV 
       held += (int)__popcll(who);
       float e = 0.f;
 #pragma unroll
-      for (int n = 0; n < N; ++n) e += x[n] < bound ? exp2_((x[n] - bound) * A.a) : 0.f;
+      for (int n = 0; n < N; ++n) e += x[n] >= bound ? 0.f : exp2_((x[n] - bound) * A.a);
       sum += above ? 0.f : e;
       asm volatile("" : "+v"(sum));
     }
@@ -948,8 +959,9 @@ __global__ __launch_bounds__(TPB, TPB != 256 ? 1 : SUB == 1 && NV < 16 ? 8 - NV 
     }
     __syncthreads();  // (red and wave_count are read above)
     add_up(wave_words([&](bool valid, bool, float x, int32_t, int) {
-      if (valid && x < bound) sum += exp2_((x - bound) * A.a);
+      if (valid && !(x >= bound)) sum += exp2_((x - bound) * A.a);
     }));
+    odd = sum != sum;  // (a NaN among vectors that were too many to look into before)
     many = full != 0u || C > room;
     // A row needs as many words at the bound as are missing of its k, a part
     // never more than k.
@@ -1048,12 +1060,23 @@ __global__ __launch_bounds__(TPB) void k_top_merge(TopArgs A, TopParts P) {
     const uint64_t least = ~wave_max64(lane < P.parts ? ~floor_of<T>(h.key) : 0ull);
     __syncthreads();
     if (C <= CAP) {
-      const int64_t lists = row * P.parts * P.room;
-      for (int i = tid; i < P.parts * P.room; i += TPB) {
-        const int part = i / P.room, n = i - part * P.room;
-        const uint32_t at = from[part];
-        const uint32_t end = part + 1 < P.parts ? from[part + 1] : (uint32_t)C;
-        if (at + (uint32_t)n < end) cand[at + n] = P.lists[lists + i];
+      // Candidate i is in the last part that starts at or before it (one load a
+      // candidate, four under way: 17 us against 21 over the lists' whole room)
+      const uint64_t* lists = P.lists + row * P.parts * P.room;
+      for (int i0 = tid; i0 < C; i0 += 4 * TPB) {
+        uint64_t c[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t i = (uint32_t)(i0 + u * TPB);
+          int part = 0;
+#pragma unroll
+          for (int d = 32; d > 0; d >>= 1)
+            part += part + d < P.parts && from[part + d] <= i ? d : 0;
+          if (i < (uint32_t)C) c[u] = lists[part * P.room + (int)(i - from[part])];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (i0 + u * TPB < C) cand[i0 + u * TPB] = c[u];
       }
       if (tid < 8) cand[C + tid] = 0ull;
       __syncthreads();

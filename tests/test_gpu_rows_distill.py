@@ -325,3 +325,31 @@ def test_masks_at_the_lowest_value_of_the_type(v, dtype):
     teacher[4, v - 1] = 2.0
     for use_tail in (True, False):
         check(rng, n, v, k, dtype, student=student, teacher=teacher, use_tail=use_tail)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", [-1e9, -1e10, -1e30, -2e38])
+@pytest.mark.parametrize("v", [300, 32000, 70000, 140001])
+def test_masks_of_great_size(v, mask, dtype):
+    """Whole threads' and whole rows' words at a large value that is not the
+    type's lowest, where a product with the exponent's factor is rounded by more
+    than an exponent holds."""
+    rng = np.random.default_rng(v + 6)
+    n, k = 6, 12
+    teacher = logits(rng, n, v)
+    student = teacher + rng.normal(size=(n, v)) * 0.5
+    best = [np.argsort(-teacher[r])[:k] for r in range(n)]
+    student[0] = mask                                  # nothing but the mask
+    student[1, v // 3:] = mask
+    teacher[1, v // 3:] = -60.0
+    student[2] = mask
+    student[2, best[2]] = teacher[2, best[2]]          # only listed words left
+    student[3] = -mask                                 # as far above zero
+    student[4] = mask
+    student[4, v - 1] = 1.0                            # one word left, at the end
+    teacher[4] = -60.0
+    teacher[4, v - 1] = 2.0
+    student[5] = mask
+    student[5, v // 2: v // 2 + 40] = 0.0
+    for temperature in (1.0, 0.8, 1.3):
+        check(rng, n, v, k, dtype, temperature=temperature, student=student, teacher=teacher)

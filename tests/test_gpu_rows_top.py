@@ -198,3 +198,53 @@ def test_clustered_and_tied_rows(v, dtype):
     x[8] = np.repeat(rng.normal(size=(v + 63) // 64), 64)[:v]   # blocks of equal words
     for k in (1, 55, 64, 128, 200, 256, 700):
         check(x, k, dtype, pad=k % 3, shift=k % 5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", [-1e9, -1e10, -1e30, -2e38])
+@pytest.mark.parametrize("v", [300, 32000, 131071])
+def test_masks_of_great_size(v, mask, dtype):
+    """Threads, and bounds, whose words are all at a large value that is not
+    the type's lowest."""
+    rng = np.random.default_rng(v + 6)
+    x = logits(rng, 5, v)
+    x[0] = mask
+    x[1, v // 4:] = mask
+    x[2] = mask
+    x[2, ::1000] = 1.0
+    x[3] = -mask
+    x[4] = mask
+    x[4, v // 2: v // 2 + 40] = 0.0
+    for k in (1, 20, 70):
+        check(x, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("v", [300, 32000, 40001, 131071])
+def test_nan_among_ties(v, dtype):
+    """One NaN in a row of equal words, or of a few values: beyond the infinity of its
+    sign, reported, and no tail."""
+    announce(f"nan among ties {v} {dtype}")
+    rng = np.random.default_rng(v + 8)
+    x = np.ones((6, v))
+    x[1] = np.round(rng.normal(size=v))
+    x[2] = -INF
+    x[3] = -3e4
+    x[4] = 2.0
+    x[4, ::2] = 1.0
+    at = [0, v - 1, v // 2, 17, v // 3, 40]
+    for r in range(6):
+        x[r, at[r]] = math.nan
+    z, exact = device_rows(x, dtype)
+    for k in (1, 64, 200):
+        plan = tk.TopLogitsPlan(6, v, k, dtype=TYPES[dtype])
+        status = torch.zeros(1, dtype=torch.int32, device=need_gpu())
+        idx, value, tail = plan.execute(z, status=status)
+        assert int(status.item()) == tk.STATUS_NAN
+        got = idx.cpu().numpy()
+        for r in range(6):
+            # (a conversion to bfloat16 makes negative NaNs, which come last)
+            order = np.nan_to_num(exact[r], nan=np.copysign(INF, exact[r][at[r]]), neginf=-1e300)
+            want = np.sort(np.argsort(-order, kind="stable")[:k])
+            assert np.array_equal(got[r], want), (r, k)
+            assert math.isnan(float(tail[r])) or k == v

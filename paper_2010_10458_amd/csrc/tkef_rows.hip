@@ -714,7 +714,7 @@ constexpr int top_workgroups() {
 // that value fill up; so too where the bound lies beyond what Product takes. A NaN
 // (in the sum), or too many words above the ties, send the row to top_radix.
 template <typename T, int TPB, int NV, int SUB, bool PART>
-__global__ __launch_bounds__(TPB, top_workgroups<TPB, NV, SUB, PART>()) void k_top_row(
+__global__ __launch_bounds__(TPB, (top_workgroups<TPB, NV, SUB, PART>())) void k_top_row(
     TopArgs A, TopParts P) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
   constexpr int kKMax = PART ? 1 : TPB * SUB / 4;                 // words to select

@@ -73,7 +73,7 @@ hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s);
 struct VerifyLayout {
   size_t best, rejected, raced, arrived, zeroed, sums, parts, bytes;
 };
-// Whether the grid over places and units of 64 KB stays within a launch's limits.
+// Whether the grid over places and units of 32 KB stays within a launch's limits.
 bool verify_fits(int64_t batch, int64_t draft, int64_t V, int32_t dtype);
 VerifyLayout verify_layout(int64_t batch, int64_t draft, int64_t V, int32_t dtype);
 

@@ -1618,6 +1618,7 @@ __device__ __forceinline__ float prob(float x, float a, LogSum v) {
   return v.m == -kInf && v.S == 0.f ? 0.f : exp2_((x - v.m) * a) / v.S;
 }
 
+// (m, S) of a wave's words. Where m is beyond what Product takes, S may be anything.
 template <typename T, int NV>
 __device__ __forceinline__ LogSum regs_sum(const uint4 (&r)[NV], float ex, float a) {
   constexpr int N = Span<T>::N;
@@ -1626,8 +1627,8 @@ __device__ __forceinline__ LogSum regs_sum(const uint4 (&r)[NV], float ex, float
   v.m = ex;
 #pragma unroll
   for (int i = 0; i < NV; ++i) v.m = max_packed(v.m, r[i], type);
-  const float ref = v.m == -kInf ? 0.f : v.m;
-  v.S = exp2_((ex - ref) * a);
+  const Product ref(v.m, a);
+  v.S = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float x[N];
@@ -1636,13 +1637,31 @@ __device__ __forceinline__ LogSum regs_sum(const uint4 (&r)[NV], float ex, float
     unpack(w, x, type);
     float e = 0.f;
 #pragma unroll
-    for (int n = 0; n < N; ++n) e += exp2_((x[n] - ref) * a);
+    for (int n = 0; n < N; ++n) e += exp2_(ref.exponent(x[n]));
     v.S += e;
   }
+  v.S = v.S * ref.rest() + exp2_((ex - ref.m) * a);
   const float m = wave_max(v.m);
   v.S = wave_sum(join_sum(v.m, v.S, m, a));
   v.m = m;
   return v;
+}
+
+// S of vectors [v0, v0 + n) of a row and, where `edges`, its extras, from their
+// maximum m by differences, by one wave.
+template <typename T>
+__device__ __forceinline__ float far_sum(const Span<T>& s, int v0, int n, bool edges, float m,
+                                         float a) {
+  const T* type = nullptr;
+  const int lane = threadIdx.x & 63, end = v0 + n < s.nvec ? v0 + n : s.nvec;
+  float sum = edges && lane < s.extras ? exp2_(((float)s.p[s.extra(lane)] - m) * a) : 0.f;
+  for (int v = v0 + lane; v < end; v += 64) {
+    float x[Span<T>::N];
+    unpack(load16<false>(s.vec(v)), x, type);
+#pragma unroll
+    for (int i = 0; i < Span<T>::N; ++i) sum += exp2_((x[i] - m) * a);
+  }
+  return wave_sum(sum);
 }
 
 // Sums of the rows at one place of a sequence, or of one chunk of them:
@@ -1684,9 +1703,19 @@ __global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch
   // the first wave alone from here on
   float4 s = red[lane < NW ? lane : 0];
   if (lane >= NW) s.y = s.w = 0.f;
+  float m0 = wave_max(s.x), m1 = wave_max(s.z);
+  if (!Product::fits(m0, A.a)) {
+    const float S = far_sum(ts, v0, TPB * NV, chunk == 0u, m0, A.a);
+    s.x = m0;
+    s.y = lane == 0 ? S : 0.f;
+  }
+  if (drafted && !Product::fits(m1, A.a)) {
+    const float S = far_sum(ds, v0, TPB * NV, chunk == 0u, m1, A.a);
+    s.z = m1;
+    s.w = lane == 0 ? S : 0.f;
+  }
   const int64_t at = b * (A.draft + 1) + place;
   if (chunks > 1) {
-    float m0 = wave_max(s.x), m1 = wave_max(s.z);
     const float s0 = wave_sum(join_sum(s.x, s.y, m0, A.a));
     const float s1 = wave_sum(join_sum(s.z, s.w, m1, A.a));
     float2* mine = W.parts + 2 * (at * chunks + chunk);
@@ -2045,23 +2074,28 @@ hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
   });
 }
 
-// Places are summed in units of 1,024 threads x 4 vectors of each row, or of 256
-// x 4 where those would leave compute units idle.
+// Places are summed in units of 512 threads x 4 vectors of each row (256 x 8 x 65,536
+// binary16 with its race: 89 us; 1,024 x 4 93, 256 x 4 95, 1,024 x 8 96), three of them
+// a compute unit for their dynamic LDS: what starts before a rejection is posted
+// is read in vain (37 x 7 x 131,071 binary32: 49 us, 51 with four). Where those would
+// leave compute units idle, in units of 256 x 4 (64 x 5 x 32,000 bfloat16: 22 us
+// against 26) or 256 x 1 (one sequence: 15.8 against 16.8), which look for no rejection.
 namespace {
-constexpr int kUnitVecs = 1024 * 4, kSmallVecs = 256 * 4;
-constexpr int64_t kFewUnits = 512;
+constexpr int kUnitVecs = 512 * 4, kSmallVecs = 256 * 4;
+constexpr int64_t kFewUnits = 1024, kTinyUnits = 64;
+constexpr unsigned kUnitSpare = 50 << 10;
 }  // namespace
 
 bool verify_fits(int64_t batch, int64_t draft, int64_t V, int32_t dtype) {
   const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
-  return batch * (draft + 1) * ceil_div(vecs, kUnitVecs) <= (int64_t)1 << 21;
+  return batch * (draft + 1) * ceil_div(vecs, kUnitVecs) <= (int64_t)1 << 22;
 }
 
 VerifyLayout verify_layout(int64_t batch, int64_t draft, int64_t V, int32_t dtype) {
   const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
   const int64_t places = batch * (draft + 1), big = ceil_div(vecs, kUnitVecs);
   // small units serve batches with fewer than kFewUnits big ones
-  const int64_t small = (places * big < kFewUnits ? places * big : kFewUnits) * 16;
+  const int64_t small = (places * big < kFewUnits ? places * big : kFewUnits) * 8;
   const int64_t parts = places * big > small ? places * big : small;
   VerifyLayout l;
   l.best = 0;
@@ -2081,9 +2115,9 @@ hipError_t launch_verify(const VerifyArgs& a, const VerifyScratch& w, hipStream_
     const int64_t vecs = a.V / Span<T>::N, places = (int64_t)a.batch * (a.draft + 1);
     const int64_t big = ceil_div(vecs, kUnitVecs);
     if (places * big > kFewUnits) {
-      k_verify_sums<T, 1024, 4, true>
-          <<<dim3((unsigned)(places * big)), 1024, 0, s>>>(a, w, (int)big);
-    } else if (places * big > 32) {
+      k_verify_sums<T, 512, 4, true>
+          <<<dim3((unsigned)(places * big)), 512, kUnitSpare, s>>>(a, w, (int)big);
+    } else if (places * big > kTinyUnits) {
       const int64_t small = ceil_div(vecs, kSmallVecs);
       k_verify_sums<T, 256, 4, false>
           <<<dim3((unsigned)(places * small)), 256, 0, s>>>(a, w, (int)small);

@@ -60,7 +60,7 @@ class _RowPlan:
     def __del__(self):
         if getattr(self, "_h", None) and self._h.value:
             self._free(self._h)
-            self._h = ctypes.c_void_p()
+            self._h.value = None
 
     def _info(self, name: str) -> None:
         ws = ctypes.c_size_t()

@@ -203,3 +203,34 @@ def test_masks_at_the_lowest_value_of_the_type(v, dtype):
     target[3, :, 7] = 0.0                    # one word left
     drafts[4] = low                          # a uniform draft
     check(rng, b, draft, v, dtype, target=target, drafts=drafts, tokens=tokens, uniform=uniform)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("b,draft,v", [(600, 2, 1030), (40, 7, 70001), (530, 1, 9001)])
+def test_many_places(b, draft, v, dtype):
+    """Enough rows to leave those after a rejection unread."""
+    rng = np.random.default_rng(b + v)
+    check(rng, b, draft, v, dtype, temperature=0.9)
+    check(rng, b, draft, v, dtype, ragged=True, pad=3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", [-1e9, -1e10, -1e30, -2e38])
+@pytest.mark.parametrize("b,v", [(5, 300), (5, 32000), (350, 8191), (20, 140001)])
+def test_masks_of_great_size(b, v, mask, dtype):
+    rng = np.random.default_rng(v + 7)
+    draft = 2
+    target = logits(rng, b * (draft + 1), v).reshape(b, draft + 1, v)
+    drafts = target[:, :draft] + rng.normal(size=(b, draft, v)) * 0.5
+    tokens = rng.integers(0, v, (b, draft))
+    uniform = np.full((b, draft), 0.25)
+    target[0] = mask                         # uniform
+    target[1, :, v // 8:] = mask             # most words masked in the target
+    tokens[1, 0] = v - 1                     # such a word drafted
+    drafts[2, :, : v // 2] = mask
+    target[3] = mask
+    target[3, :, 7] = 0.0                    # one word left
+    drafts[4] = -mask                        # a uniform draft, as far above zero
+    for temperature in (1.0, 0.8):
+        check(rng, b, draft, v, dtype, temperature=temperature, target=target, drafts=drafts,
+              tokens=tokens, uniform=uniform)

@@ -517,25 +517,24 @@ __device__ __forceinline__ uint64_t floor_of(uint32_t key) {
   return (uint64_t)(key >> key_shift(type)) << kWordBits;
 }
 
-// Ranks by counting up to this many candidates, by bisection above: counting costs
-// a comparison for each pair, bisection some twelve rounds with a barrier each.
-template <int TPB>
-constexpr int rank_limit() {
-  return TPB < 1024 ? 128 : 256;
-}
+// Ranks by counting up to this many candidates (one a thread), by bisection above:
+// counting costs a comparison for each pair, bisection some twelve rounds with a
+// barrier each. 8,192 x 32,000 bfloat16: k = 128 (some 150 candidates) 132 us counted, 147
+// bisected; k = 256 (some 290) 204 and 180.
+constexpr int kRankLimit = 256;
 
 template <int TPB, int KMAX>
 struct FinishLds {
   int32_t chosen[KMAX + 16];  // (and fillers up to a multiple of 16)
   uint64_t thr, top[TPB / 64];
-  float others[rank_limit<TPB>()];
+  float others[kRankLimit];
   uint32_t count[2][TPB / 64];
   float red[TPB / 64];
   uint32_t ntaken;
 };
 
 // The k first of C candidates (LDS, all >= least, then eight zeros), their places in ascending order of words,
-// and the rest: S * 2^(m a) and the candidates not taken. Up to rank_limit
+// and the rest: S * 2^(m a) and the candidates not taken. Up to kRankLimit
 // candidates a thread counts the better ones of its own; beyond that the k-th
 // candidate is bisected, a candidate's word being part of it, so that ties end
 // at the lower words. A selected word's place is the number of selected lower
@@ -552,7 +551,7 @@ __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const 
   if (C < k) return false;
   const bool more = k < A.V;
   uint64_t c[CPT];
-  const bool counted = C <= rank_limit<TPB>();
+  const bool counted = C <= kRankLimit;
   uint64_t thr;
   float left = 0.f;
   if (tid < 16) L.chosen[k + tid] = INT32_MAX;
@@ -720,7 +719,7 @@ __global__ __launch_bounds__(TPB, (top_workgroups<TPB, NV, SUB, PART>())) void k
   constexpr int kKMax = PART ? 1 : TPB * SUB / 4;                 // words to select
   // (sorted rows bring whole vectors, an eighth more of them than words to select)
   constexpr int kCap = PART ? 1 : (kKMax + kKMax / 8 + 2) * 8;   // candidates
-  constexpr int kVecs = TPB == 1024 ? 160 : PART && SUB > 1 ? 320 : 128;  // vectors of a wave
+  constexpr int kVecs = PART && SUB > 1 ? 320 : 128;  // vectors of a wave
   constexpr int kGroups = TPB * SUB;
   struct Vecs {
     uint4 x[NW][kVecs];
@@ -1926,16 +1925,27 @@ namespace {
 int64_t ceil_div(int64_t a, int64_t b) { return a <= 0 ? 1 : (a + b - 1) / b; }
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// A row's selection: whole in one workgroup up to kPartVecs vectors, else in
-// parts of that many.
-constexpr int kPartVecs = 256 * 16;
+// A row's selection: whole in one workgroup of 256 threads while they hold it (64 KB)
+// and k is at most 256, else in parts of that size. Two exceptions:
+//   k <= 128: whole up to 128 KB, in 512 threads (2,048 x 32,000 binary32, k = 64: 59 us
+//   against 66 in two parts; 2,048 x 64,000 bfloat16, k = 128: 89 and 80; 16 rows of
+//   64,000: 13 and 19);
+//   k > 256: rows up to 64 KB in parts of 16 KB, whose lists are some hundred words each
+//   and a thread's or two's (8,192 x 32,000 bfloat16, k = 300: 324 us, whole in 1,024 threads 1,030;
+//   k = 512: 402, 1,139; k = 1,000: 1,322, 1,573).
+constexpr int kPartVecs = 256 * 16, kSmallPartVecs = 256 * 4;
+// candidates that a merge in 256 and in 1,024 threads has LDS for: 21 KB, which leaves
+// room for other rows beside it, and 74 KB
 constexpr int kMergeSmall = 2560, kMergeLarge = 9216;
 
 TopParts top_parts(int64_t V, int64_t k, int32_t dtype) {
   TopParts p{};
   const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
-  p.parts = vecs <= 512 * 16 && k <= 128 ? 1 : (int32_t)ceil_div(vecs, kPartVecs);
-  if (p.parts == 1) return p;
+  const bool small = k > 256 && vecs <= kPartVecs;
+  p.parts = vecs <= 512 * 16 && k <= 128
+                ? 1
+                : (int32_t)ceil_div(vecs, small ? kSmallPartVecs : kPartVecs);
+  if (p.parts == 1 && k <= 256) return p;
   // a part's share of the k first and four standard deviations of it
   const double share = (double)k / p.parts;
   int64_t want = (int64_t)(share + 4.0 * std::sqrt(share)) + 8;
@@ -1948,7 +1958,7 @@ TopParts top_parts(int64_t V, int64_t k, int32_t dtype) {
 
 size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype) {
   const TopParts p = top_parts(V, k, dtype);
-  if (p.parts == 1) return 0;
+  if (p.room == 0) return 0;
   return up256((size_t)rows * (size_t)p.parts * sizeof(PartHead)) +
          (size_t)rows * (size_t)p.parts * (size_t)p.room * 8;
 }
@@ -1959,14 +1969,17 @@ hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;
     const int vecs = a.V / Span<T>::N;
-    if (p.parts > 1) {
+    if (p.room != 0) {
       p.heads = static_cast<PartHead*>(ws);
       p.lists = reinterpret_cast<uint64_t*>(
           static_cast<char*>(ws) + up256((size_t)a.rows * (size_t)p.parts * sizeof(PartHead)));
-      if (p.want <= 64)
+      if (a.k > 256 && vecs <= kPartVecs)
+        k_top_row<T, 256, 4, 4, true><<<split, 256, 0, s>>>(a, p);
+      else if (p.want <= 64)
         k_top_row<T, 256, 16, 1, true><<<split, 256, 0, s>>>(a, p);
       else
         k_top_row<T, 256, 16, 4, true><<<split, 256, 0, s>>>(a, p);
+      // (twice what the parts want; lists that are longer by ties go by top_radix)
       if (p.parts * (2 * p.want + 64) <= kMergeSmall)
         k_top_merge<T, 256, kMergeSmall><<<rows, 256, 0, s>>>(a, p);
       else
@@ -1974,21 +1987,22 @@ hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
     } else if (vecs > kPartVecs) {
       k_top_row<T, 512, 16, 1, false><<<rows, 512, 0, s>>>(a, p);
     } else if (a.k <= 64) {
+      // Shares of whole threads, 256 of them: 8,192 x 8,000 bfloat16, k = 64, 52 us, 79
+      // with four shares a thread; k = 16 of 32,000 91 and 95. Four shares for k <= 256. The
+      // fewest vectors a thread that hold the row: more registers, fewer workgroups.
       if (vecs <= 256 * 4)
         k_top_row<T, 256, 4, 1, false><<<rows, 256, 0, s>>>(a, p);
       else if (vecs <= 256 * 8)
         k_top_row<T, 256, 8, 1, false><<<rows, 256, 0, s>>>(a, p);
       else
         k_top_row<T, 256, 16, 1, false><<<rows, 256, 0, s>>>(a, p);
-    } else if (a.k <= 256) {
+    } else {
       if (vecs <= 256 * 4)
         k_top_row<T, 256, 4, 4, false><<<rows, 256, 0, s>>>(a, p);
       else if (vecs <= 256 * 8)
         k_top_row<T, 256, 8, 4, false><<<rows, 256, 0, s>>>(a, p);
       else
         k_top_row<T, 256, 16, 4, false><<<rows, 256, 0, s>>>(a, p);
-    } else {
-      k_top_row<T, 1024, 4, 4, false><<<rows, 1024, 0, s>>>(a, p);
     }
   });
 }

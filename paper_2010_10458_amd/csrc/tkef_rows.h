@@ -61,10 +61,10 @@ struct VerifyArgs {
 size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype);
 hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s);
 // A row that is too long for one workgroup is taken in this many chunks (1:
-// whole) for its loss, and for its loss and gradient; ws then holds kPartBytes
-// for each.
+// whole) for its loss, and for its loss and gradient (then never more);
+// ws then holds kPartBytes for each.
 constexpr size_t kPartBytes = 32;
-int distill_chunks(int64_t V, int32_t dtype, bool gradient);
+int distill_chunks(int64_t V, int32_t dtype, int64_t rows, bool gradient);
 hipError_t launch_distill_forward(const DistillArgs& a, void* ws, hipStream_t s);
 hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s);
 hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s);

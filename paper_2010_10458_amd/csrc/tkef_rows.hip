@@ -1919,6 +1919,11 @@ constexpr int kChunkVecs = 256 * 8;
 // whole rows leave few workgroups a compute unit, chunks of it read faster
 // (128,000 bfloat16 words: 3.6 -> 5.5 TB/s; 64,000 binary32: 4.2 -> 5.6).
 constexpr int kLossVecs = 256 * 16;
+// The step holds a row from its loss to its gradient, in chunks it reads it twice (2,048 x
+// 64,000 bfloat16: 107 us whole, 146; 1,021 x 131,064: 134, 147). In chunks all the same
+// where a row beyond 128 KB would take a compute unit to itself and leave most
+// without one (128,000 bfloat16: 64 rows 23 us whole, 14; 96 rows 23, 18; 128 rows 23, 23).
+constexpr int64_t kFewRows = 96;
 
 namespace {
 
@@ -2007,9 +2012,10 @@ hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
   });
 }
 
-int distill_chunks(int64_t V, int32_t dtype, bool gradient) {
+int distill_chunks(int64_t V, int32_t dtype, int64_t rows, bool gradient) {
   const int64_t vecs = V / (dtype == TKEF_DTYPE_F32 ? 4 : 8);
-  return vecs <= (gradient ? kRowVecs : kLossVecs) ? 1 : (int)ceil_div(vecs, kChunkVecs);
+  const int most = !gradient ? kLossVecs : rows <= kFewRows ? kRowVecs / 2 : kRowVecs;
+  return vecs <= most ? 1 : (int)ceil_div(vecs, kChunkVecs);
 }
 
 namespace {
@@ -2054,7 +2060,7 @@ void launch_grad(const DistillArgs& a, const Part* parts, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_distill_forward(const DistillArgs& a, void* ws, hipStream_t s) {
-  const int chunks = distill_chunks(a.V, a.dtype, false);
+  const int chunks = distill_chunks(a.V, a.dtype, a.rows, false);
   Part* parts = static_cast<Part*>(ws);
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;
@@ -2075,7 +2081,7 @@ hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
-  const int chunks = distill_chunks(a.V, a.dtype, true);
+  const int chunks = distill_chunks(a.V, a.dtype, a.rows, true);
   Part* parts = static_cast<Part*>(ws);
   return by_dtype(a.dtype, [&](auto* t) {
     using T = typename Pointee<decltype(t)>::type;

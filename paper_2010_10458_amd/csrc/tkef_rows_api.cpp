@@ -188,7 +188,7 @@ int tkef_distill_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dty
   p->dtype = dtype;
   p->val_format = val_format;
   p->temperature = temperature;
-  const int chunks = tkef::distill_chunks(vocab, dtype, false);  // (the more of the two)
+  const int chunks = tkef::distill_chunks(vocab, dtype, rows, false);  // (a step has no more)
   if (chunks > 1)
     p->ws_bytes = ((size_t)rows * (size_t)chunks * tkef::kPartBytes + 255) & ~(size_t)255;
   *plan_out = p;

@@ -353,3 +353,11 @@ def test_masks_of_great_size(v, mask, dtype):
     student[5, v // 2: v // 2 + 40] = 0.0
     for temperature in (1.0, 0.8, 1.3):
         check(rng, n, v, k, dtype, temperature=temperature, student=student, teacher=teacher)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_few_and_many_long_rows(dtype):
+    """Rows that a call of few takes in chunks and one of many whole."""
+    rng = np.random.default_rng(17)
+    for n in (2, 98):
+        check(rng, n, 70003, 20, dtype, ragged=True, weighted=True)

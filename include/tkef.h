@@ -442,7 +442,10 @@ const char *tkef_lars_launch_name(int32_t dense, int32_t i);
  * tail is NaN. */
 typedef struct tkef_top_plan_s *tkef_top_plan;
 
-/* Host only. rows: the most rows an execution gives. */
+/* Host only. rows: the most rows an execution gives. No workspace is needed while a
+ * row is at most 64 KB and k <= 256, or 128 KB and k <= 128; longer rows and lists
+ * are selected in parts, whose candidates take some tens of KB a row (52 KB at
+ * k = 256 over 131,071 binary32 words, 69 KB at k = 512 over 32,000 bfloat16). */
 int tkef_top_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dtype,
                          int32_t val_format, double temperature, tkef_top_plan *plan_out);
 int tkef_top_plan_destroy(tkef_top_plan plan);
@@ -531,8 +534,8 @@ int tkef_distill_step(tkef_distill_plan plan, const void *logits, int64_t row_st
 typedef struct tkef_verify_plan_s *tkef_verify_plan;
 
 /* Host only. batch: the most sequences of an execution (<= 32768); draft: tokens
- * reserved per sequence. batch * (draft + 1) rows may hold at most 2^21 pieces
- * of 64 KB (each row at least one; TKEF_ERANGE otherwise). */
+ * reserved per sequence. batch * (draft + 1) rows may hold at most 2^22 pieces
+ * of 32 KB (each row at least one; TKEF_ERANGE otherwise). */
 int tkef_verify_plan_create(int64_t batch, int64_t draft, int64_t vocab, int32_t dtype,
                             double temperature, tkef_verify_plan *plan_out);
 int tkef_verify_plan_destroy(tkef_verify_plan plan);

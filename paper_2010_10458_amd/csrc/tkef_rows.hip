@@ -413,9 +413,10 @@ struct RadixLds {
 
 // Selection from a row of any values: radix select of the k-th largest order
 // key over four 8-bit digits, then the ordered compaction and the rest's sum.
-// Seven passes over the row; the kernels below come here with rows that have
-// NaN, that have more words in reach of the k first than LDS holds, and whose
-// rest lies more than 2^-60 below their k-th word.
+// Seven passes over the row, bound by them and by their LDS atomics (4.1 ms where all
+// of 8,192 rows of 32,000 bfloat16 words come here, the ordinary way 0.1); the kernels
+// below come here with rows that have NaN, that have more words in reach of the k first
+// than LDS holds, and whose rest lies more than 2^-60 below their k-th word.
 template <typename T, int NT>
 __device__ __forceinline__ void top_radix(const TopArgs& A, RadixLds& L, const T* p,
                                           int64_t row) {
@@ -533,8 +534,8 @@ struct FinishLds {
   uint32_t ntaken;
 };
 
-// The k first of C candidates (LDS, all >= least, then eight zeros), their places in ascending order of words,
-// and the rest: S * 2^(m a) and the candidates not taken. Up to kRankLimit
+// The k first of C candidates (LDS, all >= least, then eight zeros), their places in
+// ascending order of words, and the rest: S * 2^(m a) and the candidates not taken. Up to kRankLimit
 // candidates a thread counts the better ones of its own; beyond that the k-th
 // candidate is bisected, a candidate's word being part of it, so that ties end
 // at the lower words. A selected word's place is the number of selected lower
@@ -712,6 +713,11 @@ constexpr int top_workgroups() {
 // the least value at the bound are the candidates then, and the lowest words at
 // that value fill up; so too where the bound lies beyond what Product takes. A NaN
 // (in the sum), or too many words above the ties, send the row to top_radix.
+// Bound by the reads for k <= 64 and rows of 32,000 words (8,192 of bfloat16: 100 to 110 us,
+// 5 TB/s; as parts of 509 x 131,071 binary32, k = 256, 54 us, 4.9 TB/s), by the steps after
+// them for short rows and larger k, which are a chain of barriers that five workgroups a
+// compute unit hide in part (k = 256: 180 us; 8,000 words: k = 64 49, k = 256 155). Small
+// workgroups for that reason: in 512 threads x 8 vectors k = 64 takes 132 us, in 1,024 x 4 343.
 template <typename T, int TPB, int NV, int SUB, bool PART>
 __global__ __launch_bounds__(TPB, (top_workgroups<TPB, NV, SUB, PART>())) void k_top_row(
     TopArgs A, TopParts P) {
@@ -1026,7 +1032,9 @@ __global__ __launch_bounds__(TPB, (top_workgroups<TPB, NV, SUB, PART>())) void k
   }
 }
 
-// The k first of a row from its parts' lists.
+// The k first of a row from its parts' lists. Bound by its chain of dependent steps: heads,
+// candidates, some twelve rounds of bisection, places, values (509 rows of eight lists,
+// k = 256, 540 candidates: 17 us, two workgroups a compute unit).
 template <typename T, int TPB, int CAP>
 __global__ __launch_bounds__(TPB) void k_top_merge(TopArgs A, TopParts P) {
   __shared__ __align__(16) uint64_t cand[CAP + 8];
@@ -1309,6 +1317,11 @@ enum { kLoss = 0, kStep = 1, kPart = 2 };
 // registers before the maximum and the sum, so the unlisted sum is exact even
 // where the list has nearly all the mass; the gradient's listed words are
 // written over the vectors' stores after a barrier.
+// One read and, in a step, one write of each word: bound by memory, the eight (loss)
+// to twelve (step) operations a word, two of them exponentials, close behind. Step of
+// 8,192 x 32,000 bfloat16 200 us, 5.2 TB/s read and written; of 1,021 x 131,071 binary16, one
+// workgroup a compute unit, 127 us, 4.0 TB/s; loss of 4,096 x 32,000 bfloat16, an eighth
+// of the rows without weight, 55 us, 4.2 TB/s (8,192 rows 6.3).
 template <typename T, int TPB, int NV, int MODE>
 __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
@@ -1462,7 +1475,8 @@ __device__ __forceinline__ Part join_parts(const Part* parts, int n, const Disti
   return wave_join(p, A);
 }
 
-// loss and sums of a row from its parts, one wave a row
+// loss and sums of a row from its parts, one wave a row: bound by its launch and two
+// rounds of loads (at most 128 parts of 32 bytes a row)
 __global__ __launch_bounds__(64) void k_distill_join(DistillArgs A, const Part* parts, int chunks) {
   const int64_t row = blockIdx.x;
   const float w = A.weight != nullptr ? A.weight[row] : 1.f;
@@ -1481,6 +1495,10 @@ __global__ __launch_bounds__(64) void k_distill_join(DistillArgs A, const Part* 
 
 // Gradient of one chunk (blockIdx.y of gridDim.y) of a row, from the saved
 // sums or (parts != nullptr) from the parts of the row, then with the loss.
+// Chunks of 32 KB, each with its share of the list: no thread holds more than eight
+// vectors, so many workgroups hide the loads. Bound by memory: backward of 4,096 x 32,000
+// bfloat16, an eighth of the rows without weight, 95 us, 5.2 TB/s read and written
+// (chunks of 16 KB 113 us against 106 without such rows, of 64 KB 105).
 template <typename T, int TPB, int NV>
 __global__ __launch_bounds__(TPB) void k_distill_grad(DistillArgs A, const Part* parts) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
@@ -1668,6 +1686,9 @@ __device__ __forceinline__ float far_sum(const Span<T>& s, int v0, int n, bool e
 // joins the place's sums and decides about its token; a rejection is posted, and
 // workgroups of later places that start after it leave at once, so a large
 // batch reads little beyond each sequence's first rejection. Nothing waits.
+// Bound by memory with five operations a word close behind: 256 x 8 x 65,536 binary16 60 us
+// for the 231 MB up to the rejections, 3.8 TB/s, and some tenth more read in vain;
+// 37 x 7 x 131,071 binary32 28 us. One sequence: 5 us, a chain of three device round trips.
 template <typename T, int TPB, int NV, bool CHECK>
 __global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch W, int chunks) {
   constexpr int NW = TPB / 64;
@@ -1763,6 +1784,8 @@ __device__ __forceinline__ uint64_t race_key(float score, int word) {
 // of the target's own probabilities. The noise does not depend on where the
 // drafts ended and is asked for first. The last chunk to end writes the
 // sequence's results and leaves its counters at zero.
+// Bound by memory: 256 x 65,536 binary16 26 us, 5.1 TB/s of two rows and the noise; one
+// sequence 5 us. Kept apart from the sums: what it reads is known when they have ended.
 template <typename T, int TPB, int NV>
 __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch W) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
@@ -1935,12 +1958,11 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 //   k <= 128: whole up to 128 KB, in 512 threads (2,048 x 32,000 binary32, k = 64: 59 us
 //   against 66 in two parts; 2,048 x 64,000 bfloat16, k = 128: 89 and 80; 16 rows of
 //   64,000: 13 and 19);
-//   k > 256: rows up to 64 KB in parts of 16 KB, whose lists are some hundred words each
-//   and a thread's or two's (8,192 x 32,000 bfloat16, k = 300: 324 us, whole in 1,024 threads 1,030;
-//   k = 512: 402, 1,139; k = 1,000: 1,322, 1,573).
+//   k > 256: rows up to 64 KB in parts of 16 KB and a merge (8,192 x 32,000 bfloat16, k =
+//   300: 324 us, whole in 1,024 threads 1,030; k = 512: 402, 1,139; k = 1,000: 1,322, 1,573).
 constexpr int kPartVecs = 256 * 16, kSmallPartVecs = 256 * 4;
 // candidates that a merge in 256 and in 1,024 threads has LDS for: 21 KB, which leaves
-// room for other rows beside it, and 74 KB
+// room for other rows beside it, and 74 KB (rows of k = 1,000 and longer lists)
 constexpr int kMergeSmall = 2560, kMergeLarge = 9216;
 
 TopParts top_parts(int64_t V, int64_t k, int32_t dtype) {
@@ -2098,8 +2120,9 @@ hipError_t launch_distill_step(const DistillArgs& a, void* ws, hipStream_t s) {
 // binary16 with its race: 89 us; 1,024 x 4 93, 256 x 4 95, 1,024 x 8 96), three of them
 // a compute unit for their dynamic LDS: what starts before a rejection is posted
 // is read in vain (37 x 7 x 131,071 binary32: 49 us, 51 with four). Where those would
-// leave compute units idle, in units of 256 x 4 (64 x 5 x 32,000 bfloat16: 22 us
-// against 26) or 256 x 1 (one sequence: 15.8 against 16.8), which look for no rejection.
+// leave compute units idle, smaller units that look for no rejection: 256 x 4 (sums of 64 x 5
+// x 32,000 bfloat16 14.2 us, 14.8 in 512 x 4, 17.8 in 256 x 1; 200 x 5 x 32,000 with the race 46 in
+// 256 x 4, 44 in 512 x 4) or 256 x 1 (one sequence 6.0 us, 6.2 in 256 x 4, 7.2 in 512 x 4).
 namespace {
 constexpr int kUnitVecs = 512 * 4, kSmallVecs = 256 * 4;
 constexpr int64_t kFewUnits = 1024, kTinyUnits = 64;
@@ -2146,6 +2169,8 @@ hipError_t launch_verify(const VerifyArgs& a, const VerifyScratch& w, hipStream_
       k_verify_sums<T, 256, 1, false>
           <<<dim3((unsigned)(places * tiny)), 256, 0, s>>>(a, w, (int)tiny);
     }
+    // (chunks of 4 KB of a row where those of 16 KB would leave compute units idle: one
+    // sequence of 32,000 bfloat16 words 5.8 us, 6.4; 64 of them 11.2, 8.5 in the large ones)
     if (a.batch * ceil_div(vecs, 256 * 4) <= 128)
       k_verify_race<T, 256, 1>
           <<<dim3((unsigned)ceil_div(vecs, 256), (unsigned)a.batch), 256, 0, s>>>(a, w);

@@ -695,7 +695,7 @@ struct TopParts {
 // 509 x 131,071 binary32).
 template <int TPB, int NV, int SUB, bool PART>
 constexpr int top_workgroups() {
-  return TPB != 256 ? 1 : PART ? 4 : SUB == 1 && NV < 16 ? 8 - NV / 8 : 5;
+  return TPB != 256 ? 1 : PART ? 4 : SUB <= 2 && NV < 16 ? 8 - NV / 8 : 5;
 }
 
 // One workgroup takes a row, or a part of one, into registers, NV vectors a
@@ -2015,14 +2015,23 @@ hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s) {
       k_top_row<T, 512, 16, 1, false><<<rows, 512, 0, s>>>(a, p);
     } else if (a.k <= 64) {
       // Shares of whole threads, 256 of them: 8,192 x 8,000 bfloat16, k = 64, 52 us, 79
-      // with four shares a thread; k = 16 of 32,000 91 and 95. Four shares for k <= 256. The
-      // fewest vectors a thread that hold the row: more registers, fewer workgroups.
+      // with four shares a thread; k = 16 of 32,000 91 and 95. Two shares for k <= 128 (8,000
+      // words, k = 128: 70 us, 98 with four; 32,000 128 and 128, k = 65 114 and 119), four for
+      // k <= 256: more of them are more keys to bisect and more LDS, fewer workgroups. The
+      // fewest vectors a thread that hold the row, for the same reason.
       if (vecs <= 256 * 4)
         k_top_row<T, 256, 4, 1, false><<<rows, 256, 0, s>>>(a, p);
       else if (vecs <= 256 * 8)
         k_top_row<T, 256, 8, 1, false><<<rows, 256, 0, s>>>(a, p);
       else
         k_top_row<T, 256, 16, 1, false><<<rows, 256, 0, s>>>(a, p);
+    } else if (a.k <= 128) {
+      if (vecs <= 256 * 4)
+        k_top_row<T, 256, 4, 2, false><<<rows, 256, 0, s>>>(a, p);
+      else if (vecs <= 256 * 8)
+        k_top_row<T, 256, 8, 2, false><<<rows, 256, 0, s>>>(a, p);
+      else
+        k_top_row<T, 256, 16, 2, false><<<rows, 256, 0, s>>>(a, p);
     } else {
       if (vecs <= 256 * 4)
         k_top_row<T, 256, 4, 4, false><<<rows, 256, 0, s>>>(a, p);

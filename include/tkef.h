@@ -417,7 +417,9 @@ const char *tkef_lars_launch_name(int32_t dense, int32_t i);
  * The plans below hold sizes only, no buffers, and a call may give
  * fewer rows than the plan was created for (0 rows: nothing is launched).
  * Executions are asynchronous, only launch kernels and can be captured into a
- * graph. Limits: rows, V <= 2^20; k <= min(V, 1024); 1 <= draft <= 63;
+ * graph. A graph uses at every replay the workspace that its call was captured
+ * with: executions that may run at the same time (two graphs, or a graph and
+ * eager calls) need one each. Limits: rows, V <= 2^20; k <= min(V, 1024); 1 <= draft <= 63;
  * 1e-6 <= temperature <= 1e6 (TKEF_ERANGE otherwise).
  * ====================================================================== */
 
@@ -544,7 +546,9 @@ int tkef_verify_plan_info(tkef_verify_plan plan, size_t *workspace_bytes);
 /* Readies a workspace for the plan's executions: clears its counters on
  * `stream` (asynchronous). Every execution leaves them cleared, so a workspace
  * is bound once; a plan may have several (one for each stream that it runs
- * on). A workspace that another call has written must be bound again. */
+ * on). A workspace that another call has written must be bound again. A bind on a
+ * capturing stream is recorded, not run: it readies the workspace for that
+ * graph's executions alone. */
 int tkef_verify_plan_bind(tkef_verify_plan plan, void *ws, size_t ws_bytes,
                           hipStream_t stream);
 

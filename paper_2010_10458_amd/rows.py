@@ -11,6 +11,12 @@ only marshals arguments; the computation runs in the library's HIP kernels.
 
     vp = VerifyPlan(batch, draft, vocab, dtype=torch.bfloat16)
     accepted, tokens, logp = vp.execute(target_logits, draft_logits, drafted, uniform, noise)
+
+Every call can be captured into a graph, with or without an eager call before
+it. A captured call has a workspace of its own in the graph's memory, so graphs
+of one plan may be replayed in any order, between eager calls, and at the same
+time on several streams (graphs that were told to share one memory pool: as
+that pool allows).
 """
 from __future__ import annotations
 
@@ -55,7 +61,7 @@ class _RowPlan:
         self.dtype, self.temperature, self.check = dtype, float(temperature), bool(check)
         self._h = ctypes.c_void_p()
         self._free = getattr(lib(), self._destroy)
-        self._ws = {}  # one workspace per stream, so that calls on two streams do not share one
+        self._ws = {}  # one per stream, so that eager calls on two streams do not share one
 
     def __del__(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -67,18 +73,28 @@ class _RowPlan:
         _check(name, getattr(lib(), name)(self._h, ctypes.byref(ws)))
         self.ws_bytes = ws.value
 
-    def _workspace(self, stream: Optional[int], dev) -> Optional[int]:
+    def _workspace(self, stream: Optional[int], dev) -> Optional[torch.Tensor]:
+        """The workspace of one call, on the current stream (the caller holds it
+        until the call's launches are issued).
+
+        A captured call gets one of its own from the graph's memory, and what
+        readies it is recorded in front of the call: the graph then depends neither
+        on work that ran, or did not, before its replay, nor on what other graphs and
+        eager calls leave in a workspace of the plan. It is not kept for later
+        calls, since nothing that is captured has run."""
         if not self.ws_bytes:
             return None
-        ws = self._ws.get((stream, dev))
+        captured = torch.cuda.is_current_stream_capturing()
+        ws = None if captured else self._ws.get((stream, dev))
         if ws is None:
             ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
             self._ready(ws, stream)
-            self._ws[(stream, dev)] = ws
-        return ws.data_ptr()
+            if not captured:
+                self._ws[(stream, dev)] = ws
+        return ws
 
     def _ready(self, ws: torch.Tensor, stream: Optional[int]) -> None:
-        """Readies a new workspace on the stream that will use it."""
+        """Readies a new workspace on the stream that will use it (asynchronous)."""
 
     def _logits(self, x: torch.Tensor, what: str) -> Tuple[int, int]:
         """(rows, row stride) of a 2-D tensor of the plan's type whose rows are
@@ -164,7 +180,7 @@ class TopLogitsPlan(_RowPlan):
             ws = self._workspace(h, dev)
         rc = self._execute(
             self._h, logits.data_ptr(), ld, n, idx_out.data_ptr(), val_out.data_ptr(),
-            tail_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h)
+            tail_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_top_execute", rc)
         if own:
@@ -228,7 +244,7 @@ class DistillPlan(_RowPlan):
             ws = self._workspace(h, dev)
         rc = self._forward(
             self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
-            stats_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h)
+            stats_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_distill_forward", rc)
         if own:
@@ -254,7 +270,7 @@ class DistillPlan(_RowPlan):
             ws = self._workspace(h, dev)
         rc = self._backward(
             self._h, logits.data_ptr(), ld, n, *lists, stats.data_ptr(), _ptr(dloss),
-            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h)
+            grad_out.data_ptr(), gld, _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_distill_backward", rc)
         if own:
@@ -279,7 +295,7 @@ class DistillPlan(_RowPlan):
             ws = self._workspace(h, dev)
         rc = self._step(
             self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
-            grad_out.data_ptr(), gld, ws, self.ws_bytes, _ptr(status), h)
+            grad_out.data_ptr(), gld, _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_distill_step", rc)
         if own:
@@ -379,7 +395,7 @@ class VerifyPlan(_RowPlan):
             self._h, target.data_ptr(), tb, ti, drafts.data_ptr(), db, di, b,
             tokens.data_ptr(), uniform.data_ptr(), noise.data_ptr(),
             noise.stride(0) if b > 1 else self.vocab, _ptr(length), accepted_out.data_ptr(),
-            tokens_out.data_ptr(), logp_out.data_ptr(), ws, self.ws_bytes, _ptr(status), h)
+            tokens_out.data_ptr(), logp_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_verify_execute", rc)
         if own:

@@ -1805,8 +1805,11 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
         e[i][h] = load16_loose(noise + (int64_t)(v0 + i * TPB) * N + 4 * h);
     }
   const int len = draft_length(A, b);
-  const uint32_t posted = W.rejected[b];
-  const int n = posted != 0u ? TKEF_VERIFY_MAX_DRAFT + 1 - (int)posted : len;
+  // (0: none posted, a place beyond every length. What the workspace holds chooses among
+  // the call's rows, tokens and words and never leads outside them, also where it
+  // was not readied or something else wrote it.)
+  const uint32_t place = (uint32_t)(TKEF_VERIFY_MAX_DRAFT + 1) - W.rejected[b];
+  const int n = place < (uint32_t)len ? (int)place : len;
   const bool drafted = n < len;
   const T* type = nullptr;
   const T* tp = static_cast<const T*>(A.target) + b * A.tb + n * A.ti;
@@ -1860,7 +1863,10 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
     A.tokens_out[b * places + tid] = token;
     if (A.logp != nullptr) {
       const float4 at = W.sums[b * places + tid];
-      const float x = (float)static_cast<const T*>(A.target)[b * A.tb + tid * A.ti + token];
+      const float x =
+          (uint32_t)token < (uint32_t)A.V
+              ? (float)static_cast<const T*>(A.target)[b * A.tb + tid * A.ti + token]
+              : -kInf;
       A.logp[b * places + tid] = (x - at.x) * A.inv_t - kLn2 * log2_(at.y);
     }
   }
@@ -1889,7 +1895,8 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
     own = agent_load(&W.best[2 * b + 1]);
   }
   const uint64_t key = over != 0ull ? over : own;
-  const int word = key != 0ull ? (int)(0xFFFFFFFFu - (uint32_t)key) : -1;
+  const uint32_t best = 0xFFFFFFFFu - (uint32_t)key;
+  const int word = key != 0ull && best < (uint32_t)A.V ? (int)best : -1;
   if (lane < places) {  // (at most 64)
     if (lane >= n) {
       const int token = lane == n ? word : -1;

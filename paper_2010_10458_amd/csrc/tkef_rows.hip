@@ -526,7 +526,8 @@ constexpr int kRankLimit = 256;
 
 template <int TPB, int KMAX>
 struct FinishLds {
-  int32_t chosen[KMAX + 16];  // (and fillers up to a multiple of 16)
+  // read as int4, wherever the struct lies; and fillers up to a multiple of 16
+  alignas(16) int32_t chosen[KMAX + 16];
   uint64_t thr, top[TPB / 64];
   float others[kRankLimit];
   uint32_t count[2][TPB / 64];
@@ -548,6 +549,8 @@ __device__ __forceinline__ bool top_finish(const TopArgs& A, int64_t row, const 
                                            uint64_t lowest, float m, float S,
                                            FinishLds<TPB, KMAX>& L) {
   constexpr int NW = TPB / 64, CPT = (CAP + TPB - 1) / TPB;
+  static_assert(alignof(FinishLds<TPB, KMAX>) >= alignof(int4) && alignof(int4) == 16,
+                "L.chosen is read as int4");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, k = A.k;
   if (C < k) return false;
   const bool more = k < A.V;

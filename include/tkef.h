@@ -524,8 +524,8 @@ int tkef_distill_step(tkef_distill_plan plan, const void *logits, int64_t row_st
  * u_i in [0, 1) and noise e_v > 0 drawn from the exponential distribution:
  *   n = the first i < m with not (u_i q_i(x_i) < p_i(x_i)), or m
  *   r = max(0, p_n - q_n) if n < m (p_n if that is 0 everywhere), p_m if n == m
- *   y = the word with the largest r_v / e_v among those with r_v > 0, ties to
- *       the lower one; -1 if there is none
+ *   y = the word with the largest r_v / e_v (a quotient in binary32) among those
+ *       with r_v > 0, ties to the lower one; -1 if there is none
  *   accepted = n; tokens = x_0 .. x_{n-1}, y, -1 ...; logp = log p_i of each
  *   token (0 beside a -1)
  * The largest quotient is distributed as a draw from r / sum r, so the

@@ -1790,7 +1790,7 @@ __device__ __forceinline__ uint64_t race_key(float score, int word) {
 // of the target's own probabilities. The noise does not depend on where the
 // drafts ended and is asked for first. The last chunk to end writes the
 // sequence's results and leaves its counters at zero.
-// Bound by memory: 256 x 65,536 binary16 26 us, 5.1 TB/s of two rows and the noise; one
+// Bound by memory: 256 x 65,536 binary16 28 us, 4.8 TB/s of two rows and the noise; one
 // sequence 5 us. Kept apart from the sums: what it reads is known when they have ended.
 template <typename T, int TPB, int NV>
 __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch W) {
@@ -1831,18 +1831,31 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
   // p = 2^((x - pm) a) * pi; nothing where the row has no words
   const float pm = s.x == -kInf ? 0.f : s.x, qm = s.z == -kInf ? 0.f : s.z;
   const float pi = s.y == 0.f ? 0.f : 1.f / s.y, qi = s.w == 0.f ? 0.f : 1.f / s.w;
-  // (a thread meets its words in ascending order: a tie keeps the first)
-  float over_s = 0.f, own_s = 0.f;
-  int over_w = 0, own_w = 0;
+  // Scores are quotients, not products with the hardware's reciprocal: that is off by a
+  // unit, and infinite for noise below 2^-126. (256 x 65,536 binary16 28 us, products 27;
+  // two quotients a word, for the residual and for the target's own, 34.) A thread
+  // meets its words in ascending order: a tie keeps the first.
+  struct Best {
+    float score = 0.f;
+    int word = 0;
+    __device__ void meet(float mass, float noise_of, int w) {
+      const float q = mass > 0.f ? mass / noise_of : 0.f;
+      word = q > score ? w : word;
+      score = q > score ? q : score;
+    }
+    __device__ uint64_t key() const { return score > 0.f ? race_key(score, word) : 0ull; }
+  };
+  Best residual, target;
+  float most = 0.f;  // largest p met
+  const auto prob_of = [&](float x) { return exp2_((x - pm) * A.a) * pi; };
   const auto offer = [&](float x, float y, float noise_of, int word) {
-    const float p = exp2_((x - pm) * A.a) * pi;
-    const float r = drafted ? p - exp2_((y - qm) * A.a) * qi : p;
-    const float inv = __builtin_amdgcn_rcpf(noise_of);
-    const float so = r > 0.f ? r * inv : 0.f, sp = p > 0.f ? p * inv : 0.f;
-    over_w = so > over_s ? word : over_w;
-    over_s = so > over_s ? so : over_s;
-    own_w = sp > own_s ? word : own_w;
-    own_s = sp > own_s ? sp : own_s;
+    const float p = prob_of(x);
+    most = fmaxf(most, p);
+    residual.meet(drafted ? p - exp2_((y - qm) * A.a) * qi : p, noise_of, word);
+  };
+  const auto word_of_vec = [](const uint4 (&u)[N / 4], int j) {
+    const uint4 h = u[j / 4];
+    return __uint_as_float(j % 4 == 0 ? h.x : j % 4 == 1 ? h.y : j % 4 == 2 ? h.z : h.w);
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -1852,17 +1865,28 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
       unpack(r[i], x, type);
       unpack(drafted ? q[i] : none_of(type), y, type);
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const uint4 u = e[i][j / 4];
-        const uint32_t w = j % 4 == 0 ? u.x : j % 4 == 1 ? u.y : j % 4 == 2 ? u.z : u.w;
-        offer(x[j], y[j], __uint_as_float(w), v * N + j);
-      }
+      for (int j = 0; j < N; ++j) offer(x[j], y[j], word_of_vec(e[i], j), v * N + j);
     }
   }
+  // a word after the vectors, by a thread that has met lower words alone
   const int w = nvec * N + tid;
-  if (blockIdx.x == 0 && w < A.V) {
-    // a word after the vectors, by a thread that has met lower words alone
-    offer((float)tp[w], drafted ? (float)dp[w] : -kInf, noise[w], w);
+  const bool more = blockIdx.x == 0 && w < A.V;
+  if (more) offer((float)tp[w], drafted ? (float)dp[w] : -kInf, noise[w], w);
+  // The target's own probabilities count where the whole row's residual is empty, so
+  // they are raced for by waves that met no residual, from memory again.
+  if (drafted && __ballot(residual.score > 0.f) == 0ull && __ballot(most > 0.f) != 0ull) {
+    for (int i = 0; i < NV; ++i) {
+      const int v = v0 + i * TPB;
+      if (v >= nvec) break;
+      float x[N];
+      unpack(load16_loose(tp + (int64_t)v * N), x, type);
+      uint4 u[N / 4];
+#pragma unroll
+      for (int h = 0; h < N / 4; ++h) u[h] = load16_loose(noise + (int64_t)v * N + 4 * h);
+#pragma unroll
+      for (int j = 0; j < N; ++j) target.meet(prob_of(x[j]), word_of_vec(u, j), v * N + j);
+    }
+    if (more) target.meet(prob_of((float)tp[w]), noise[w], w);
   }
   if (blockIdx.x == 0 && tid < n) {  // the accepted drafts
     const int token = A.tokens[b * A.draft + tid];
@@ -1876,10 +1900,7 @@ __global__ __launch_bounds__(TPB) void k_verify_race(VerifyArgs A, VerifyScratch
       A.logp[b * places + tid] = (x - at.x) * A.inv_t - kLn2 * log2_(at.y);
     }
   }
-  uint64_t over = over_s > 0.f ? race_key(over_s, over_w) : 0ull;
-  uint64_t own = own_s > 0.f ? race_key(own_s, own_w) : 0ull;
-  over = wave_max64(over);
-  own = wave_max64(own);
+  uint64_t over = wave_max64(residual.key()), own = wave_max64(target.key());
   if (lane == 0) {
     red[0][tid >> 6] = over;
     red[1][tid >> 6] = own;

@@ -228,11 +228,10 @@ int tkef_distill_forward(tkef_distill_plan plan, const void* logits, int64_t row
 int tkef_distill_backward(tkef_distill_plan plan, const void* logits, int64_t row_stride,
                           int64_t rows, const int32_t* idx, const void* val, const float* tail,
                           const int32_t* count, const float* weight, const float* stats,
-                          const float* dloss, void* grad, int64_t grad_stride, void* ws,
-                          size_t ws_bytes, uint32_t* status, hipStream_t stream) {
+                          const float* dloss, void* grad, int64_t grad_stride, void* /*ws*/,
+                          size_t /*ws_bytes*/, uint32_t* status, hipStream_t stream) {
   if (plan == nullptr) return TKEF_EINVAL;
   int rc = check_rows(*plan, logits, row_stride, rows);
-  if (rc == TKEF_OK) rc = check_ws(plan->ws_bytes, ws, ws_bytes);
   if (rc != TKEF_OK || rows == 0) return rc;
   rc = check_lists(*plan, idx, val, tail, count, weight);
   if (rc == TKEF_OK) rc = check_grad(*plan, logits, row_stride, rows, grad, grad_stride);

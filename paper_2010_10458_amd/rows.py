@@ -267,10 +267,9 @@ class DistillPlan(_RowPlan):
         with _on(stream):
             grad_out, gld = self._grad(logits, grad_out)
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
         rc = self._backward(
             self._h, logits.data_ptr(), ld, n, *lists, stats.data_ptr(), _ptr(dloss),
-            grad_out.data_ptr(), gld, _ptr(ws), self.ws_bytes, _ptr(status), h)
+            grad_out.data_ptr(), gld, None, 0, _ptr(status), h)
         if rc:
             _check("tkef_distill_backward", rc)
         if own:

@@ -52,10 +52,10 @@ int check_rows(const RowPlan& p, const void* z, int64_t ld, int64_t rows) {
 }
 
 int check_lists(const RowPlan& p, const int32_t* idx, const void* val, const float* tail,
-                const int32_t* count, const float* weight) {
+                const int32_t* count, const float* weight, const uint32_t* status) {
   if (idx == nullptr || val == nullptr) return TKEF_EINVAL;
   if (!aligned(idx, 4) || !aligned(val, p.val_format == TKEF_VAL_F16 ? 2 : 4) ||
-      !aligned(tail, 4) || !aligned(count, 4) || !aligned(weight, 4))
+      !aligned(tail, 4) || !aligned(count, 4) || !aligned(weight, 4) || !aligned(status, 4))
     return TKEF_EINVAL;
   return TKEF_OK;
 }
@@ -153,7 +153,8 @@ int tkef_top_execute(tkef_top_plan plan, const void* logits, int64_t row_stride,
   if (rc == TKEF_OK) rc = check_ws(plan->ws_bytes, ws, ws_bytes);
   if (rc != TKEF_OK || rows == 0) return rc;
   if (idx_out == nullptr || val_out == nullptr || !aligned(idx_out, 4) ||
-      !aligned(val_out, plan->val_format == TKEF_VAL_F16 ? 2 : 4) || !aligned(tail_out, 4))
+      !aligned(val_out, plan->val_format == TKEF_VAL_F16 ? 2 : 4) || !aligned(tail_out, 4) ||
+      !aligned(status, 4))
     return TKEF_EINVAL;
   tkef::TopArgs a{};
   a.z = logits;
@@ -215,7 +216,7 @@ int tkef_distill_forward(tkef_distill_plan plan, const void* logits, int64_t row
   int rc = check_rows(*plan, logits, row_stride, rows);
   if (rc == TKEF_OK) rc = check_ws(plan->ws_bytes, ws, ws_bytes);
   if (rc != TKEF_OK || rows == 0) return rc;
-  rc = check_lists(*plan, idx, val, tail, count, weight);
+  rc = check_lists(*plan, idx, val, tail, count, weight, status);
   if (rc != TKEF_OK) return rc;
   if (loss == nullptr || !aligned(loss, 4) || !aligned(stats, 16)) return TKEF_EINVAL;
   tkef::DistillArgs a =
@@ -233,7 +234,7 @@ int tkef_distill_backward(tkef_distill_plan plan, const void* logits, int64_t ro
   if (plan == nullptr) return TKEF_EINVAL;
   int rc = check_rows(*plan, logits, row_stride, rows);
   if (rc != TKEF_OK || rows == 0) return rc;
-  rc = check_lists(*plan, idx, val, tail, count, weight);
+  rc = check_lists(*plan, idx, val, tail, count, weight, status);
   if (rc == TKEF_OK) rc = check_grad(*plan, logits, row_stride, rows, grad, grad_stride);
   if (rc != TKEF_OK) return rc;
   if (stats == nullptr || !aligned(stats, 16) || !aligned(dloss, 4)) return TKEF_EINVAL;
@@ -255,7 +256,7 @@ int tkef_distill_step(tkef_distill_plan plan, const void* logits, int64_t row_st
   int rc = check_rows(*plan, logits, row_stride, rows);
   if (rc == TKEF_OK) rc = check_ws(plan->ws_bytes, ws, ws_bytes);
   if (rc != TKEF_OK || rows == 0) return rc;
-  rc = check_lists(*plan, idx, val, tail, count, weight);
+  rc = check_lists(*plan, idx, val, tail, count, weight, status);
   if (rc == TKEF_OK) rc = check_grad(*plan, logits, row_stride, rows, grad, grad_stride);
   if (rc != TKEF_OK) return rc;
   if (loss == nullptr || !aligned(loss, 4)) return TKEF_EINVAL;
@@ -333,7 +334,8 @@ int tkef_verify_execute(tkef_verify_plan plan, const void* target, int64_t targe
       tokens_out == nullptr)
     return TKEF_EINVAL;
   if (!aligned(tokens, 4) || !aligned(uniform, 4) || !aligned(noise, 4) || !aligned(length, 4) ||
-      !aligned(accepted, 4) || !aligned(tokens_out, 4) || !aligned(logp_out, 4))
+      !aligned(accepted, 4) || !aligned(tokens_out, 4) || !aligned(logp_out, 4) ||
+      !aligned(status, 4))
     return TKEF_EINVAL;
   tkef::VerifyArgs a{};
   a.target = target;

@@ -120,8 +120,11 @@ class _RowPlan:
         return n, (x.stride(0) if n > 1 else vocab)
 
     def _status_of(self, status, dev):
-        if status is None and self.check:
-            return _new_status(dev), True
+        if status is None:
+            return (_new_status(dev), True) if self.check else (None, False)
+        if status.dtype not in (torch.int32, torch.uint32) or status.numel() < 1 \
+                or not status.is_cuda:
+            raise ValueError("status: expected an int32 CUDA tensor")
         return status, False
 
 

@@ -12,6 +12,9 @@ only marshals arguments; the computation runs in the library's HIP kernels.
     vp = VerifyPlan(batch, draft, vocab, dtype=torch.bfloat16)
     accepted, tokens, logp = vp.execute(target_logits, draft_logits, drafted, uniform, noise)
 
+A call's tensors are all on one GPU, that of the stream it runs on (the current
+one, or the caller's `stream`).
+
 Every call can be captured into a graph, with or without an eager call before
 it. A captured call has a workspace of its own in the graph's memory, so graphs
 of one plan may be replayed in any order, between eager calls, and at the same
@@ -25,7 +28,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import _check, _new_status, _raise_on_status, _stream_handle, _val_format, lib
+from . import _check, _new_status, _raise_on_status, _val_format, lib
 
 DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
 ROWS_MAX_ROWS = ROWS_MAX_VOCAB = 1 << 20
@@ -47,10 +50,26 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr() if t is not None else None
 
 
-def _check_vector(t: Optional[torch.Tensor], n: int, dtype, what: str) -> None:
-    if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_cuda
+def _check_vector(t: Optional[torch.Tensor], n: int, dtype, what: str, gpu: int) -> None:
+    """(get_device: 0.05 us less than a comparison of devices, which a small call
+    makes six times)"""
+    if t is not None and (t.dtype is not dtype or t.numel() != n or t.get_device() != gpu
                           or not t.is_contiguous()):
-        raise ValueError(f"{what}: expected {n} contiguous {dtype} CUDA values")
+        raise ValueError(f"{what}: expected {n} contiguous {dtype} values on cuda:{gpu}")
+
+
+def _launch_on(gpu: int, stream) -> Optional[int]:
+    """Handle of the stream that a call on tensors of a GPU launches on: the
+    caller's, or the current one."""
+    if stream is not None:
+        index, handle = stream.device_index, stream.cuda_stream
+    else:
+        # (0.4 us without building a Stream object)
+        index = torch.cuda.current_device()
+        handle = torch._C._cuda_getCurrentRawStream(index)
+    if index != gpu:
+        raise ValueError(f"the tensors are on cuda:{gpu}, the call's stream is on cuda:{index}")
+    return handle or None
 
 
 class _RowPlan:
@@ -123,8 +142,8 @@ class _RowPlan:
         if status is None:
             return (_new_status(dev), True) if self.check else (None, False)
         if status.dtype not in (torch.int32, torch.uint32) or status.numel() < 1 \
-                or not status.is_cuda:
-            raise ValueError("status: expected an int32 CUDA tensor")
+                or not status.is_cuda or status.device != dev:
+            raise ValueError(f"status: expected an int32 CUDA tensor on {dev}")
         return status, False
 
 
@@ -154,7 +173,7 @@ def _out(t: Optional[torch.Tensor], shape: Tuple[int, ...], dtype, dev, what: st
     n = 1
     for d in shape:
         n *= d
-    _check_vector(t, n, dtype, what)
+    _check_vector(t, n, dtype, what, dev.index)
     return t
 
 
@@ -185,7 +204,7 @@ class TopLogitsPlan(_RowPlan):
         """Returns idx (n, k) int32, val (n, k) of val_dtype, tail (n,) float32."""
         n, ld = self._logits(logits, "logits")
         dev = logits.device
-        h = _stream_handle(stream)
+        h = _launch_on(dev.index, stream)
         with _on(stream):
             idx_out = _out(idx_out, (n, self.k), torch.int32, dev, "idx_out")
             val_out = _out(val_out, (n, self.k), self.val_dtype, dev, "val_out")
@@ -224,20 +243,20 @@ class DistillPlan(_RowPlan):
         self._forward, self._backward, self._step = (
             L.tkef_distill_forward, L.tkef_distill_backward, L.tkef_distill_step)
 
-    def _lists(self, n, idx, val, tail, count, weight):
-        _check_vector(idx, n * self.k, torch.int32, "idx")
-        _check_vector(val, n * self.k, self.val_dtype, "val")
-        _check_vector(tail, n, torch.float32, "tail")
-        _check_vector(count, n, torch.int32, "count")
-        _check_vector(weight, n, torch.float32, "weight")
+    def _lists(self, n, idx, val, tail, count, weight, gpu):
+        _check_vector(idx, n * self.k, torch.int32, "idx", gpu)
+        _check_vector(val, n * self.k, self.val_dtype, "val", gpu)
+        _check_vector(tail, n, torch.float32, "tail", gpu)
+        _check_vector(count, n, torch.int32, "count", gpu)
+        _check_vector(weight, n, torch.float32, "weight", gpu)
         return (idx.data_ptr(), val.data_ptr(), _ptr(tail), _ptr(count), _ptr(weight))
 
     def _grad(self, logits, grad_out):
         if grad_out is None:
             grad_out = _out(None, tuple(logits.shape), self.dtype, logits.device, "grad_out")
             return grad_out, self.vocab
-        elif grad_out.shape != logits.shape:
-            raise ValueError("grad_out: expected the shape of the logits")
+        elif grad_out.shape != logits.shape or grad_out.device != logits.device:
+            raise ValueError("grad_out: expected the shape and device of the logits")
         return grad_out, self._logits(grad_out, "grad_out")[1]
 
     def forward(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
@@ -248,9 +267,9 @@ class DistillPlan(_RowPlan):
                 ) -> Tuple[torch.Tensor, torch.Tensor]:
         """Returns loss (n,) float32 and stats (n, 4) float32, which backward takes."""
         n, ld = self._logits(logits, "logits")
-        lists = self._lists(n, idx, val, tail, count, weight)
         dev = logits.device
-        h = _stream_handle(stream)
+        lists = self._lists(n, idx, val, tail, count, weight, dev.index)
+        h = _launch_on(dev.index, stream)
         with _on(stream):
             loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
             stats_out = _out(stats_out, (n, 4), torch.float32, dev, "stats_out")
@@ -273,11 +292,11 @@ class DistillPlan(_RowPlan):
         """Gradient of sum(dloss * loss) (dloss (n,) float32, default 1) in the
         logits' type. grad_out may be the logits themselves."""
         n, ld = self._logits(logits, "logits")
-        lists = self._lists(n, idx, val, tail, count, weight)
-        _check_vector(stats, n * 4, torch.float32, "stats")
-        _check_vector(dloss, n, torch.float32, "dloss")
         dev = logits.device
-        h = _stream_handle(stream)
+        lists = self._lists(n, idx, val, tail, count, weight, dev.index)
+        _check_vector(stats, n * 4, torch.float32, "stats", dev.index)
+        _check_vector(dloss, n, torch.float32, "dloss", dev.index)
+        h = _launch_on(dev.index, stream)
         with _on(stream):
             grad_out, gld = self._grad(logits, grad_out)
             status, own = self._status_of(status, dev)
@@ -298,9 +317,9 @@ class DistillPlan(_RowPlan):
         """Loss (n,) float32 and the gradient of its sum, in one call.
         grad_out may be the logits themselves."""
         n, ld = self._logits(logits, "logits")
-        lists = self._lists(n, idx, val, tail, count, weight)
         dev = logits.device
-        h = _stream_handle(stream)
+        lists = self._lists(n, idx, val, tail, count, weight, dev.index)
+        h = _launch_on(dev.index, stream)
         with _on(stream):
             loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
             grad_out, gld = self._grad(logits, grad_out)
@@ -389,16 +408,16 @@ class VerifyPlan(_RowPlan):
         tb, ti = self._block(target, self.draft + 1, "target")
         db, di = self._block(drafts, self.draft, "drafts")
         b = target.shape[0]
-        if drafts.shape[0] != b:
-            raise ValueError("target and drafts differ in their number of sequences")
-        _check_vector(tokens, b * self.draft, torch.int32, "tokens")
-        _check_vector(uniform, b * self.draft, torch.float32, "uniform")
-        _check_vector(length, b, torch.int32, "length")
-        if noise.dtype != torch.float32 or not noise.is_cuda or \
-                noise.shape != (b, self.vocab) or (self.vocab > 1 and noise.stride(1) != 1):
-            raise ValueError("noise: expected (batch, vocab) float32 CUDA values in rows")
         dev = target.device
-        h = _stream_handle(stream)
+        if drafts.shape[0] != b or drafts.device != dev:
+            raise ValueError("target and drafts differ in their number of sequences or device")
+        _check_vector(tokens, b * self.draft, torch.int32, "tokens", dev.index)
+        _check_vector(uniform, b * self.draft, torch.float32, "uniform", dev.index)
+        _check_vector(length, b, torch.int32, "length", dev.index)
+        if noise.dtype != torch.float32 or noise.device != dev or \
+                noise.shape != (b, self.vocab) or (self.vocab > 1 and noise.stride(1) != 1):
+            raise ValueError(f"noise: expected (batch, vocab) float32 values in rows on {dev}")
+        h = _launch_on(dev.index, stream)
         with _on(stream):
             accepted_out = _out(accepted_out, (b,), torch.int32, dev, "accepted_out")
             tokens_out = _out(tokens_out, (b, self.draft + 1), torch.int32, dev, "tokens_out")

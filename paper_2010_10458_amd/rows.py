@@ -381,6 +381,20 @@ class VerifyPlan(_RowPlan):
         _check("tkef_verify_plan_bind", lib().tkef_verify_plan_bind(
             self._h, ws.data_ptr(), ws.numel(), stream))
 
+    def workspace(self, stream=None) -> torch.Tensor:
+        """A readied workspace for `execute(ws=...)` on the current GPU, cleared on
+        `stream` (asynchronous). The caller keeps it for as long as calls, or graphs
+        that captured one, may use it, and gives it to no two that may run at the same
+        time. Without one a captured call clears its own at every replay, a launch
+        more (64 sequences of 5 tokens: 32 us a replay, 26 with a workspace given)."""
+        with _on(stream):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a workspace is readied before the capture that uses it")
+            gpu = torch.cuda.current_device()
+            ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=torch.device("cuda", gpu))
+            self._ready(ws, _launch_on(gpu, stream))
+        return ws
+
     def _block(self, x: torch.Tensor, places: int, what: str) -> Tuple[int, int]:
         if x.dim() != 3 or x.dtype != self.dtype or not x.is_cuda:
             raise ValueError(f"{what}: expected a 3-D CUDA tensor of {self.dtype}")
@@ -397,14 +411,17 @@ class VerifyPlan(_RowPlan):
                 accepted_out: Optional[torch.Tensor] = None,
                 tokens_out: Optional[torch.Tensor] = None,
                 logp_out: Optional[torch.Tensor] = None,
-                status: Optional[torch.Tensor] = None, stream=None
+                status: Optional[torch.Tensor] = None, stream=None,
+                ws: Optional[torch.Tensor] = None
                 ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
         """target (b, draft + 1, vocab) and drafts (b, draft, vocab) logits,
         tokens (b, draft) int32, uniform (b, draft) float32 in [0, 1), noise
         (b, vocab) float32 from the exponential distribution, length (b,) int32.
         Returns accepted (b,) int32, tokens (b, draft + 1) int32 (accepted
         drafts, the token after them, then -1) and their log-probabilities
-        under the target (b, draft + 1) float32."""
+        under the target (b, draft + 1) float32. ws: a workspace of this plan
+        (`workspace`); by default the plan has one for each stream, and a captured call
+        its own."""
         tb, ti = self._block(target, self.draft + 1, "target")
         db, di = self._block(drafts, self.draft, "drafts")
         b = target.shape[0]
@@ -423,7 +440,10 @@ class VerifyPlan(_RowPlan):
             tokens_out = _out(tokens_out, (b, self.draft + 1), torch.int32, dev, "tokens_out")
             logp_out = _out(logp_out, (b, self.draft + 1), torch.float32, dev, "logp_out")
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
+            if ws is None:
+                ws = self._workspace(h, dev)
+            else:
+                _check_vector(ws, self.ws_bytes, torch.uint8, "ws", dev.index)
         rc = self._execute(
             self._h, target.data_ptr(), tb, ti, drafts.data_ptr(), db, di, b,
             tokens.data_ptr(), uniform.data_ptr(), noise.data_ptr(),

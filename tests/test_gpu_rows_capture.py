@@ -105,3 +105,38 @@ def test_two_graphs_of_plans_over_long_rows():
         torch.cuda.synchronize()
         for n in fixed:
             assert same(outs[n], want[n]), n
+
+
+def test_graphs_with_workspaces_given():
+    """A workspace that was readied before the capture serves its graph's replays,
+    each of which leaves it ready; two such graphs run at the same time."""
+    dev = need_gpu()
+    gen = torch.Generator(device=dev).manual_seed(8)
+    draft, vocab = 3, 32000
+    plan = tk.VerifyPlan(24, draft, vocab, dtype=torch.float32)
+    fixed = {b: verify_inputs(gen, b, draft, vocab) for b in (24, 2)}
+    announce("graphs with workspaces given")
+    plan.execute(*fixed[24])
+    ws = {b: plan.workspace() for b in fixed}
+    assert ws[24].data_ptr() != ws[2].data_ptr()
+    torch.cuda.synchronize()
+    graphs, outs, streams = {}, {}, {}
+    for b in fixed:
+        graphs[b], streams[b] = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graphs[b]):
+            outs[b] = plan.execute(*fixed[b], ws=ws[b])
+    for _ in range(4):
+        want = {}
+        for b in fixed:
+            for a, x in zip(fixed[b], verify_inputs(gen, b, draft, vocab)):
+                a.copy_(x)
+            want[b] = [w.clone() for w in plan.execute(*fixed[b])]
+            assert same(plan.execute(*fixed[b], ws=ws[b]), want[b])
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for b in fixed:
+                with torch.cuda.stream(streams[b]):
+                    graphs[b].replay()
+        torch.cuda.synchronize()
+        for b in fixed:
+            assert same(outs[b], want[b]), b

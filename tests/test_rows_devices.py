@@ -109,3 +109,21 @@ def test_one_tensor_of_the_other_calls_on_another_gpu():
         top(out=1)
     with pytest.raises(ValueError, match="status"):
         top(status=1)
+
+
+def test_a_given_workspace_of_another_size_type_or_gpu():
+    p = tk.VerifyPlan(2, 3, 50, dtype=torch.float32)
+    kw = dict(target=(2, 4, 50), drafts=(2, 3, 50), tokens=(2, 3), uniform=(2, 3), noise=(2, 50),
+              accepted_out=(2,), tokens_out=(2, 4), logp_out=(2, 4))
+    ints = ("tokens", "accepted_out", "tokens_out")
+    args = {k: OnGpu(v, torch.int32 if k in ints else torch.float32) for k, v in kw.items()}
+    for bad in (OnGpu((p.ws_bytes - 1,), torch.uint8), OnGpu((p.ws_bytes,), torch.int8),
+                OnGpu((p.ws_bytes,), torch.uint8, gpu=1)):
+        with pytest.raises(ValueError, match="ws"):
+            p.execute(ws=bad, **args)
+
+
+def test_no_workspace_is_readied_in_a_capture(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="before the capture"):
+        tk.VerifyPlan(2, 3, 50, dtype=torch.float32).workspace()

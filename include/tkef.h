@@ -503,8 +503,10 @@ int tkef_distill_forward(tkef_distill_plan plan, const void *logits, int64_t row
  * type. dloss: device, one binary32 value per row, or NULL (1). The other
  * inputs are those of the forward pass, stats what it gave. grad: device, rows
  * grad_stride elements apart (grad_stride >= V); it may be the logits
- * themselves (same address and stride), and must not overlap them otherwise. ws
- * is not used and may be NULL. */
+ * themselves (same address and stride), and must not overlap them otherwise. It
+ * may lie between their rows at the same stride (other columns of one buffer),
+ * at another stride only before or after all of them. ws is not used and may be
+ * NULL. */
 int tkef_distill_backward(tkef_distill_plan plan, const void *logits, int64_t row_stride,
                           int64_t rows, const int32_t *idx, const void *val, const float *tail,
                           const int32_t *count, const float *weight, const float *stats,

@@ -60,17 +60,22 @@ int check_lists(const RowPlan& p, const int32_t* idx, const void* val, const flo
   return TKEF_OK;
 }
 
-// grad is the logits themselves or does not touch them
+// grad is the logits themselves or does not touch them: it lies before or after all of
+// their rows, or between them at their stride
 int check_grad(const RowPlan& p, const void* z, int64_t ld, int64_t rows, const void* g,
                int64_t gld) {
   if (gld > kMaxStride) return TKEF_ERANGE;
   if (g == nullptr || !aligned(g, elem_size(p.dtype)) || gld < p.vocab) return TKEF_EINVAL;
   if (g == z && gld == ld) return TKEF_OK;
-  const size_t e = elem_size(p.dtype);
+  const size_t e = elem_size(p.dtype), row = (size_t)p.vocab * e, step = (size_t)ld * e;
   const uintptr_t za = reinterpret_cast<uintptr_t>(z), ga = reinterpret_cast<uintptr_t>(g);
-  const uintptr_t ze = za + ((size_t)(rows - 1) * (size_t)ld + (size_t)p.vocab) * e;
-  const uintptr_t ge = ga + ((size_t)(rows - 1) * (size_t)gld + (size_t)p.vocab) * e;
-  return za < ge && ga < ze ? TKEF_EINVAL : TKEF_OK;
+  const uintptr_t ze = za + (size_t)(rows - 1) * step + row;
+  const uintptr_t ge = ga + (size_t)(rows - 1) * (size_t)gld * e + row;
+  if (za >= ge || ga >= ze) return TKEF_OK;
+  if (gld != ld) return TKEF_EINVAL;
+  // where a row of grad begins behind the row of logits before it
+  const size_t at = ga >= za ? (ga - za) % step : (step - (za - ga) % step) % step;
+  return at >= row && at + row <= step ? TKEF_OK : TKEF_EINVAL;
 }
 
 int done(hipError_t e) { return e == hipSuccess ? TKEF_OK : TKEF_EHIP; }

@@ -533,9 +533,11 @@ int tkef_distill_step(tkef_distill_plan plan, const void *logits, int64_t row_st
  *   token (0 beside a -1)
  * The largest quotient is distributed as a draw from r / sum r, so the
  * sequence that results is distributed as the target's own. A drafted token
- * outside [0, V) is rejected and sets TKEF_STATUS_INDEX_RANGE; a NaN or +inf
- * logit makes its row's probabilities NaN, which accepts nothing and samples
- * nothing, and sets TKEF_STATUS_NAN where the result depends on it. */
+ * outside [0, V) is rejected and sets TKEF_STATUS_INDEX_RANGE. A NaN or +inf
+ * logit makes its row's probabilities NaN, and sets TKEF_STATUS_NAN where the
+ * result depends on them. They accept nothing: a place with such a drafts row
+ * rejects its token, its residual is empty, and y is drawn from the target's p_n;
+ * one with such a target row has y = -1. */
 typedef struct tkef_verify_plan_s *tkef_verify_plan;
 
 /* Host only. batch: the most sequences of an execution (<= 32768); draft: tokens

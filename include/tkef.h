@@ -445,9 +445,12 @@ const char *tkef_lars_launch_name(int32_t dense, int32_t i);
 typedef struct tkef_top_plan_s *tkef_top_plan;
 
 /* Host only. rows: the most rows an execution gives. No workspace is needed while a
- * row is at most 64 KB and k <= 256, or 128 KB and k <= 128; longer rows and lists
- * are selected in parts, whose candidates take some tens of KB a row (52 KB at
- * k = 256 over 131,071 binary32 words, 69 KB at k = 512 over 32,000 bfloat16). */
+ * row is at most 64 KB and k <= 256, or 128 KB and k <= 128. Longer rows and lists
+ * are selected in P parts of 64 KB (16 KB where k > 256 and the row has at most 64 KB),
+ * whose candidates take, with s = k / P, at most P (8 k + 72 (s + 4 sqrt(s) + 8) +
+ * 160) bytes a row, for all rows of the plan: 53 KB at k = 256 over 131,071 binary32
+ * words, 69 KB at k = 512 over 32,000 bfloat16, 171 KB at k = 1,024 over 131,071
+ * binary32, and 718 KB, the most, at k = 1,024 over 2^20 binary32. */
 int tkef_top_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dtype,
                          int32_t val_format, double temperature, tkef_top_plan *plan_out);
 int tkef_top_plan_destroy(tkef_top_plan plan);

@@ -1,6 +1,7 @@
 """Workspaces of the row operators on the CPU: which calls ask for one (no call
 here reaches the GPU)."""
 import ctypes
+import math
 import weakref
 
 import pytest
@@ -41,3 +42,38 @@ def test_large_scratch_is_given_back_after_the_call(make):
     gone = [weakref.ref(t) for t in held]
     del held
     assert all(g() is None for g in gone)
+
+
+def top_bytes(rows, v, k, dtype):
+    h, ws = ctypes.c_void_p(), ctypes.c_size_t()
+    assert tk.lib().tkef_top_plan_create(rows, v, k, dtype, tk.VAL_F32, 1.0,
+                                         ctypes.byref(h)) == tk.OK
+    assert tk.lib().tkef_top_plan_info(h, ctypes.byref(ws)) == tk.OK
+    tk.lib().tkef_top_plan_destroy(h)
+    return ws.value
+
+
+@pytest.mark.parametrize("dtype", [tk.DTYPE_F32, tk.DTYPE_F16, tk.DTYPE_BF16])
+def test_the_selection_keeps_to_the_stated_workspace(dtype):
+    rows, size = 1024, 4 if dtype == tk.DTYPE_F32 else 2
+    for v in (300, 1000, 4100, 8300, 16384, 16400, 32000, 32768, 32800, 65536, 70001, 131071,
+              262147, 1 << 20):
+        for k in (1, 64, 65, 128, 129, 256, 257, 300, 512, 700, 1000, 1024):
+            if k > v:
+                continue
+            got = top_bytes(rows, v, k, dtype)
+            vectors = v * size // 16
+            if vectors <= 4096 and k <= 256 or vectors <= 8192 and k <= 128:
+                assert got == 0
+                continue
+            part = 1024 if k > 256 and vectors <= 4096 else 4096
+            parts = max(1, -(-vectors // part))
+            s = k / parts
+            most = parts * (8 * k + 72 * (s + 4 * math.sqrt(s) + 8) + 160)
+            assert 0 < got <= rows * most + 512, (v, k, got / rows, most)
+
+
+def test_the_stated_figures_of_the_selections_workspace():
+    for v, k, dtype, kb in ((131071, 256, tk.DTYPE_F32, 53), (32000, 512, tk.DTYPE_BF16, 69),
+                            (131071, 1024, tk.DTYPE_F32, 171), (1 << 20, 1024, tk.DTYPE_F32, 718)):
+        assert round(top_bytes(1 << 10, v, k, dtype) / (1 << 10) / 1000) == kb, (v, k)

@@ -1300,8 +1300,8 @@ __device__ __forceinline__ int used_entries(const DistillArgs& A, int64_t row) {
   return c < 0 ? 0 : c < A.k ? c : A.k;
 }
 
-// Zeros over elements [v0, v1) of vectors and, where `edges`, the extras of a
-// row of grad (its own span: the gradient's address decides the vectors).
+// Zeros over the vectors of chunk `chunk` of `chunks` of a row of grad (its own span: the
+// gradient's address decides the vectors), the first chunk with the extras.
 template <typename T, int TPB>
 __device__ __forceinline__ void zero_row(T* g, int V, int chunk, int chunks) {
   const Span<T> s(g, V);

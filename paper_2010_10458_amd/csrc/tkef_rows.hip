@@ -1327,7 +1327,8 @@ enum { kLoss = 0, kStep = 1, kPart = 2 };
 // to twelve (step) operations a word, two of them exponentials, close behind. Step of
 // 8,192 x 32,000 bfloat16 200 us, 5.2 TB/s read and written; of 1,021 x 131,071 binary16, one
 // workgroup a compute unit, 127 us, 4.0 TB/s; loss of 4,096 x 32,000 bfloat16, an eighth
-// of the rows without weight, 55 us, 4.2 TB/s (8,192 rows 6.3).
+// of the rows without weight, 55 us, 4.2 TB/s: 14 us of a row's chain that nothing hides at
+// the start and the end, and 10.6 ns a row, 6.1 TB/s (8,192 rows 101 us).
 template <typename T, int TPB, int NV, int MODE>
 __global__ __launch_bounds__(TPB) void k_distill_row(DistillArgs A, Part* parts) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
@@ -1692,9 +1693,9 @@ __device__ __forceinline__ float far_sum(const Span<T>& s, int v0, int n, bool e
 // joins the place's sums and decides about its token; a rejection is posted, and
 // workgroups of later places that start after it leave at once, so a large
 // batch reads little beyond each sequence's first rejection. Nothing waits.
-// Bound by memory with five operations a word close behind: 256 x 8 x 65,536 binary16 60 us
-// for the 231 MB up to the rejections, 3.8 TB/s, and some tenth more read in vain;
-// 37 x 7 x 131,071 binary32 28 us. One sequence: 5 us, a chain of three device round trips.
+// Bound by memory with five operations a word close behind: 256 x 8 x 65,536 binary16 62 to
+// 67 us for the 231 MB up to the rejections, 3.6 TB/s, and some tenth more read in vain;
+// 37 x 7 x 131,071 binary32 29 to 32 us. One sequence: 5 us, a chain of three device round trips.
 template <typename T, int TPB, int NV, bool CHECK>
 __global__ __launch_bounds__(TPB) void k_verify_sums(VerifyArgs A, VerifyScratch W, int chunks) {
   constexpr int NW = TPB / 64;
@@ -1993,7 +1994,7 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 //   against 66 in two parts; 2,048 x 64,000 bfloat16, k = 128: 89 and 80; 16 rows of
 //   64,000: 13 and 19);
 //   k > 256: rows up to 64 KB in parts of 16 KB and a merge (8,192 x 32,000 bfloat16, k =
-//   300: 324 us, whole in 1,024 threads 1,030; k = 512: 402, 1,139; k = 1,000: 1,322, 1,573).
+//   300: 318 us, whole in 1,024 threads 1,030; k = 512: 392, 1,139; k = 1,000: 1,304, 1,573).
 constexpr int kPartVecs = 256 * 16, kSmallPartVecs = 256 * 4;
 // candidates that a merge in 256 and in 1,024 threads has LDS for: 21 KB, which leaves
 // room for other rows beside it, and 74 KB (rows of k = 1,000 and longer lists)

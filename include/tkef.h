@@ -406,7 +406,8 @@ const char *tkef_lars_launch_name(int32_t dense, int32_t i);
 
 /* ========================================================================
  * Rows of logits over a vocabulary: a teacher's top logits as (idx, val)
- * lists, distillation on such lists, verification of drafted tokens
+ * lists, distillation on such lists, verification of drafted tokens, scores of
+ * given tokens
  *
  * A row is V consecutive logits x_0 .. x_{V-1} of one type (TKEF_DTYPE_*);
  * rows lie row_stride elements apart (row_stride >= V; what lies between
@@ -574,6 +575,113 @@ int tkef_verify_execute(tkef_verify_plan plan, const void *target, int64_t targe
                         const int32_t *length, int32_t *accepted, int32_t *tokens_out,
                         float *logp_out, void *ws, size_t ws_bytes, uint32_t *status,
                         hipStream_t stream);
+
+/* ---- scores of tokens -----------------------------------------------------
+ * For each row with a token t in [0, V):
+ *   LZ = log sum_i exp(s x_i),  p_i = exp(s x_i - LZ)
+ *   logp = s x_t - LZ,  entropy = -sum_i p_i log p_i  (terms with p = 0 are 0)
+ *   alternatives: the k words first in the order (x descending, word
+ *   ascending), in that order, with their s x_i - LZ
+ * (0 <= k <= min(V, TKEF_SCORE_MAX_K)), and the gradient of dlogp * logp + dentropy *
+ * entropy with respect to the logits,
+ *   s [dlogp (1{i = t} - p_i) - dentropy p_i (log p_i + entropy)].
+ * A row with token -1 has no token: it is not read, its results are 0, its
+ * alternatives words -1 with 0, its gradient 0. Another token outside [0, V)
+ * does the same and sets TKEF_STATUS_INDEX_RANGE. A row with a NaN or +inf
+ * logit, or whose logits are all -inf, has NaN for its results and gradient and words
+ * -1 with NaN for its alternatives, and sets TKEF_STATUS_NAN. A masked (-inf) token
+ * has logp -inf; so has a masked alternative, where a row has fewer words than k. */
+typedef struct tkef_score_plan_s *tkef_score_plan;
+
+#define TKEF_SCORE_MAX_K 64
+
+/* Host only. rows: the most rows an execution gives; k: alternatives, 0 for none. No
+ * workspace is needed while a row is at most 64 KB. Longer rows are taken in chunks, each
+ * of which leaves 16 bytes for 32 KB of a row, or 16 + 8 k bytes for 64 KB. */
+int tkef_score_plan_create(int64_t rows, int64_t vocab, int64_t k, int32_t dtype,
+                           double temperature, tkef_score_plan *plan_out);
+int tkef_score_plan_destroy(tkef_score_plan plan);
+int tkef_score_plan_info(tkef_score_plan plan, size_t *workspace_bytes);
+
+/* logits: device, `rows` rows of the plan's type. tokens: device int32, one per row.
+ * logp, entropy: device, rows binary32 values; entropy may be NULL. idx_out (int32),
+ * val_out (binary32): device, rows * k entries, or both NULL (no alternatives). stats:
+ * device, rows * 4 binary32 values that the backward pass takes (16-byte aligned; their
+ * layout is the library's), or NULL. */
+int tkef_score_forward(tkef_score_plan plan, const void *logits, int64_t row_stride, int64_t rows,
+                       const int32_t *tokens, float *logp, float *entropy, int32_t *idx_out,
+                       float *val_out, float *stats, void *ws, size_t ws_bytes, uint32_t *status,
+                       hipStream_t stream);
+
+/* Gradient of sum_rows dlogp * logp + dentropy * entropy with respect to the logits, in
+ * their type. dlogp, dentropy: device, one binary32 value per row; one of them may be
+ * NULL (0). A row where both are 0 is not read. logits, tokens: those of the forward
+ * pass, stats what it gave. grad: as in tkef_distill_backward. */
+int tkef_score_backward(tkef_score_plan plan, const void *logits, int64_t row_stride, int64_t rows,
+                        const int32_t *tokens, const float *stats, const float *dlogp,
+                        const float *dentropy, void *grad, int64_t grad_stride, uint32_t *status,
+                        hipStream_t stream);
+
+/* ========================================================================
+ * Embedding of tokens: scaled rows of a table, and the table's gradient, dense or
+ * as the list that a worker sends
+ *
+ * For a table of V rows of `width` elements and n tokens t_i in [0, V):
+ *   out_i = scale * table[t_i]
+ *   G_w   = scale * sum_{i: t_i = w} dout_i
+ * Sums are held in binary32, each word's in a fixed order, so a call's results are
+ * the same on every run; each result is rounded once to its type. A token -1 is
+ * padding: its row of out is 0, its row of dout is not read. Other tokens outside [0, V)
+ * do the same and set TKEF_STATUS_INDEX_RANGE. Table, out and dout, and gradient have
+ * types of their own (TKEF_DTYPE_*); rows lie strides apart (elements, >= width), what
+ * lies between them is neither read nor written.
+ *
+ * A plan holds sizes only, no buffers; a call may give fewer tokens than the plan
+ * was created for. Executions are asynchronous, only launch kernels and can be
+ * captured into a graph, with a workspace each where they may run at the same time.
+ * Limits: tokens, V <= 2^20; width <= 65536; scale finite as binary32.
+ * ====================================================================== */
+
+#define TKEF_EMBED_MAX_ROWS (1 << 20)
+#define TKEF_EMBED_MAX_WIDTH (1 << 16)
+
+typedef struct tkef_embed_plan_s *tkef_embed_plan;
+
+/* Host only. dtype: of the table; out_dtype: of out and dout; grad_dtype: of the dense
+ * gradient; val_format: of the list's values. The workspace (of the gradient; a lookup
+ * needs none) holds 8 bytes a token, 8 bytes a word, and 8 width bytes for each of at
+ * most 4,096 tiles of 8 or more tokens. */
+int tkef_embed_plan_create(int64_t rows, int64_t vocab, int64_t width, int32_t dtype,
+                           int32_t out_dtype, int32_t grad_dtype, int32_t val_format,
+                           double scale, tkef_embed_plan *plan_out);
+int tkef_embed_plan_destroy(tkef_embed_plan plan);
+int tkef_embed_plan_info(tkef_embed_plan plan, size_t *workspace_bytes);
+
+/* table: device, V rows; tokens: device int32, `rows` of them; out: device, `rows`
+ * rows, no part of the table. */
+int tkef_embed_forward(tkef_embed_plan plan, const void *table, int64_t table_stride,
+                       const int32_t *tokens, int64_t rows, void *out, int64_t out_stride,
+                       uint32_t *status, hipStream_t stream);
+
+/* The dense gradient, V rows: grad = G, or grad = add + G (add: device, V rows of the
+ * gradient's type, or NULL). With add == grad, at the same stride, only rows of words that
+ * occur are read and written; add and grad must not overlap otherwise, nor dout and grad.
+ * rows == 0: grad = 0, or add. */
+int tkef_embed_backward(tkef_embed_plan plan, const int32_t *tokens, int64_t rows,
+                        const void *dout, int64_t dout_stride, const void *add,
+                        int64_t add_stride, void *grad, int64_t grad_stride, void *ws,
+                        size_t ws_bytes, uint32_t *status, hipStream_t stream);
+
+/* The same gradient as one worker's list, in the layout that tkef_update_execute
+ * and its like take: for each word that occurs, ascending, `width` pairs of a global
+ * position offset + word * width + column (idx_out, int32) and a value (val_out); nnz_out:
+ * device int32, their number. idx_out, val_out: device, min(rows, V) * width entries; those
+ * behind nnz are left as they were. offset: the table's first position among the update's
+ * tensors; offset + V * width <= 2^31 - 1 (TKEF_ERANGE otherwise). */
+int tkef_embed_lists(tkef_embed_plan plan, const int32_t *tokens, int64_t rows, const void *dout,
+                     int64_t dout_stride, int64_t offset, int32_t *idx_out, void *val_out,
+                     int32_t *nnz_out, void *ws, size_t ws_bytes, uint32_t *status,
+                     hipStream_t stream);
 
 #ifdef __cplusplus
 }

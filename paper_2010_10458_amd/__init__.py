@@ -13,8 +13,9 @@ the library's HIP kernels. PyTorch supplies device memory and streams.
     up.bind(params, momentum)              # once
     up.execute(idx_all, val_all, lr=0.1, mu=0.9, wd=5e-5)
 
-Operators on rows of logits (TopLogitsPlan, DistillPlan, VerifyPlan and their
-one-shot calls) are in ``rows.py`` and exported here.
+Operators on rows of logits (TopLogitsPlan, DistillPlan, VerifyPlan, ScorePlan and their
+one-shot calls) are in ``rows.py``, the embedding of tokens (EmbedPlan) in ``embed.py``;
+both are exported here.
 """
 from __future__ import annotations
 
@@ -132,6 +133,21 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         "tkef_verify_plan_bind": ([vp, vp, sz, vp], ctypes.c_int),
         "tkef_verify_execute": ([vp, vp, i64, i64, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp,
                                  vp, vp, vp, sz, vp, vp], ctypes.c_int),
+        "tkef_score_plan_create": ([i64, i64, i64, i32, f64, P(vp)], ctypes.c_int),
+        "tkef_score_plan_destroy": ([vp], ctypes.c_int),
+        "tkef_score_plan_info": ([vp, P(sz)], ctypes.c_int),
+        "tkef_score_forward": ([vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp],
+                               ctypes.c_int),
+        "tkef_score_backward": ([vp, vp, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp],
+                                ctypes.c_int),
+        "tkef_embed_plan_create": ([i64, i64, i64, i32, i32, i32, i32, f64, P(vp)], ctypes.c_int),
+        "tkef_embed_plan_destroy": ([vp], ctypes.c_int),
+        "tkef_embed_plan_info": ([vp, P(sz)], ctypes.c_int),
+        "tkef_embed_forward": ([vp, vp, i64, vp, i64, vp, i64, vp, vp], ctypes.c_int),
+        "tkef_embed_backward": ([vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp, vp],
+                                ctypes.c_int),
+        "tkef_embed_lists": ([vp, vp, i64, vp, i64, i64, vp, vp, vp, vp, sz, vp, vp],
+                             ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -707,5 +723,8 @@ def sparse_aggregate(outs: Sequence[torch.Tensor], idx: torch.Tensor, val: torch
 
 
 from .rows import (DTYPE_BF16, DTYPE_F16, DTYPE_F32, ROWS_MAX_K, ROWS_MAX_ROWS,  # noqa: E402,F401
-                   ROWS_MAX_VOCAB, VERIFY_MAX_BATCH, VERIFY_MAX_DRAFT, DistillPlan, TopLogitsPlan,
-                   VerifyPlan, distill_step, top_logits, verify_draft)
+                   ROWS_MAX_VOCAB, SCORE_MAX_K, VERIFY_MAX_BATCH, VERIFY_MAX_DRAFT, DistillPlan,
+                   ScorePlan, TopLogitsPlan, VerifyPlan, distill_step, score_tokens, top_logits,
+                   verify_draft)
+from .embed import (EMBED_MAX_ROWS, EMBED_MAX_WIDTH, EmbedPlan, embed_gradient,  # noqa: E402,F401
+                    embed_lists, embed_tokens)

@@ -12,7 +12,8 @@ LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libtkef.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-SOURCES = ["tkef_kernels.hip", "tkef_api.cpp", "tkef_rows.hip", "tkef_rows_api.cpp"]
+SOURCES = ["tkef_kernels.hip", "tkef_api.cpp", "tkef_rows.hip", "tkef_rows_api.cpp",
+           "tkef_score.hip", "tkef_score_api.cpp", "tkef_embed.hip", "tkef_embed_api.cpp"]
 
 FLAGS = [
     "--offload-arch=gfx950",

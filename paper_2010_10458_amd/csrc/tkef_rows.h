@@ -1,5 +1,6 @@
 // Internal interface of the row operators (top logits, distillation, draft
-// verification): argument blocks the host fills and the gfx950 kernels read.
+// verification, scores of tokens): argument blocks the host fills and the gfx950
+// kernels read.
 #pragma once
 
 #include <stddef.h>
@@ -57,6 +58,24 @@ struct VerifyArgs {
   uint32_t* status;       // may be null
 };
 
+struct ScoreArgs {
+  const void* z;
+  int64_t ld, rows;
+  int32_t V, k, dtype;    // k: alternatives, 0: none asked for
+  float a, inv_t;
+  const int32_t* tokens;
+  float* logp;
+  float* entropy;         // may be null
+  int32_t* idx;
+  float* val;
+  float4* stats;          // forward: out (may be null); backward: in
+  const float* dlogp;     // backward; may be null
+  const float* dentropy;  // backward; may be null
+  void* grad;
+  int64_t gld;
+  uint32_t* status;       // may be null
+};
+
 // Bytes of ws that launch_top uses (0: rows short enough for one workgroup).
 size_t top_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype);
 hipError_t launch_top(const TopArgs& a, void* ws, hipStream_t s);
@@ -86,5 +105,12 @@ struct VerifyScratch {
   float2* parts;        // per sequence, place and chunk: the same of a chunk, as two pairs
 };
 hipError_t launch_verify(const VerifyArgs& a, const VerifyScratch& w, hipStream_t s);
+
+
+// Bytes of ws that launch_score_forward uses for calls with up to k alternatives
+// (0: rows short enough for one workgroup).
+size_t score_workspace(int64_t rows, int64_t V, int64_t k, int32_t dtype);
+hipError_t launch_score_forward(const ScoreArgs& a, void* ws, hipStream_t s);
+hipError_t launch_score_backward(const ScoreArgs& a, hipStream_t s);
 
 }  // namespace tkef

@@ -123,31 +123,6 @@ __device__ __forceinline__ void top_radix(const TopArgs& A, RadixLds& L, const T
   }
 }
 
-// A candidate: the distinct upper bits of its order key, then the complement of
-// its word, so that a larger candidate is selected first.
-constexpr int kWordBits = 20;
-static_assert(TKEF_ROWS_MAX_VOCAB <= 1 << kWordBits, "words of a candidate");
-__device__ __forceinline__ constexpr int key_shift(const float*) { return 0; }
-__device__ __forceinline__ constexpr int key_shift(const _Float16*) { return 13; }
-__device__ __forceinline__ constexpr int key_shift(const __bf16*) { return 16; }
-
-template <typename T>
-__device__ __forceinline__ uint64_t candidate(uint32_t key, int32_t word) {
-  const T* type = nullptr;
-  return ((uint64_t)(key >> key_shift(type)) << kWordBits) |
-         (uint32_t)((1 << kWordBits) - 1 - word);
-}
-__device__ __forceinline__ int32_t word_of(uint64_t c) {
-  return (1 << kWordBits) - 1 - (int32_t)((uint32_t)c & ((1u << kWordBits) - 1u));
-}
-template <typename T>
-__device__ __forceinline__ float value_of(uint64_t c) {
-  const T* type = nullptr;
-  uint32_t key = (uint32_t)(c >> kWordBits) << key_shift(type);
-  if (!(key >> 31)) key |= (1u << key_shift(type)) - 1u;  // (a negative value's key is inverted)
-  return key_value(key);
-}
-
 // the least candidate at or above an order key
 template <typename T>
 __device__ __forceinline__ uint64_t floor_of(uint32_t key) {
@@ -932,18 +907,6 @@ __device__ __forceinline__ int used_entries(const DistillArgs& A, int64_t row) {
   if (A.count == nullptr) return A.k;
   const int c = A.count[row];
   return c < 0 ? 0 : c < A.k ? c : A.k;
-}
-
-// Zeros over the vectors of chunk `chunk` of `chunks` of a row of grad (its own span: the
-// gradient's address decides the vectors), the first chunk with the extras.
-template <typename T, int TPB>
-__device__ __forceinline__ void zero_row(T* g, int V, int chunk, int chunks) {
-  const Span<T> s(g, V);
-  const int per = (s.nvec + chunks - 1) / chunks;
-  const int v0 = chunk * per, v1 = v0 + per < s.nvec ? v0 + per : s.nvec;
-  for (int v = v0 + (int)threadIdx.x; v < v1; v += TPB)
-    *reinterpret_cast<uint4*>(g + s.head + (int64_t)v * Span<T>::N) = make_uint4(0u, 0u, 0u, 0u);
-  if (chunk == 0 && (int)threadIdx.x < s.extras) g[s.extra((int)threadIdx.x)] = (T)0.f;
 }
 
 enum { kLoss = 0, kStep = 1, kPart = 2 };

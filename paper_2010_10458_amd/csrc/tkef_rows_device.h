@@ -58,6 +58,13 @@ __device__ __forceinline__ float load1(const T* p, int64_t i) {
   return (float)p[i];
 }
 
+// element i of rows of a type
+__device__ __forceinline__ float load1_of(const void* p, int dtype, int64_t i) {
+  return dtype == TKEF_DTYPE_F32   ? static_cast<const float*>(p)[i]
+         : dtype == TKEF_DTYPE_F16 ? (float)static_cast<const _Float16*>(p)[i]
+                                   : (float)static_cast<const __bf16*>(p)[i];
+}
+
 // value j of a list in the wire format (binary32 or binary16)
 __device__ __forceinline__ float load_val(const void* p, int format, int64_t j) {
   return format == TKEF_VAL_F16 ? (float)static_cast<const _Float16*>(p)[j]
@@ -378,6 +385,43 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
     x = o > x ? o : x;
   }
   return x;
+}
+
+// A candidate: the distinct upper bits of its order key, then the complement of
+// its word, so that a larger candidate is selected first.
+constexpr int kWordBits = 20;
+static_assert(TKEF_ROWS_MAX_VOCAB <= 1 << kWordBits, "words of a candidate");
+__device__ __forceinline__ constexpr int key_shift(const float*) { return 0; }
+__device__ __forceinline__ constexpr int key_shift(const _Float16*) { return 13; }
+__device__ __forceinline__ constexpr int key_shift(const __bf16*) { return 16; }
+
+template <typename T>
+__device__ __forceinline__ uint64_t candidate(uint32_t key, int32_t word) {
+  const T* type = nullptr;
+  return ((uint64_t)(key >> key_shift(type)) << kWordBits) |
+         (uint32_t)((1 << kWordBits) - 1 - word);
+}
+__device__ __forceinline__ int32_t word_of(uint64_t c) {
+  return (1 << kWordBits) - 1 - (int32_t)((uint32_t)c & ((1u << kWordBits) - 1u));
+}
+template <typename T>
+__device__ __forceinline__ float value_of(uint64_t c) {
+  const T* type = nullptr;
+  uint32_t key = (uint32_t)(c >> kWordBits) << key_shift(type);
+  if (!(key >> 31)) key |= (1u << key_shift(type)) - 1u;  // (a negative value's key is inverted)
+  return key_value(key);
+}
+
+// Zeros over the vectors of chunk `chunk` of `chunks` of a row of grad (its own span: the
+// gradient's address decides the vectors), the first chunk with the extras.
+template <typename T, int TPB>
+__device__ __forceinline__ void zero_row(T* g, int V, int chunk, int chunks) {
+  const Span<T> s(g, V);
+  const int per = (s.nvec + chunks - 1) / chunks;
+  const int v0 = chunk * per, v1 = v0 + per < s.nvec ? v0 + per : s.nvec;
+  for (int v = v0 + (int)threadIdx.x; v < v1; v += TPB)
+    *reinterpret_cast<uint4*>(g + s.head + (int64_t)v * Span<T>::N) = make_uint4(0u, 0u, 0u, 0u);
+  if (chunk == 0 && (int)threadIdx.x < s.extras) g[s.extra((int)threadIdx.x)] = (T)0.f;
 }
 
 // 16 bytes from any address of the element's alignment

@@ -48,22 +48,29 @@ inline int check_rows(const RowPlan& p, const void* z, int64_t ld, int64_t rows)
   return TKEF_OK;
 }
 
-// grad is the logits themselves or does not touch them: it lies before or after all of
-// their rows, or between them at their stride
+// Whether rows of `row` bytes, `step` apart, do not touch others: they lie before or
+// after all of them, or between them at their step.
+inline bool apart(const void* z, size_t row, size_t step, int64_t rows, const void* g, size_t grow,
+                  size_t gstep, int64_t grows) {
+  if (rows < 1 || grows < 1) return true;
+  const uintptr_t za = reinterpret_cast<uintptr_t>(z), ga = reinterpret_cast<uintptr_t>(g);
+  const uintptr_t ze = za + (size_t)(rows - 1) * step + row;
+  const uintptr_t ge = ga + (size_t)(grows - 1) * gstep + grow;
+  if (za >= ge || ga >= ze) return true;
+  if (gstep != step) return false;
+  // where a row of g begins behind the row of z before it
+  const size_t at = ga >= za ? (ga - za) % step : (step - (za - ga) % step) % step;
+  return at >= row && at + grow <= step;
+}
+
+// grad is the logits themselves or does not touch them
 inline int check_grad(const RowPlan& p, const void* z, int64_t ld, int64_t rows, const void* g,
                       int64_t gld) {
   if (gld > kMaxStride) return TKEF_ERANGE;
   if (g == nullptr || !aligned(g, elem_size(p.dtype)) || gld < p.vocab) return TKEF_EINVAL;
   if (g == z && gld == ld) return TKEF_OK;
-  const size_t e = elem_size(p.dtype), row = (size_t)p.vocab * e, step = (size_t)ld * e;
-  const uintptr_t za = reinterpret_cast<uintptr_t>(z), ga = reinterpret_cast<uintptr_t>(g);
-  const uintptr_t ze = za + (size_t)(rows - 1) * step + row;
-  const uintptr_t ge = ga + (size_t)(rows - 1) * (size_t)gld * e + row;
-  if (za >= ge || ga >= ze) return TKEF_OK;
-  if (gld != ld) return TKEF_EINVAL;
-  // where a row of grad begins behind the row of logits before it
-  const size_t at = ga >= za ? (ga - za) % step : (step - (za - ga) % step) % step;
-  return at >= row && at + row <= step ? TKEF_OK : TKEF_EINVAL;
+  const size_t e = elem_size(p.dtype), row = (size_t)p.vocab * e;
+  return apart(z, row, (size_t)ld * e, rows, g, row, (size_t)gld * e, rows) ? TKEF_OK : TKEF_EINVAL;
 }
 
 inline int done(hipError_t e) { return e == hipSuccess ? TKEF_OK : TKEF_EHIP; }

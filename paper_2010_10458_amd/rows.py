@@ -1,7 +1,8 @@
 """Operators on rows of logits over a vocabulary (include/tkef.h, "Rows of
 logits"): a teacher's top logits as (idx, val) lists, distillation on such
-lists, verification of drafted tokens. Like the rest of the package this module
-only marshals arguments; the computation runs in the library's HIP kernels.
+lists, verification of drafted tokens, scores of given tokens. Like the rest of the
+package this module only marshals arguments; the computation runs in the library's HIP
+kernels.
 
     top = TopLogitsPlan(rows, vocab, k, dtype=torch.bfloat16, temperature=2.0)
     idx, val, tail = top.execute(teacher_logits)
@@ -11,6 +12,11 @@ only marshals arguments; the computation runs in the library's HIP kernels.
 
     vp = VerifyPlan(batch, draft, vocab, dtype=torch.bfloat16)
     accepted, tokens, logp = vp.execute(target_logits, draft_logits, drafted, uniform, noise)
+
+    sp = ScorePlan(rows, vocab, k=5, dtype=torch.bfloat16)
+    logp, entropy, words, word_logp = sp.execute(logits, tokens)
+    logp, entropy, stats = sp.forward(logits, tokens)              # or .score() under autograd
+    grad = sp.backward(logits, tokens, stats, dlogp=dlogp, dentropy=dentropy)
 
 A call's tensors are all on one GPU, that of the stream it runs on (the current
 one, or the caller's `stream`).
@@ -33,6 +39,7 @@ from . import _check, _new_status, _raise_on_status, _val_format, lib
 DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
 ROWS_MAX_ROWS = ROWS_MAX_VOCAB = 1 << 20
 ROWS_MAX_K = 1024
+SCORE_MAX_K = 64
 VERIFY_MAX_DRAFT = 63
 VERIFY_MAX_BATCH = 32768
 
@@ -137,6 +144,14 @@ class _RowPlan:
         if vocab > 1 and x.stride(1) != 1:
             raise ValueError(f"{what}: the words of a row must be contiguous")
         return n, (x.stride(0) if n > 1 else vocab)
+
+    def _grad(self, logits, grad_out):
+        if grad_out is None:
+            grad_out = _out(None, tuple(logits.shape), self.dtype, logits.device, "grad_out")
+            return grad_out, self.vocab
+        elif grad_out.shape != logits.shape or grad_out.device != logits.device:
+            raise ValueError("grad_out: expected the shape and device of the logits")
+        return grad_out, self._logits(grad_out, "grad_out")[1]
 
     def _status_of(self, status, dev):
         if status is None:
@@ -250,14 +265,6 @@ class DistillPlan(_RowPlan):
         _check_vector(count, n, torch.int32, "count", gpu)
         _check_vector(weight, n, torch.float32, "weight", gpu)
         return (idx.data_ptr(), val.data_ptr(), _ptr(tail), _ptr(count), _ptr(weight))
-
-    def _grad(self, logits, grad_out):
-        if grad_out is None:
-            grad_out = _out(None, tuple(logits.shape), self.dtype, logits.device, "grad_out")
-            return grad_out, self.vocab
-        elif grad_out.shape != logits.shape or grad_out.device != logits.device:
-            raise ValueError("grad_out: expected the shape and device of the logits")
-        return grad_out, self._logits(grad_out, "grad_out")[1]
 
     def forward(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
                 tail: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
@@ -457,6 +464,141 @@ class VerifyPlan(_RowPlan):
 
 
 # ----------------------------------------------------------------------------
+class ScorePlan(_RowPlan):
+    """Scores of given tokens: each row's log-probability of its token, entropy,
+    and k greatest words in descending order (tkef_score_forward), and the gradient of the
+    first two (tkef_score_backward). tokens (n,) int32; a row with token -1 is not read, its
+    results and gradient are 0."""
+
+    _destroy = "tkef_score_plan_destroy"
+
+    def __init__(self, rows: int, vocab: int, k: int = 0, dtype=torch.bfloat16,
+                 temperature: float = 1.0, check: bool = False):
+        """rows: the most rows a call gives; k: alternatives that `execute` returns (0 to
+        SCORE_MAX_K)."""
+        super().__init__(rows, vocab, dtype, temperature, check)
+        self.k = int(k)
+        _check("tkef_score_plan_create", lib().tkef_score_plan_create(
+            self.rows, self.vocab, self.k, _dtype_code(dtype), self.temperature,
+            ctypes.byref(self._h)))
+        self._info("tkef_score_plan_info")
+        self._forward, self._backward = lib().tkef_score_forward, lib().tkef_score_backward
+
+    def execute(self, logits: torch.Tensor, tokens: torch.Tensor,
+                logp_out: Optional[torch.Tensor] = None,
+                entropy_out: Optional[torch.Tensor] = None,
+                idx_out: Optional[torch.Tensor] = None, val_out: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None, stream=None
+                ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+        """Returns logp (n,), entropy (n,), and the alternatives idx (n, k) int32 with
+        their log-probabilities val (n, k); values are float32."""
+        n, ld = self._logits(logits, "logits")
+        dev = logits.device
+        _check_vector(tokens, n, torch.int32, "tokens", dev.index)
+        h = _launch_on(dev.index, stream)
+        with _on(stream):
+            logp_out = _out(logp_out, (n,), torch.float32, dev, "logp_out")
+            entropy_out = _out(entropy_out, (n,), torch.float32, dev, "entropy_out")
+            idx_out = _out(idx_out, (n, self.k), torch.int32, dev, "idx_out")
+            val_out = _out(val_out, (n, self.k), torch.float32, dev, "val_out")
+            status, own = self._status_of(status, dev)
+            ws = self._workspace(h, dev)
+        rc = self._forward(
+            self._h, logits.data_ptr(), ld, n, tokens.data_ptr(), logp_out.data_ptr(),
+            entropy_out.data_ptr(), idx_out.data_ptr() if self.k else None,
+            val_out.data_ptr() if self.k else None, None, _ptr(ws), self.ws_bytes, _ptr(status), h)
+        if rc:
+            _check("tkef_score_forward", rc)
+        if own:
+            _raise_on_status("tkef_score_forward", status, stream)
+        return logp_out, entropy_out, idx_out, val_out
+
+    def forward(self, logits: torch.Tensor, tokens: torch.Tensor,
+                logp_out: Optional[torch.Tensor] = None,
+                entropy_out: Optional[torch.Tensor] = None,
+                stats_out: Optional[torch.Tensor] = None,
+                status: Optional[torch.Tensor] = None, stream=None
+                ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """Returns logp (n,) and entropy (n,) float32, and stats (n, 4) float32, which
+        backward takes. No alternatives are looked for, whatever the plan's k."""
+        n, ld = self._logits(logits, "logits")
+        dev = logits.device
+        _check_vector(tokens, n, torch.int32, "tokens", dev.index)
+        h = _launch_on(dev.index, stream)
+        with _on(stream):
+            logp_out = _out(logp_out, (n,), torch.float32, dev, "logp_out")
+            entropy_out = _out(entropy_out, (n,), torch.float32, dev, "entropy_out")
+            stats_out = _out(stats_out, (n, 4), torch.float32, dev, "stats_out")
+            status, own = self._status_of(status, dev)
+            ws = self._workspace(h, dev)
+        rc = self._forward(
+            self._h, logits.data_ptr(), ld, n, tokens.data_ptr(), logp_out.data_ptr(),
+            entropy_out.data_ptr(), None, None, stats_out.data_ptr(), _ptr(ws), self.ws_bytes,
+            _ptr(status), h)
+        if rc:
+            _check("tkef_score_forward", rc)
+        if own:
+            _raise_on_status("tkef_score_forward", status, stream)
+        return logp_out, entropy_out, stats_out
+
+    def backward(self, logits: torch.Tensor, tokens: torch.Tensor, stats: torch.Tensor,
+                 dlogp: Optional[torch.Tensor] = None, dentropy: Optional[torch.Tensor] = None,
+                 grad_out: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Gradient of sum(dlogp * logp + dentropy * entropy) in the logits' type (dlogp,
+        dentropy (n,) float32; one of them may be None, 0). grad_out may be the logits
+        themselves."""
+        n, ld = self._logits(logits, "logits")
+        dev = logits.device
+        if dlogp is None and dentropy is None:
+            raise ValueError("backward: expected dlogp or dentropy")
+        _check_vector(tokens, n, torch.int32, "tokens", dev.index)
+        _check_vector(stats, n * 4, torch.float32, "stats", dev.index)
+        _check_vector(dlogp, n, torch.float32, "dlogp", dev.index)
+        _check_vector(dentropy, n, torch.float32, "dentropy", dev.index)
+        h = _launch_on(dev.index, stream)
+        with _on(stream):
+            grad_out, gld = self._grad(logits, grad_out)
+            status, own = self._status_of(status, dev)
+        rc = self._backward(
+            self._h, logits.data_ptr(), ld, n, tokens.data_ptr(), stats.data_ptr(), _ptr(dlogp),
+            _ptr(dentropy), grad_out.data_ptr(), gld, _ptr(status), h)
+        if rc:
+            _check("tkef_score_backward", rc)
+        if own:
+            _raise_on_status("tkef_score_backward", status, stream)
+        return grad_out
+
+    def score(self, logits: torch.Tensor, tokens: torch.Tensor
+              ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """logp (n,) and entropy (n,) as outputs of a node of torch's autograd graph, whose
+        backward pass is `backward`. (A training step that is captured into a graph: torch
+        keeps a leaf's accumulation on the stream of the first graph that it is part of, so no
+        eager result of the same leaves may be alive when the backward pass is captured.)"""
+        return _Score.apply(logits, self, tokens)
+
+
+class _Score(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, plan, tokens):
+        logp, entropy, stats = plan.forward(logits, tokens)
+        ctx.plan = plan
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(logits, tokens, stats)
+        return logp, entropy
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dlogp, dentropy):
+        if dlogp is None and dentropy is None:
+            return None, None, None
+        logits, tokens, stats = ctx.saved_tensors
+        dlogp, dentropy = (d if d is None else d.to(torch.float32).contiguous()
+                           for d in (dlogp, dentropy))
+        return ctx.plan.backward(logits, tokens, stats, dlogp=dlogp, dentropy=dentropy), None, None
+
+
+# ----------------------------------------------------------------------------
 # one-shot calls: a plan, one execution, and TkefStatusError on any status bit
 # (they synchronize), unless the caller gives a status word to check itself
 
@@ -485,3 +627,11 @@ def verify_draft(target: torch.Tensor, drafts: torch.Tensor, tokens: torch.Tenso
     plan = VerifyPlan(max(1, target.shape[0]), drafts.shape[1], target.shape[2], target.dtype,
                       temperature, check=status is None)
     return plan.execute(target, drafts, tokens, uniform, noise, length=length, status=status)
+
+
+def score_tokens(logits: torch.Tensor, tokens: torch.Tensor, k: int = 0, temperature: float = 1.0,
+                 status: Optional[torch.Tensor] = None):
+    """(logp, entropy, idx, val) of each row: ScorePlan.execute."""
+    plan = ScorePlan(max(1, logits.shape[0]), logits.shape[1], k, logits.dtype, temperature,
+                     check=status is None)
+    return plan.execute(logits, tokens, status=status)

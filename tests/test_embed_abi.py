@@ -1,0 +1,208 @@
+"""Embedding of tokens on the CPU: sizes, arguments, overlaps, devices and workspaces are checked
+before any GPU work (no call here reaches the GPU), and the oracle's pins."""
+import ctypes
+import math
+import types
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2010_10458_amd as tk
+from oracle import score as oracle
+from test_rows_devices import OnGpu, current_gpu_is_the_first  # noqa: F401 (a fixture)
+
+VP = ctypes.c_void_p
+P = 1 << 24  # addresses that nothing dereferences
+Q = 1 << 28
+R = 1 << 30
+F32, F16, BF16 = tk.DTYPE_F32, tk.DTYPE_F16, tk.DTYPE_BF16
+
+
+def make(rows=64, vocab=100, width=16, dtype=F32, out=BF16, grad=F32, val=tk.VAL_F32, scale=1.0):
+    h = VP()
+    return tk.lib().tkef_embed_plan_create(rows, vocab, width, dtype, out, grad, val, scale,
+                                           ctypes.byref(h)), h
+
+
+def size(h):
+    ws = ctypes.c_size_t()
+    assert tk.lib().tkef_embed_plan_info(h, ctypes.byref(ws)) == tk.OK
+    return ws.value
+
+
+@pytest.mark.parametrize("change,code", [
+    ({}, tk.OK), (dict(rows=1, vocab=1, width=1), tk.OK),
+    (dict(rows=1 << 20, vocab=1 << 20, width=1 << 16), tk.OK), (dict(scale=-0.5), tk.OK),
+    (dict(scale=0.0), tk.OK), (dict(rows=0), tk.ERANGE), (dict(rows=(1 << 20) + 1), tk.ERANGE),
+    (dict(vocab=0), tk.ERANGE), (dict(vocab=(1 << 20) + 1), tk.ERANGE), (dict(width=0), tk.ERANGE),
+    (dict(width=(1 << 16) + 1), tk.ERANGE), (dict(scale=math.nan), tk.ERANGE),
+    (dict(scale=math.inf), tk.ERANGE), (dict(scale=1e39), tk.ERANGE), (dict(dtype=3), tk.EINVAL),
+    (dict(out=3), tk.EINVAL), (dict(grad=-1), tk.EINVAL), (dict(val=2), tk.EINVAL)])
+def test_plans(change, code):
+    rc, h = make(**change)
+    assert rc == code and bool(h.value) == (code == tk.OK)
+    if code == tk.OK:
+        assert size(h) % 256 == 0
+        assert tk.lib().tkef_embed_plan_destroy(h) == tk.OK
+
+
+def test_null_plans():
+    L = tk.lib()
+    assert L.tkef_embed_plan_destroy(None) == tk.EINVAL
+    assert L.tkef_embed_plan_info(None, None) == tk.EINVAL
+    assert L.tkef_embed_plan_create(1, 1, 1, 0, 0, 0, 0, 1.0, None) == tk.EINVAL
+    assert L.tkef_embed_forward(None, P, 16, P, 1, Q, 16, None, None) == tk.EINVAL
+    assert L.tkef_embed_backward(None, P, 1, P, 16, None, 0, Q, 16, R, 0, None, None) == tk.EINVAL
+    assert L.tkef_embed_lists(None, P, 1, P, 16, 0, Q, Q, Q, R, 0, None, None) == tk.EINVAL
+
+
+def test_forward_arguments():
+    L = tk.lib()
+    _, h = make()
+
+    def call(table=P, tld=16, tok=R, rows=64, out=Q, old=16, status=None):
+        return L.tkef_embed_forward(h, table, tld, tok, rows, out, old, status, None)
+
+    assert call(rows=0, table=None, tok=None, out=None) == tk.OK
+    assert call(rows=65) == tk.ERANGE and call(rows=-1) == tk.ERANGE
+    assert call(tld=1 << 41) == tk.ERANGE and call(old=1 << 41) == tk.ERANGE
+    for bad in (dict(table=None), dict(table=P + 2), dict(tld=15), dict(tok=None), dict(tok=R + 2),
+                dict(out=None), dict(out=Q + 1), dict(old=15), dict(status=R + 1),
+                dict(out=P), dict(out=P + 100 * 64 - 2), dict(out=P - 64 * 32 + 2),
+                dict(tld=64, old=128, out=P + 32)):      # in the table's columns, but for the last
+        assert call(**bad) == tk.EINVAL, bad
+    assert L.tkef_embed_plan_destroy(h) == tk.OK
+
+
+def test_backward_arguments():
+    L = tk.lib()
+    _, h = make()
+    need = size(h)
+
+    def call(tok=R, rows=64, dout=P, old=16, add=None, ald=0, grad=Q, gld=16, ws=R, n=need,
+             status=None):
+        return L.tkef_embed_backward(h, tok, rows, dout, old, add, ald, grad, gld, ws, n, status,
+                                     None)
+
+    assert call(rows=65) == tk.ERANGE and call(old=1 << 41) == tk.ERANGE
+    assert call(gld=1 << 41) == tk.ERANGE and call(add=P, ald=1 << 41) == tk.ERANGE
+    for bad in (dict(tok=None), dict(dout=None), dict(dout=P + 1), dict(old=15), dict(grad=None),
+                dict(grad=Q + 2), dict(gld=15), dict(add=P, ald=15), dict(add=P + 2, ald=16),
+                dict(tok=R + 1), dict(status=R + 2),
+                dict(grad=P), dict(grad=P + 64 * 32 - 4), dict(rows=0, grad=None),
+                dict(add=Q, ald=17), dict(add=Q + 64, ald=16), dict(add=Q - 64, ald=16)):
+        assert call(**bad) == tk.EINVAL, bad
+    for bad in (dict(ws=None), dict(n=need - 1), dict(ws=R + 128)):
+        assert call(**bad) == tk.EWORKSPACE
+    assert L.tkef_embed_plan_destroy(h) == tk.OK
+
+
+def test_lists_arguments():
+    L = tk.lib()
+    _, h = make(val=tk.VAL_F16)
+    need = size(h)
+
+    def call(tok=R, rows=64, dout=P, old=16, offset=0, idx=Q, val=Q, nnz=Q, ws=R, n=need,
+             status=None):
+        return L.tkef_embed_lists(h, tok, rows, dout, old, offset, idx, val, nnz, ws, n, status,
+                                  None)
+
+    top = 2 ** 31 - 1 - 1600
+    assert call(rows=65) == tk.ERANGE and call(offset=-1) == tk.ERANGE
+    assert call(offset=top + 1) == tk.ERANGE and call(offset=2 ** 62) == tk.ERANGE
+    for bad in (dict(tok=None), dict(dout=None), dict(old=15), dict(idx=None), dict(val=None),
+                dict(nnz=None), dict(idx=Q + 2), dict(val=Q + 1), dict(nnz=Q + 2),
+                dict(offset=top, idx=None), dict(rows=0, nnz=None)):
+        assert call(**bad) == tk.EINVAL, bad
+    assert call(ws=None) == tk.EWORKSPACE
+    assert L.tkef_embed_plan_destroy(h) == tk.OK
+    # positions of a table of 2^20 x 2^16 do not fit; its dense gradient does
+    _, h = make(vocab=1 << 20, width=1 << 16, rows=1)
+    need = size(h)
+    assert L.tkef_embed_lists(h, R, 1, P, 1 << 16, 0, Q, Q, Q, R, need, None, None) == tk.ERANGE
+    assert L.tkef_embed_plan_destroy(h) == tk.OK
+
+
+def test_stated_workspace():
+    for rows in (1, 8, 9, 4096, 32768, 32769, 100_000, 1 << 20):
+        for vocab, width in ((1, 1), (1000, 64), (32000, 512), (1 << 20, 5)):
+            _, h = make(rows=rows, vocab=vocab, width=width)
+            most = 8 * rows + 8 * vocab + 8 * width * min(4096, -(-rows // 8)) + vocab // 16 + 2048
+            assert 8 * rows <= size(h) <= most, (rows, vocab, width, size(h), most)
+            tk.lib().tkef_embed_plan_destroy(h)
+
+
+def call(which, gpu=0, stream=None, change=(), **other):
+    p = tk.EmbedPlan(6, 20, 8, dtype=torch.float32, out_dtype=torch.float16)
+    half, ints = torch.float16, torch.int32
+    kw = dict(tokens=((6,), ints))
+    if which == "forward":
+        kw.update(table=((20, 8), torch.float32), out=((6, 8), half))
+    else:
+        kw.update(dout=((6, 8), half))
+    if which == "backward":
+        kw.update(add=((20, 8), torch.float32), grad_out=((20, 8), torch.float32))
+    if which == "lists":
+        kw.update(idx_out=((48,), ints), val_out=((48,), torch.float32), nnz_out=((1,), ints))
+    kw.update(change)
+    return getattr(p, which)(stream=stream, **{k: OnGpu(s, t, other.get(k, gpu))
+                                               for k, (s, t) in kw.items()})
+
+
+@pytest.mark.parametrize("which", ["forward", "backward", "lists"])
+def test_devices(which):
+    with pytest.raises(ValueError, match="cuda:1.*stream is on cuda:0"):
+        call(which, gpu=1)
+    with pytest.raises(ValueError, match="cuda:0.*stream is on cuda:1"):
+        call(which, stream=types.SimpleNamespace(device_index=1, cuda_stream=0))
+    names = dict(forward=("tokens", "out"), backward=("tokens", "add", "grad_out"),
+                 lists=("tokens", "idx_out", "val_out", "nnz_out"))[which]
+    for name in names:
+        with pytest.raises(ValueError, match=name):
+            call(which, **{name: 1})
+
+
+@pytest.mark.parametrize("which,name,bad", [
+    ("forward", "tokens", ((7,), torch.int32)), ("forward", "tokens", ((6,), torch.int64)),
+    ("forward", "table", ((21, 8), torch.float32)), ("forward", "table", ((20, 8), torch.float16)),
+    ("forward", "out", ((5, 8), torch.float16)), ("forward", "out", ((6, 8), torch.float32)),
+    ("backward", "dout", ((6, 9), torch.float16)), ("backward", "dout", ((6, 8), torch.float32)),
+    ("backward", "add", ((19, 8), torch.float32)), ("backward", "grad_out", ((20, 8), torch.float16)),
+    ("lists", "dout", ((48,), torch.float16)), ("lists", "idx_out", ((47,), torch.int32)),
+    ("lists", "idx_out", ((48,), torch.int64)), ("lists", "val_out", ((47,), torch.float32)),
+    ("lists", "val_out", ((48,), torch.float16)), ("lists", "nnz_out", ((2,), torch.int32))])
+def test_tensors_of_other_types_and_shapes(which, name, bad):
+    with pytest.raises(ValueError, match=name):
+        call(which, change={name: bad})
+
+
+def test_host_tensors_and_types_of_a_node():
+    p = tk.EmbedPlan(6, 20, 8, dtype=torch.float16, grad_dtype=torch.float32)
+    with pytest.raises(ValueError, match="table"):
+        p.forward(torch.zeros(20, 8, dtype=torch.float16), torch.zeros(6, dtype=torch.int32))
+    with pytest.raises(ValueError, match="type"):
+        p.lookup(OnGpu((20, 8), torch.float16), OnGpu((6,), torch.int32))
+    with pytest.raises(ValueError):
+        tk.EmbedPlan(6, 20, 8, dtype=torch.float64)
+    with pytest.raises(ValueError):
+        tk.EmbedPlan(6, 20, 8, val_dtype=torch.bfloat16)
+
+
+def test_captured_calls_share_no_scratch(monkeypatch):
+    state = [False]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state[0])
+    plan = tk.EmbedPlan(64, 1000, 32)
+    eager = plan._workspace(7, "cpu")
+    assert plan._workspace(7, "cpu") is eager
+    state[0] = True
+    first, second = plan._workspace(7, "cpu"), plan._workspace(7, "cpu")
+    assert len({w.data_ptr() for w in (eager, first, second)}) == 3
+
+
+def test_oracle_pins():
+    dout = np.array([[1.0, 2.0], [3.0, -4.0], [5.0, 6.0], [7.0, 8.0]])
+    g, a, c = oracle.embed_sums([2, 0, 2, -1], dout, 3, 0.5)
+    assert g.tolist() == [[1.5, -2.0], [0.0, 0.0], [3.0, 4.0]]
+    assert a.tolist() == [[1.5, 2.0], [0.0, 0.0], [3.0, 4.0]]
+    assert c.tolist() == [1, 0, 2]

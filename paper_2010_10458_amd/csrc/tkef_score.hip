@@ -1,6 +1,8 @@
 // gfx950 kernels for scores of given tokens: log-probability, the row's entropy,
 // its greatest words in descending order, and the gradient of the first two.
 // Exponentials, sums and vectors of rows: tkef_rows_device.h.
+#include <type_traits>
+
 #include <hip/hip_runtime.h>
 
 #include "tkef.h"
@@ -148,6 +150,161 @@ __device__ __forceinline__ void extract(const Share<T, TPB, NV>& mine, int k, ui
   }
 }
 
+// LDS of a selection. kVecs vectors of 16 bytes, kCand candidates: the words of a row with
+// fewer than TKEF_SCORE_MAX_K vectors fit (63 of eight, and 14 extras).
+constexpr int kVecs = 192, kCand = 576;
+struct SelectLds {
+  alignas(16) uint4 vec[kVecs];
+  alignas(16) uint64_t cand[kCand + 8];
+  int32_t word[kVecs];
+  uint32_t group[256];
+  uint32_t bound, vecs, count, scan[4];
+  uint64_t top[2][4];
+};
+
+struct Nothing {};
+template <bool ALT>
+using Maybe = std::conditional_t<ALT, SelectLds, Nothing>;
+
+// The k first words of a workgroup's share, which its threads hold in registers (r: vectors v0
+// + i * 256 + tid; m: their greatest), in descending order, zeros behind them where there are
+// fewer.
+//   1. The k-th greatest of the threads' own greatest words, bisected on order keys by one wave,
+//      is at most the k-th greatest word, and few others reach it (of 32,000 words, k = 20:
+//      some 21).
+//   2. Vectors that have a word which does go to LDS, and their words that do become candidates.
+//   3. A candidate's place is the number of better ones.
+// Where more reach the bound than LDS holds, they mostly do so by ties (rows with fewer
+// unmasked words than k, constant rows): the words above it are the candidates then, and the
+// lowest at it fill up. Where even those are too many (the greatest words in few threads'
+// shares), they are taken one after the other.
+template <typename T, int NV>
+__device__ __forceinline__ void select(uint4 (&r)[NV], float m, const Share<T, 256, NV>& mine, int k,
+                                       uint64_t* picked, SelectLds& L) {
+  constexpr int N = Span<T>::N, TPB = 256;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const T* type = nullptr;
+  const Span<T>& s = mine.s;
+  L.group[tid] = order_key(m);
+  if (tid < k) picked[tid] = 0ull;
+  if (tid == 0) L.vecs = L.count = 0u;
+  __syncthreads();
+  if (tid < 64) {
+    uint32_t g[4], lo = 0xFFFFFFFFu, hi = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      g[i] = L.group[i * 64 + lane];
+      lo = g[i] < lo ? g[i] : lo;
+      hi = g[i] > hi ? g[i] : hi;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      const uint32_t a = __shfl_xor(lo, d), b = __shfl_xor(hi, d);
+      lo = a < lo ? a : lo;
+      hi = b > hi ? b : hi;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi) + 1u;
+    // at least k keys are >= lo, fewer than k are >= hi
+    const uint32_t least = 1u << key_shift(type), enough = (uint32_t)k + ((uint32_t)k >> 3) + 1u;
+    while (hi - lo > least) {
+      const uint32_t mid = lo + (hi - lo) / 2u;
+      uint32_t c = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c += (uint32_t)__popcll(__ballot(g[i] >= mid));
+      if (c >= (uint32_t)k) {
+        lo = mid;
+        if (c <= enough) break;
+      } else {
+        hi = mid;
+      }
+    }
+    // the least key at or above lo that a value of the type has: ties lie at the bound
+    lo = (lo >> 31) ? (lo + least - 1u) & ~(least - 1u) : lo | (least - 1u);
+    if (lane == 0) L.bound = lo;
+  }
+  __syncthreads();
+  const float bound = key_value(L.bound);
+  // words that reach the bound, or lie above it
+  const auto collect = [&](bool strict) {
+    const auto reaches = [&](float x) { return strict ? x > bound : x >= bound; };
+    const auto put = [&](float x, int32_t word) {
+      const uint32_t at = atomicAdd(&L.count, 1u);
+      if (at < (uint32_t)kCand) L.cand[at] = candidate<T>(order_key(x), word);
+    };
+    const int tid2 = renew(tid);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = mine.v0 + i * TPB + tid2;
+      renew(r[i]);
+      const bool above = reaches(max_packed(-kInf, r[i], type)) && v < s.nvec;
+      const uint64_t who = __ballot(above);
+      if (who == 0ull) continue;
+      uint32_t at = 0u;
+      if (lane == 0) at = atomicAdd(&L.vecs, (uint32_t)__popcll(who));
+      at = __builtin_amdgcn_readfirstlane(at) +
+           __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32),
+                                     __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+      if (above && at < (uint32_t)kVecs) {
+        L.vec[at] = r[i];
+        L.word[at] = s.head + v * N;
+      }
+    }
+    if (mine.has_ex && reaches(mine.ex)) put(mine.ex, s.extra(tid));
+    __syncthreads();
+    const uint32_t vecs = L.vecs;
+    if (vecs <= (uint32_t)kVecs)
+      for (int e = tid; e < (int)vecs * N; e += TPB) {
+        const float x = (float)reinterpret_cast<const T*>(&L.vec[e / N])[e % N];
+        if (reaches(x)) put(x, L.word[e / N] + e % N);
+      }
+    __syncthreads();
+    return vecs <= (uint32_t)kVecs && L.count <= (uint32_t)kCand ? (int)L.count : -1;
+  };
+  int C = collect(false);
+  if (C < 0) {  // (the same for the whole workgroup, as all that is decided here)
+    __syncthreads();
+    if (tid == 0) L.vecs = L.count = 0u;
+    __syncthreads();
+    C = collect(true);
+    if (C < 0) {
+      extract<T, TPB, NV>(mine, k, picked, L.top);
+      return;
+    }
+    // the lowest words at the bound, in rounds over the share in ascending order
+    const int wanted = C < k ? k - C : 0;
+    int done = 0;
+    const auto round = [&](bool valid, int32_t word) {
+      const bool tie = valid && load1(s.p, word) == bound;
+      uint32_t total;
+      const int at = done + (int)block_scan<TPB>(tie ? 1u : 0u, L.scan, &total);
+      if (tie && at < wanted) L.cand[C + at] = candidate<T>(L.bound, word);
+      done += (int)total;
+    };
+    const bool edges = mine.v0 == 0;
+    const int end = s.nvec - mine.v0 < TPB * NV ? s.nvec - mine.v0 : TPB * NV;
+    const int32_t first = s.head + mine.v0 * N, behind = s.head + s.nvec * N;
+    if (edges && wanted > 0) round(tid < s.head, tid);
+    for (int i = 0; i < end * N && done < wanted; i += TPB) round(i + tid < end * N, first + i + tid);
+    if (edges && done < wanted) round(behind + tid < (int)(s.extras - s.head) + behind, behind + tid);
+    C += done < wanted ? done : wanted;
+  }
+  if (tid < 8) L.cand[C + tid] = 0ull;
+  __syncthreads();
+  for (int q = tid; q < C; q += TPB) {
+    const uint64_t c = L.cand[q];
+    int rank = 0;
+    for (int j = 0; j < C; j += 8) {  // (zeros follow; all reads before the first use)
+      ulonglong2 o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] = *reinterpret_cast<const ulonglong2*>(&L.cand[j + 2 * u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) rank += (o[u].x > c ? 1 : 0) + (o[u].y > c ? 1 : 0);
+    }
+    if (rank < k) picked[rank] = c;
+  }
+}
+
 // One workgroup takes a row, or one of a row's chunks (PART, blockIdx.y), and holds it
 // in registers: NV vectors a thread, loaded once.
 template <typename T, int TPB, int NV, bool ALT, bool PART>
@@ -155,7 +312,7 @@ __global__ __launch_bounds__(TPB) void k_score_row(ScoreArgs A, ScorePart* parts
   constexpr int N = Span<T>::N, NW = TPB / 64;
   __shared__ ScorePart red[NW];
   __shared__ uint64_t picked[ALT ? TKEF_SCORE_MAX_K : 1];
-  __shared__ uint64_t top[2][NW];
+  __shared__ Maybe<ALT> L;
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x;
   const int32_t token = A.tokens[row];
@@ -227,7 +384,7 @@ __global__ __launch_bounds__(TPB) void k_score_row(ScoreArgs A, ScorePart* parts
   if constexpr (ALT) {
     if (!(part.S != part.S)) {
       const Share<T, TPB, NV> mine = {s, v0, tid, has_ex, ex};
-      extract<T, TPB, NV>(mine, A.k, picked, top);
+      select<T, NV>(r, m, mine, A.k, picked, L);
     }
     __syncthreads();
   }

@@ -3,6 +3,8 @@
 // tokens stay in their order), the sorted ones are summed in tiles, and the sums of words
 // that cross tiles are joined in their order. Nothing is added atomically: the same
 // call gives the same bits.
+#include <type_traits>
+
 #include <hip/hip_runtime.h>
 
 #include "tkef.h"
@@ -58,28 +60,7 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[E]) {
     const float y[8] = {x[0], x[1], x[2], x[3], 0.f, 0.f, 0.f, 0.f};
     const uint4 u = pack(y, static_cast<const T*>(nullptr));
     const loose2_ v = {u.x, u.y};
-    *reinterpret_cast<loose2_*>(p) = v;
-  }
-}
-
-// `ne` of E elements; whole vectors where they are all there
-template <typename T, int E>
-__device__ __forceinline__ void load_some(const T* p, int ne, float (&x)[E]) {
-  if (ne == E) {
-    load_vec<T, E>(p, x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = i < ne ? (float)p[i] : 0.f;
-  }
-}
-template <typename T, int E>
-__device__ __forceinline__ void store_some(T* p, int ne, const float (&x)[E]) {
-  if (ne == E) {
-    store_vec<T, E>(p, x);
-  } else {
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (i < ne) p[i] = (T)x[i];
+    __builtin_nontemporal_store(v, reinterpret_cast<loose2_*>(p));
   }
 }
 
@@ -90,9 +71,12 @@ constexpr int vector_of() {
 }
 
 // A workgroup of 256 threads holds 256 >> lg groups of 1 << lg threads; a group has a row
-// (or a tile), thread l of it the columns (slice << lg + l) E ...
+// (or a tile), thread l of it the columns from (slice << lg + l) E on. The last vector of a row
+// whose width is no multiple of E lies back over its neighbour's columns, so that it is whole;
+// its thread writes the last `have` of its columns, from `skip` on. (Rows shorter than a
+// vector: skip == 0, have < E.)
 struct Columns {
-  int group, c0, ne;
+  int group, c0, skip, have;
   template <int E>
   __device__ static Columns of(int lg, int width) {
     Columns c;
@@ -100,10 +84,36 @@ struct Columns {
     c.group = tid >> lg;
     c.c0 = (((int)blockIdx.y << lg) + l) * E;
     const int left = width - c.c0;
-    c.ne = left < 0 ? 0 : left < E ? left : E;
+    c.skip = 0;
+    c.have = left < 0 ? 0 : left < E ? left : E;
+    if (left > 0 && left < E && width >= E) {
+      c.skip = E - left;
+      c.c0 = width - E;
+    }
     return c;
   }
+  __device__ bool none() const { return have == 0; }
 };
+
+template <typename T, int E>
+__device__ __forceinline__ void load_row(const T* row, const Columns& c, float (&x)[E]) {
+  if (c.skip + c.have == E) {
+    load_vec<T, E>(row + c.c0, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = i < c.have ? (float)row[i] : 0.f;
+  }
+}
+template <typename T, int E>
+__device__ __forceinline__ void store_row(T* row, const Columns& c, const float (&x)[E]) {
+  if (c.have == E) {
+    store_vec<T, E>(row + c.c0, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (i >= c.skip && i < c.skip + c.have) row[c.c0 + i] = (T)x[i];
+  }
+}
 
 // ----------------------------------------------------------------------------
 // lookup
@@ -128,18 +138,72 @@ __global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs A, int lg) {
     if (!in && word[r] != -1) bits = TKEF_STATUS_INDEX_RANGE;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[r][e] = 0.f;
-    if (in && c.ne > 0) {
-      load_some<T, E>(table + word[r] * A.table_ld + c.c0, c.ne, x[r]);
+    if (in && !c.none()) {
+      load_row<T, E>(table + word[r] * A.table_ld, c, x[r]);
 #pragma unroll
       for (int e = 0; e < E; ++e) x[r][e] *= A.scale;
     }
   }
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if (i0 + r >= A.n || c.ne == 0) continue;
-    store_some<O, E>(out + (i0 + r) * A.out_ld + c.c0, c.ne, x[r]);
-  }
+  for (int r = 0; r < R; ++r)
+    if (i0 + r < A.n && !c.none()) store_row<O, E>(out + (i0 + r) * A.out_ld, c, x[r]);
   raise_status(A.status, c.c0 == 0 ? bits : 0u);
+}
+
+// ----------------------------------------------------------------------------
+// rows of words without tokens
+
+constexpr int kRestRows = 2;  // rows of a group under way
+
+// The rows w0 + absent[0 .. count) of the gradient: zeros, or the added rows as they are
+// (U: their bits). A group of 1 << lg threads has a row, the slices from `slice` on.
+template <typename U>
+__device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* absent, int count,
+                                         int64_t w0, int lg, int slice, int step) {
+  constexpr int E = 16 / (int)sizeof(U);
+  const int tid = (int)threadIdx.x, groups = (int)blockDim.x >> lg;
+  U* grad = static_cast<U*>(A.grad);
+  const U* add = static_cast<const U*>(A.add);
+  if (A.width < E) {
+    for (int r = tid; r < count; r += (int)blockDim.x)
+      for (int e = 0; e < A.width; ++e) {
+        const int64_t w = w0 + absent[r];
+        grad[w * A.grad_ld + e] = add != nullptr ? add[w * A.add_ld + e] : (U)0;
+      }
+    return;
+  }
+  for (;; slice += step) {
+    int c0 = ((slice << lg) + (tid & ((1 << lg) - 1))) * E;
+    if (c0 >= A.width) break;
+    // (the last vector lies over its neighbour's columns: both write the same)
+    c0 = c0 + E < A.width ? c0 : A.width - E;
+    for (int r = tid >> lg; r < count; r += groups * kRestRows) {
+      loose4_ x[kRestRows];
+      int64_t w[kRestRows];
+#pragma unroll
+      for (int j = 0; j < kRestRows; ++j) {
+        const int at = r + j * groups;
+        w[j] = w0 + absent[at < count ? at : r];
+        x[j] = loose4_{0u, 0u, 0u, 0u};
+        if (add != nullptr)
+          x[j] = __builtin_nontemporal_load(
+              reinterpret_cast<const loose4_*>(add + w[j] * A.add_ld + c0));
+      }
+#pragma unroll
+      for (int j = 0; j < kRestRows; ++j)
+        if (r + j * groups < count)
+          __builtin_nontemporal_store(x[j],
+                                      reinterpret_cast<loose4_*>(grad + w[j] * A.grad_ld + c0));
+    }
+  }
+}
+
+__device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* absent, int count,
+                                         int64_t w0, int lg, int slice, int step) {
+  if (A.grad_dtype == TKEF_DTYPE_F32)
+    put_rest<uint32_t>(A, absent, count, w0, lg, slice, step);
+  else
+    put_rest<uint16_t>(A, absent, count, w0, lg, slice, step);
 }
 
 // ----------------------------------------------------------------------------
@@ -151,23 +215,27 @@ struct Token {
 
 struct EmbedScratch {
   Token* sorted;    // the batch's tokens that are words, by word, then by place
+  int32_t* slots;   // of each of them: its word's number among its bin's words that occur
   int32_t* first;   // V + 1: each word's first place in `sorted`
-  int32_t* slot;    // V: number of a word among its bin's words that occur
-  int32_t* bins;    // per bin: words that occur; then of all bins before it
+  int32_t* bins;    // per bin: words that occur
+  int32_t* before;  // per bin: words that occur in the bins before it
   float* partial;   // per tile: sums of the word that began before it, of the one that goes on
 };
 
-constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
-constexpr int kMaxBinBits = 10;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kSortAhead = 8;  // tokens a lane reads at once
+constexpr int kMaxBinBits = 9;
 
 // Lanes of the wave whose word (lgw bits) is the lane's own, among the lanes of `who`.
 __device__ __forceinline__ uint64_t same_word(uint32_t word, int lgw, uint64_t who) {
   uint64_t same = who;
-  for (int b = 0; b < lgw; ++b) {
-    const bool one = (word >> b) & 1u;
-    const uint64_t with = __ballot(one);
-    same &= one ? with : ~with;
-  }
+#pragma unroll
+  for (int b = 0; b < kMaxBinBits; ++b)
+    if (b < lgw) {
+      const bool one = (word >> b) & 1u;
+      const uint64_t with = __ballot(one);
+      same &= one ? with : ~with;
+    }
   return same;
 }
 
@@ -184,238 +252,377 @@ __device__ __forceinline__ void wave_fence() {
 
 // Workgroup b sorts the tokens of the words [b << lgw, (b + 1) << lgw): it reads all
 // tokens, counts those of lower words (they come before) and its own word by word, and
-// in a second reading puts its own in place. Wave w has the w-th share of the batch, so
+// in a second reading puts its own in place; between them it writes the gradient's rows of
+// words that do not occur (rest_lg >= 0). Wave w has the w-th share of the batch, so
 // a word's tokens are in the batch's order: waves in turn, and in a wave, lanes.
-__global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs A, EmbedScratch W, int lgw) {
+__global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, EmbedScratch W,
+                                                               int lgw, int rest_lg) {
   extern __shared__ uint32_t hist[];  // wave x word
   __shared__ uint32_t red[kSortWaves], below_of[kSortWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ uint32_t slot_of[1 << kMaxBinBits];
+  __shared__ uint16_t absent[1 << kMaxBinBits];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int words = 1 << lgw;
   const int32_t w0 = (int32_t)blockIdx.x << lgw;
+  const int n = (int)A.n;
+  const int per = ((n + kSortThreads - 1) / kSortThreads) * 64;
+  const int begin = wave * per, end = begin + per < n ? begin + per : n;
+  int32_t t[kSortAhead];
+  const auto read = [&](int from) {
+#pragma unroll
+    for (int j = 0; j < kSortAhead; ++j) {
+      const int i = from + j * 64 + lane;
+      t[j] = i < end ? A.tokens[i] : -1;
+    }
+  };
+  read(begin);
   for (int i = tid; i < words * kSortWaves; i += kSortThreads) hist[i] = 0u;
   __syncthreads();
-  const int n = (int)A.n;
-  const int per = ((n + kSortWaves * 64 - 1) / (kSortWaves * 64)) * 64;
-  const int begin = wave * per, end = begin + per < n ? begin + per : n;
   uint32_t* mine = hist + wave * words;
   uint32_t below = 0u, bits = 0u;
-  for (int i = begin + lane; i < end; i += 64) {
-    const int32_t t = A.tokens[i];
-    const bool in = t >= 0 && t < A.V;
-    if (!in && t != -1) bits = TKEF_STATUS_INDEX_RANGE;
-    below += in && t < w0 ? 1u : 0u;
-    if (in && t >= w0 && t - w0 < words) atomicAdd(&mine[t - w0], 1u);
+  for (int from = begin;;) {
+#pragma unroll
+    for (int j = 0; j < kSortAhead; ++j) {
+      const bool in = t[j] >= 0 && t[j] < A.V;
+      if (!in && t[j] != -1) bits = TKEF_STATUS_INDEX_RANGE;
+      below += in && t[j] < w0 ? 1u : 0u;
+      if (in && t[j] >= w0 && t[j] - w0 < words) atomicAdd(&mine[t[j] - w0], 1u);
+    }
+    from += kSortAhead * 64;
+    if (from >= end) break;
+    read(from);
   }
   if (blockIdx.x == 0) raise_status(A.status, bits);
+  if (per > kSortAhead * 64) read(begin);
   below = wave_incl(below);
   if (lane == 63) below_of[wave] = below;
   __syncthreads();
   uint32_t at = 0u;
 #pragma unroll
   for (int w = 0; w < kSortWaves; ++w) at += below_of[w];
-  // places of each word, and of each wave's share of it
-  uint32_t occur = 0u;
-  for (int base = 0; base < words; base += kSortThreads) {
-    const int w = base + tid;
-    uint32_t count = 0u;
-    if (w < words)
-      for (int v = 0; v < kSortWaves; ++v) count += hist[v * words + w];
-    uint32_t total, there;
-    const uint32_t before = block_scan<kSortThreads>(count, red, &total);
-    const uint32_t number = block_scan<kSortThreads>(count > 0u ? 1u : 0u, red, &there);
-    if (w < words) {
-      uint32_t place = at + before;
-      if (w0 + w < A.V) {
-        W.first[w0 + w] = (int32_t)place;
-        W.slot[w0 + w] = (int32_t)(occur + number);
-        if (w0 + w == A.V - 1) W.first[A.V] = (int32_t)(place + count);
-      }
-      for (int v = 0; v < kSortWaves; ++v) {
-        const uint32_t c = hist[v * words + w];
-        hist[v * words + w] = place;
-        place += c;
-      }
+  // places of each word, and of each wave's share of it; both counts in one scan (at most
+  // 2^20 tokens, 2^9 words)
+  uint32_t count = 0u, all;
+  if (tid < words)
+    for (int v = 0; v < kSortWaves; ++v) count += hist[v * words + tid];
+  const uint32_t ahead = block_scan<kSortThreads>(count | (count > 0u ? 1u << 21 : 0u), red, &all);
+  if (tid < words) {
+    uint32_t place = at + (ahead & ((1u << 21) - 1u));
+    if (w0 + tid < A.V) {
+      W.first[w0 + tid] = (int32_t)place;
+      if (w0 + tid == A.V - 1) W.first[A.V] = (int32_t)(place + count);
     }
-    at += total;
-    occur += there;
+    slot_of[tid] = ahead >> 21;
+    if (count == 0u) absent[tid - (int)(ahead >> 21)] = (uint16_t)tid;
+    for (int v = 0; v < kSortWaves; ++v) {
+      const uint32_t c = hist[v * words + tid];
+      hist[v * words + tid] = place;
+      place += c;
+    }
   }
-  if (tid == 0) W.bins[blockIdx.x] = (int32_t)occur;
+  if (tid == 0) W.bins[blockIdx.x] = (int32_t)(all >> 21);
   __syncthreads();
-  for (int i0 = begin; i0 < end; i0 += 64) {
-    const int i = i0 + lane;
-    const int32_t t = i < end ? A.tokens[i] : -1;
-    const bool own = t >= w0 && t < A.V && t - w0 < words;
-    const uint64_t who = __ballot(own);
-    if (who == 0ull) continue;
-    const uint32_t word = own ? (uint32_t)(t - w0) : 0u;
-    const uint64_t same = same_word(word, lgw, who);
-    const int rank = lanes_below(same);
-    const uint32_t place = mine[word] + (uint32_t)rank;
-    wave_fence();  // every lane has read before one writes, and before the next 64 read
-    if (own) {
-      W.sorted[place] = Token{i, t};
-      if (rank == 0) mine[word] = place + (uint32_t)__popcll(same);
+  if (rest_lg >= 0) {
+    const int there = A.V - w0 < words ? A.V - w0 : words;
+    put_rest(A, absent, there - (int)(all >> 21), w0, rest_lg, 0, 1);
+  }
+  for (int from = begin;;) {
+#pragma unroll
+    for (int j = 0; j < kSortAhead; ++j) {
+      const bool own = t[j] >= w0 && t[j] < A.V && t[j] - w0 < words;
+      const uint64_t who = __ballot(own);
+      if (who == 0ull) continue;
+      const uint32_t word = own ? (uint32_t)(t[j] - w0) : 0u;
+      const uint64_t same = same_word(word, lgw, who);
+      const int rank = lanes_below(same);
+      const uint32_t place = mine[word] + (uint32_t)rank;
+      wave_fence();  // every lane has read before one writes, and before the next 64 read
+      if (own) {
+        W.sorted[place] = Token{from + j * 64 + lane, t[j]};
+        if (A.idx != nullptr) W.slots[place] = (int32_t)slot_of[word];
+        if (rank == 0) mine[word] = place + (uint32_t)__popcll(same);
+      }
+      wave_fence();
     }
-    wave_fence();
+    from += kSortAhead * 64;
+    if (from >= end) break;
+    read(from);
   }
-}
-
-// Words that occur in the bins before each bin, and the lists' length.
-__global__ __launch_bounds__(1024) void k_embed_bins(EmbedArgs A, EmbedScratch W, int bins) {
-  __shared__ uint32_t red[16];
-  uint32_t done = 0u;
-  for (int base = 0; base < bins; base += 1024) {
-    const int b = base + (int)threadIdx.x;
-    uint32_t total;
-    const uint32_t before = block_scan<1024>(b < bins ? (uint32_t)W.bins[b] : 0u, red, &total);
-    if (b < bins) W.bins[b] = (int32_t)(done + before);
-    done += total;
-  }
-  if (threadIdx.x == 0) *A.nnz = (int32_t)(done * (uint32_t)A.width);
 }
 
 // ----------------------------------------------------------------------------
 // sums
 
-// Where a word's sum goes: a row of the gradient (with another gradient's added), or a
-// piece of the lists.
-template <int E>
-__device__ __forceinline__ void put_row(const EmbedArgs& A, const EmbedScratch& W, int lgw,
-                                        int32_t word, const Columns& c, float (&x)[E]) {
-  if (A.idx != nullptr) {
-    const int64_t o = (int64_t)(W.bins[word >> lgw] + W.slot[word]) * A.width + c.c0;
-    const int32_t p = (int32_t)(A.offset + (int64_t)word * A.width + c.c0);
+// Where a word's sum goes: a row of the gradient (R: its type), with another gradient's row
+// added, or a piece of the lists (R: of their values), the number-th. Rounded once.
+template <typename R, bool LISTS, int E>
+__device__ __forceinline__ void put_sum(const EmbedArgs& A, int32_t word, int32_t number,
+                                        const Columns& c, float (&x)[E]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (e < c.ne) A.idx[o + e] = p + e;
-    if (A.val_format == TKEF_VAL_F16)
-      store_some<_Float16, E>(static_cast<_Float16*>(A.val) + o, c.ne, x);
-    else
-      store_some<float, E>(static_cast<float*>(A.val) + o, c.ne, x);
-    return;
-  }
-  const auto row = [&](auto* g, const auto* add) {
-    using G = typename Pointee<decltype(g)>::type;
-    if (add != nullptr) {
+  for (int e = 0; e < E; ++e) x[e] *= A.scale;
+  if constexpr (LISTS) {
+    const int64_t o = (int64_t)number * A.width;
+    const int32_t p = (int32_t)(A.offset + (int64_t)word * A.width + c.c0);
+    if (c.have == E) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4)
+        store16(A.idx + o + c.c0 + e, make_uint4((uint32_t)(p + e), (uint32_t)(p + e + 1),
+                                                 (uint32_t)(p + e + 2), (uint32_t)(p + e + 3)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (e >= c.skip && e < c.skip + c.have) A.idx[o + c.c0 + e] = p + e;
+    }
+    store_row<R, E>(static_cast<R*>(A.val) + o, c, x);
+  } else {
+    if (A.add != nullptr) {
       float y[E];
-      load_some<G, E>(add + word * A.add_ld + c.c0, c.ne, y);
+      load_row<R, E>(static_cast<const R*>(A.add) + word * A.add_ld, c, y);
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] += y[e];
     }
-    store_some<G, E>(g + word * A.grad_ld + c.c0, c.ne, x);
-  };
-  if (A.grad_dtype == TKEF_DTYPE_F32)
-    row(static_cast<float*>(A.grad), static_cast<const float*>(A.add));
-  else if (A.grad_dtype == TKEF_DTYPE_F16)
-    row(static_cast<_Float16*>(A.grad), static_cast<const _Float16*>(A.add));
-  else
-    row(static_cast<__bf16*>(A.grad), static_cast<const __bf16*>(A.add));
+    store_row<R, E>(static_cast<R*>(A.grad) + word * A.grad_ld, c, x);
+  }
 }
 
-template <int E>
-__device__ __forceinline__ void put_sum(const EmbedArgs& A, const EmbedScratch& W, int lgw,
-                                        int32_t word, const Columns& c, float (&sum)[E]) {
+// Rows of dout, K of them under way.
+template <typename O, int E, int K>
+__device__ __forceinline__ void load_rows(uint4 (&raw)[K], const O* dout, int64_t ld,
+                                          const int32_t (&at)[K], const Columns& c) {
+  if (c.skip + c.have == E) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) sum[e] *= A.scale;
-  put_row<E>(A, W, lgw, word, c, sum);
+    for (int j = 0; j < K; ++j) {
+      const loose4_ v = *reinterpret_cast<const loose4_*>(dout + at[j] * ld + c.c0);
+      raw[j] = make_uint4(v.x, v.y, v.z, v.w);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      float x[E];
+      load_row<O, E>(dout + at[j] * ld, c, x);
+      raw[j] = pack(x, dout);
+    }
+  }
 }
 
-constexpr int kAhead = 8;      // rows of a tile under way
-constexpr int kWordsAGroup = 8;  // of words without tokens
+constexpr int kMaxBins = 1 << (20 - kMaxBinBits);
+static_assert(TKEF_ROWS_MAX_VOCAB <= kMaxBins << kMaxBinBits, "bins of a vocabulary");
+constexpr int kAhead = 16;  // rows of a tile under way
 
 // Group g sums the sorted tokens [g tile, (g + 1) tile). A word that lies within them is
 // done; the sums of one that began before them, and of one that goes on behind them, are
-// left for k_embed_join. Groups from `tiles` on write the rows of words without tokens,
-// among the first `rest` words (0 or V).
-template <typename O>
+// left for k_embed_join.
+template <typename O, typename R, bool LISTS>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, int lgw, int lg,
-                                                   int tile, int64_t tiles, int64_t rest) {
-  constexpr int E = sizeof(O) == 4 ? 4 : 8;
+                                                   int tile) {
+  constexpr int E = 16 / (int)sizeof(O);
+  __shared__ int32_t number_of[LISTS ? kMaxBins : 1];
+  __shared__ uint32_t red[4];
   const Columns c = Columns::of<E>(lg, A.width);
   const int64_t g = (int64_t)blockIdx.x * (256 >> lg) + c.group;
-  if (c.ne == 0) return;
-  if (g >= tiles) {
-    const int64_t w0 = (g - tiles) * kWordsAGroup;
-    for (int64_t w = w0; w < w0 + kWordsAGroup && w < rest; ++w)
-      if (W.first[w] == W.first[w + 1]) {
-        float x[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = 0.f;
-        put_row<E>(A, W, lgw, (int32_t)w, c, x);
+  if constexpr (LISTS) {
+    // words that occur before each bin's
+    const int bins = (int)(((int64_t)A.V + (1 << lgw) - 1) >> lgw);
+    const bool writes = blockIdx.x == 0 && blockIdx.y == 0;
+    uint32_t done = 0u;
+    for (int base = 0; base < bins; base += 256) {
+      const int b = base + (int)threadIdx.x;
+      uint32_t total;
+      const uint32_t before = block_scan<256>(b < bins ? (uint32_t)W.bins[b] : 0u, red, &total);
+      if (b < bins) {
+        number_of[b] = (int32_t)(done + before);
+        if (writes) W.before[b] = (int32_t)(done + before);
       }
-    return;
-  }
-  const int total = W.first[A.V];
-  const int p0 = (int)(g * tile), p1 = p0 + tile < total ? p0 + tile : total;
-  if (p0 >= p1) return;
-  const O* dout = static_cast<const O*>(A.dout);
-  float sum[E];
-  int32_t word = W.sorted[p0].word;
-#pragma unroll
-  for (int e = 0; e < E; ++e) sum[e] = 0.f;
-  const auto flush = [&]() {
-    const bool before = W.first[word] < p0, behind = W.first[word + 1] > p1;
-    if (before || behind) {
-      float* to = W.partial + (2 * g + (before ? 0 : 1)) * A.width + c.c0;
-      store_some<float, E>(to, c.ne, sum);
-    } else {
-      put_sum<E>(A, W, lgw, word, c, sum);
+      done += total;
     }
+    if (writes && threadIdx.x == 0) *A.nnz = (int32_t)(done * (uint32_t)A.width);
+    __syncthreads();
+  }
+  if (c.none()) return;
+  const int total = W.first[A.V];
+  if (g * tile >= total) return;
+  const int p0 = (int)g * tile, p1 = p0 + tile < total ? p0 + tile : total;
+  const O* dout = static_cast<const O*>(A.dout);
+  // the words before and behind the tile
+  const int32_t left = p0 > 0 ? W.sorted[p0 - 1].word : -1;
+  const int32_t right = p1 < total ? W.sorted[p1].word : -1;
+  float sum[E];
+  int32_t word = -1, number = 0;
+  const auto flush = [&]() {
+    const bool before = word == left, behind = word == right;
+    if (before || behind)
+      store_row<float, E>(W.partial + (2 * g + (before ? 0 : 1)) * A.width, c, sum);
+    else
+      put_sum<R, LISTS, E>(A, word, number, c, sum);
   };
   for (int p = p0; p < p1; p += kAhead) {
-    Token t[kAhead];
-    float x[kAhead][E];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) t[j] = W.sorted[p + j < p1 ? p + j : p1 - 1];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      load_some<O, E>(dout + t[j].at * A.out_ld + c.c0, c.ne, x[j]);
+    int32_t at[kAhead], of[kAhead], slot[LISTS ? kAhead : 1];
+    uint4 raw[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      if (p + j >= p1) continue;
-      if (t[j].word != word) {
-        flush();
-        word = t[j].word;
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] = 0.f;
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] += x[j][e];
+      const int q = p + j < p1 ? p + j : p1 - 1;
+      const Token t = W.sorted[q];
+      at[j] = t.at;
+      of[j] = t.word;
+      if constexpr (LISTS) slot[j] = W.slots[q];
     }
+    load_rows<O, E, kAhead>(raw, dout, A.out_ld, at, c);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (p + j < p1) {
+        float x[E];
+        unpack(raw[j], x, dout);
+        if (of[j] != word) {
+          if (word >= 0) flush();
+          word = of[j];
+          if constexpr (LISTS) number = number_of[word >> lgw] + slot[j];
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum[e] = x[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum[e] += x[e];
+        }
+      }
   }
   flush();
 }
 
 // The word that begins in tile g and goes on behind it: its sums, tile after tile.
-template <int E>
+template <typename R, int E, bool LISTS>
 __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W, int lgw, int lg,
                                                     int tile, int64_t tiles) {
   const Columns c = Columns::of<E>(lg, A.width);
   const int64_t g = (int64_t)blockIdx.x * (256 >> lg) + c.group;
-  if (g >= tiles || c.ne == 0) return;
-  const int total = W.first[A.V];
+  if (g + 1 >= tiles || c.none()) return;
+  // (all read at once: places behind the last token hold no words, but lie in the workspace)
   const int64_t p0 = g * tile, p1 = p0 + tile;
-  if (p1 >= total) return;
-  const int32_t word = W.sorted[p1 - 1].word;
+  const int total = W.first[A.V];
+  const int32_t left = p0 > 0 ? W.sorted[p0 - 1].word : -1;
+  const int32_t word = W.sorted[p1 - 1].word, right = W.sorted[p1].word;
+  if (p1 >= total || word != right || word == left) return;
   const int end = W.first[word + 1];
-  if (W.first[word] < p0 || end <= p1) return;
+  int32_t number = 0;
+  if constexpr (LISTS) number = W.before[word >> lgw] + W.slots[p1 - 1];
   float sum[E];
-  load_some<float, E>(W.partial + (2 * g + 1) * A.width + c.c0, c.ne, sum);
+  load_row<float, E>(W.partial + (2 * g + 1) * A.width, c, sum);
   const int64_t last = (end - 1) / tile;
-  for (int64_t h = g + 1; h <= last; h += 4) {
-    float x[4][E];
+  constexpr int kJoin = 96 / E;  // partial sums under way
+  for (int64_t h = g + 1; h <= last; h += kJoin) {
+    float x[kJoin][E];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      load_some<float, E>(W.partial + 2 * (h + j < last ? h + j : last) * A.width + c.c0, c.ne,
-                          x[j]);
+    for (int j = 0; j < kJoin; ++j)
+      load_row<float, E>(W.partial + 2 * (h + j < last ? h + j : last) * A.width, c, x[j]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kJoin; ++j)
       if (h + j <= last) {
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] += x[j][e];
       }
   }
-  put_sum<E>(A, W, lgw, word, c, sum);
+  put_sum<R, LISTS, E>(A, word, number, c, sum);
+}
+
+// ----------------------------------------------------------------------------
+// few tokens: one launch, no workspace
+
+constexpr int kFew = 256, kFewWords = 64, kFewAhead = 8;
+
+// Each workgroup reads all tokens. A group (of whole waves) has token i; if no earlier
+// one is of its word, it sums the word's rows. Workgroups from `token_blocks` on write the
+// rows of words that do not occur, kFewWords each.
+template <typename O, typename R, bool LISTS>
+__global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int token_blocks,
+                                                    int rest_lg) {
+  constexpr int E = 16 / (int)sizeof(O), kParts = kFew / 64;
+  __shared__ int32_t word_at[kFew];
+  __shared__ int32_t distinct[LISTS ? kFew : 1];
+  __shared__ uint16_t absent[kFewWords];
+  const int tid = threadIdx.x, lane = tid & 63, n = (int)A.n;
+  int32_t mine = tid < n ? A.tokens[tid] : -1;
+  if (mine < 0 || mine >= A.V) {
+    if (mine != -1 && blockIdx.x == 0 && blockIdx.y == 0)
+      raise_status(A.status, TKEF_STATUS_INDEX_RANGE);
+    mine = -1;
+  }
+  word_at[tid] = mine;
+  __syncthreads();
+  int32_t tok[kParts];
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) tok[i] = word_at[i * 64 + lane];
+  if ((int)blockIdx.x >= token_blocks) {
+    const int64_t w0 = (int64_t)((int)blockIdx.x - token_blocks) * kFewWords;
+    uint64_t there = 0ull;  // words that occur, or are none
+    for (int w = 0; w < kFewWords; ++w) {
+      bool hit = false;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) hit |= tok[i] == (int32_t)(w0 + w);
+      if (__ballot(hit) != 0ull || w0 + w >= A.V) there |= 1ull << w;
+    }
+    if (tid < 64 && !((there >> tid) & 1ull)) absent[lanes_below(~there)] = (uint16_t)tid;
+    __syncthreads();
+    put_rest(A, absent, __popcll(~there), w0, rest_lg, (int)blockIdx.y, (int)gridDim.y);
+    return;
+  }
+  if constexpr (LISTS) {
+    bool again = mine < 0;
+    for (int j = 0; j < tid && !again; ++j) again = word_at[j] == mine;
+    distinct[tid] = again ? 0x7FFFFFFF : mine;
+    __syncthreads();
+  }
+  const Columns c = Columns::of<E>(lg, A.width);
+  const int i = (int)blockIdx.x * (kFew >> lg) + c.group;  // (the same for the whole wave)
+  const int32_t word = __builtin_amdgcn_readfirstlane(i < n ? word_at[i] : -1);
+  const auto below = [&](int32_t limit) {
+    int count = 0;
+    if constexpr (LISTS) {
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) count += __popcll(__ballot(distinct[p * 64 + lane] < limit));
+    }
+    return count;
+  };
+  if constexpr (LISTS) {
+    const int all = below(0x7FFFFFFF);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *A.nnz = (int32_t)((uint32_t)all * (uint32_t)A.width);
+  }
+  if (word < 0) return;
+  const int number = below(word);
+  uint64_t same[kParts];
+  bool earlier = false;
+#pragma unroll
+  for (int p = 0; p < kParts; ++p) {
+    same[p] = __ballot(tok[p] == word);
+    const int bits = i - p * 64;  // places of this part before i
+    const uint64_t before = bits >= 64 ? ~0ull : bits > 0 ? (1ull << bits) - 1ull : 0ull;
+    earlier |= (same[p] & before) != 0ull;
+  }
+  if (earlier || c.none()) return;
+  const O* dout = static_cast<const O*>(A.dout);
+  float sum[E];
+  bool begun = false;
+#pragma unroll
+  for (int p = 0; p < kParts; ++p)
+    while (same[p] != 0ull) {
+      int32_t at[kFewAhead];
+      uint4 raw[kFewAhead];
+      int count = __popcll(same[p]);
+#pragma unroll
+      for (int j = 0; j < kFewAhead; ++j) {
+        at[j] = j < count ? p * 64 + (int)__builtin_ctzll(same[p]) : at[0];
+        same[p] &= same[p] - 1ull;
+      }
+      load_rows<O, E, kFewAhead>(raw, dout, A.out_ld, at, c);
+#pragma unroll
+      for (int j = 0; j < kFewAhead; ++j)
+        if (j < count) {
+          float x[E];
+          unpack(raw[j], x, dout);
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum[e] = begun ? sum[e] + x[e] : x[e];
+          begun = true;
+        }
+    }
+  put_sum<R, LISTS, E>(A, word, number, c, sum);
 }
 
 // threads of a group, as a power of two: a vector each, up to a workgroup
@@ -430,16 +637,18 @@ unsigned slices(int64_t width, int E, int lg) {
   return (unsigned)ceil_div(width, (int64_t)E << lg);
 }
 
-constexpr int kLeastTile = 8;
+// Tokens of a tile, in no more than 4,096 tiles.
+constexpr int64_t kMostTiles = 4096;
+constexpr int kTile = 16;
 int tile_of(int64_t n) {
-  int tile = kLeastTile;
-  while ((int64_t)tile * 4096 < n) tile *= 2;
+  int tile = kTile;
+  while (tile * kMostTiles < n) tile *= 2;
   return tile;
 }
 
-// bits of a bin's words: about 512 bins
+// bits of a bin's words: at most 512 bins, but for vocabularies beyond 2^18
 int bin_bits(int64_t V) {
-  int lgw = 6;
+  int lgw = 0;
   while (lgw < kMaxBinBits && (V >> lgw) > 512) ++lgw;
   return lgw;
 }
@@ -452,14 +661,16 @@ void by_types(int32_t a, int32_t b, F f) {
 }  // namespace
 
 EmbedLayout embed_layout(int64_t rows, int64_t V, int64_t width) {
+  const size_t bins = up256((size_t)ceil_div(V, (int64_t)1 << bin_bits(V)) * 4);
   EmbedLayout l;
   l.sorted = 0;
-  l.first = up256((size_t)rows * sizeof(Token));
-  l.slot = l.first + up256((size_t)(V + 1) * 4);
-  l.bins = l.slot + up256((size_t)V * 4);
-  l.partial = l.bins + up256((size_t)ceil_div(V, (int64_t)1 << bin_bits(V)) * 4);
-  // (fewer tokens than the plan's have tiles no larger, and no more of them than this)
-  const int64_t tiles = rows <= 4096 * kLeastTile ? ceil_div(rows, kLeastTile) : 4096;
+  l.slots = up256((size_t)rows * sizeof(Token));
+  l.first = l.slots + up256((size_t)rows * 4);
+  l.bins = l.first + up256((size_t)(V + 1) * 4);
+  l.before = l.bins + bins;
+  l.partial = l.before + bins;
+  // (a call with fewer tokens than the plan's has no more tiles than this)
+  const int64_t tiles = ceil_div(rows, kTile) < kMostTiles ? ceil_div(rows, kTile) : kMostTiles;
   l.bytes = l.partial + up256((size_t)tiles * 2 * (size_t)width * 4);
   return l;
 }
@@ -476,37 +687,62 @@ hipError_t launch_embed_forward(const EmbedArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t s) {
+namespace {
+
+template <typename O, typename R, bool LISTS>
+void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
+  constexpr int E = 16 / (int)sizeof(O);
+  int lg = lg_threads(a.width, E);
+  const unsigned cut = slices(a.width, E, lg);
+  if (a.n <= kFew) {
+    lg = lg < 6 ? 6 : lg;  // whole waves
+    const int64_t tokens = LISTS && a.n == 0 ? 1 : (a.n + (kFew >> lg) - 1) / (kFew >> lg);
+    const int64_t rest = rest_lg < 0 ? 0 : ceil_div(a.V, kFewWords);
+    if (tokens + rest > 0)
+      k_embed_few<O, R, LISTS>
+          <<<dim3((unsigned)(tokens + rest), cut), kFew, 0, s>>>(a, lg, (int)tokens, rest_lg);
+    return;
+  }
   const EmbedLayout l = embed_layout(a.n, a.V, a.width);
   char* base = static_cast<char*>(ws);
   EmbedScratch w;
   w.sorted = reinterpret_cast<Token*>(base + l.sorted);
+  w.slots = reinterpret_cast<int32_t*>(base + l.slots);
   w.first = reinterpret_cast<int32_t*>(base + l.first);
-  w.slot = reinterpret_cast<int32_t*>(base + l.slot);
   w.bins = reinterpret_cast<int32_t*>(base + l.bins);
+  w.before = reinterpret_cast<int32_t*>(base + l.before);
   w.partial = reinterpret_cast<float*>(base + l.partial);
-  const int lgw = bin_bits(a.V);
-  const unsigned bins = (unsigned)ceil_div(a.V, (int64_t)1 << lgw);
-  k_embed_sort<<<bins, kSortThreads, ((size_t)kSortWaves << lgw) * 4, s>>>(a, w, lgw);
-  if (a.idx != nullptr) k_embed_bins<<<1, 1024, 0, s>>>(a, w, (int)bins);
-  const int tile = tile_of(a.n);
-  const int64_t tiles = a.n == 0 ? 0 : ceil_div(a.n, tile);
-  // rows of words without tokens: written, unless they are there or lists have none
-  const int64_t rest =
-      a.idx != nullptr || (a.add == a.grad && a.add_ld == a.grad_ld) ? 0 : a.V;
-  const int64_t groups = tiles + (rest > 0 ? ceil_div(rest, kWordsAGroup) : 0);
-  return by_dtype(a.out_dtype, [&](auto* o) {
+  const int lgw = bin_bits(a.V), tile = tile_of(a.n);
+  const int64_t tiles = ceil_div(a.n, tile);
+  const dim3 groups((unsigned)ceil_div(tiles, 256 >> lg), cut);
+  k_embed_sort<<<(unsigned)ceil_div(a.V, (int64_t)1 << lgw), kSortThreads,
+                 ((size_t)kSortWaves << lgw) * 4, s>>>(a, w, lgw, rest_lg);
+  k_embed_sum<O, R, LISTS><<<groups, 256, 0, s>>>(a, w, lgw, lg, tile);
+  k_embed_join<R, E, LISTS><<<groups, 256, 0, s>>>(a, w, lgw, lg, tile, tiles);
+}
+
+}  // namespace
+
+hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t s) {
+  if (a.idx != nullptr) {
+    by_types(a.out_dtype, a.val_format == TKEF_VAL_F16 ? TKEF_DTYPE_F16 : TKEF_DTYPE_F32,
+             [&](auto* o, auto* r) {
+               using O = typename Pointee<decltype(o)>::type;
+               using R = typename Pointee<decltype(r)>::type;
+               if constexpr (!std::is_same_v<R, __bf16>) launch_sums<O, R, true>(a, ws, -1, s);
+             });
+    return hipGetLastError();
+  }
+  // rows of words without tokens: written, unless they are there
+  const bool there = a.add == a.grad && a.add_ld == a.grad_ld;
+  const int rest_lg =
+      there ? -1 : lg_threads(a.width, a.grad_dtype == TKEF_DTYPE_F32 ? 4 : 8);
+  by_types(a.out_dtype, a.grad_dtype, [&](auto* o, auto* r) {
     using O = typename Pointee<decltype(o)>::type;
-    constexpr int E = sizeof(O) == 4 ? 4 : 8;
-    const int lg = lg_threads(a.width, E);
-    const unsigned cut = slices(a.width, E, lg);
-    if (groups > 0)
-      k_embed_sum<O><<<dim3((unsigned)ceil_div(groups, 256 >> lg), cut), 256, 0, s>>>(
-          a, w, lgw, lg, tile, tiles, rest);
-    if (tiles > 1)
-      k_embed_join<E><<<dim3((unsigned)ceil_div(tiles, 256 >> lg), cut), 256, 0, s>>>(
-          a, w, lgw, lg, tile, tiles);
+    using R = typename Pointee<decltype(r)>::type;
+    launch_sums<O, R, false>(a, ws, rest_lg, s);
   });
+  return hipGetLastError();
 }
 
 }  // namespace tkef

@@ -128,7 +128,7 @@ def test_stated_workspace():
     for rows in (1, 8, 9, 4096, 32768, 32769, 100_000, 1 << 20):
         for vocab, width in ((1, 1), (1000, 64), (32000, 512), (1 << 20, 5)):
             _, h = make(rows=rows, vocab=vocab, width=width)
-            most = 8 * rows + 8 * vocab + 8 * width * min(4096, -(-rows // 8)) + vocab // 16 + 2048
+            most = 12 * rows + 4 * vocab + 8 * width * min(4096, -(-rows // 16)) + vocab // 8 + 8192
             assert 8 * rows <= size(h) <= most, (rows, vocab, width, size(h), most)
             tk.lib().tkef_embed_plan_destroy(h)
 

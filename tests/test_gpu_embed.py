@@ -146,7 +146,7 @@ def test_lookup_sizes(n, width):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("n", [1, 7, 8, 9, 64, 100, 513, 3000])
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 64, 65, 100, 255, 256, 257, 513, 3000])
 def test_gradient_tokens(n, kind):
     rng = np.random.default_rng(n)
     for vocab, width in ((1, 5), (50, 33), (1000, 64), (2111, 8)):
@@ -160,7 +160,7 @@ def test_gradient_tokens(n, kind):
 def test_gradient_types(grad_type, out_type):
     rng = np.random.default_rng(2)
     for n, vocab, width in ((300, 90, 512), (200, 70, 515), (64, 40, 1030), (50, 30, 2051),
-                            (77, 1100, 64)):
+                            (77, 1100, 64), (270, 500, 515), (290, 30, 2051), (301, 2000, 4)):
         tokens = some_tokens(rng, "law", n, vocab)
         check_gradient(rng, n, vocab, width, out_type, grad_type, 0.37, tokens, pad=n % 3,
                        shift=n % 5, gpad=n % 4)
@@ -180,10 +180,10 @@ def test_gradient_of_many_tokens(n, width, kind):
 @pytest.mark.parametrize("vocab", [(1 << 17) + 5, 1 << 20])
 def test_gradient_of_large_vocabularies(vocab):
     rng = np.random.default_rng(vocab)
-    for kind in ("uniform", "law", "ends"):
-        tokens = some_tokens(rng, kind, 700, vocab)
-        check_gradient(rng, 700, vocab, 3, "f32", "f32", 1.0, tokens)
-        check_lists(rng, 700, vocab, 3, "f32", "f32", 1.0, tokens)
+    for n, kind in ((700, "uniform"), (700, "law"), (700, "ends"), (130, "uniform"), (9, "ends")):
+        tokens = some_tokens(rng, kind, n, vocab)
+        check_gradient(rng, n, vocab, 3, "f32", "f32", 1.0, tokens)
+        check_lists(rng, n, vocab, 3, "f32", "f32", 1.0, tokens)
 
 
 def test_no_tokens():

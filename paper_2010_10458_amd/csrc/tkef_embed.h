@@ -33,7 +33,7 @@ struct EmbedArgs {
 
 // Offsets into the workspace of a gradient, for up to `rows` tokens.
 struct EmbedLayout {
-  size_t sorted, slots, first, bins, before, partial, bytes;
+  size_t sorted, slots, first, bins, before, partial, part, ends, bytes;
 };
 EmbedLayout embed_layout(int64_t rows, int64_t V, int64_t width);
 

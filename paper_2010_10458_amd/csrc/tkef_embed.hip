@@ -115,6 +115,22 @@ __device__ __forceinline__ void store_row(T* row, const Columns& c, const float 
   }
 }
 
+// A row of partial sums: read again soon, so not streamed as results are.
+template <int E>
+__device__ __forceinline__ void keep_row(float* row, const Columns& c, const float (&x)[E]) {
+  if (c.skip + c.have == E) {  // (a shared column's values are the same)
+#pragma unroll
+    for (int i = 0; i < E; i += 4)
+      *reinterpret_cast<loose4_*>(row + c.c0 + i) =
+          loose4_{__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]),
+                  __float_as_uint(x[i + 3])};
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (i < c.have) row[i] = x[i];
+  }
+}
+
 // ----------------------------------------------------------------------------
 // lookup
 
@@ -155,11 +171,11 @@ __global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs A, int lg) {
 
 constexpr int kRestRows = 2;  // rows of a group under way
 
-// The rows w0 + absent[0 .. count) of the gradient: zeros, or the added rows as they are
-// (U: their bits). A group of 1 << lg threads has a row, the slices from `slice` on.
+// The rows w0 + (absent[0 .. count) << shift) of the gradient: zeros, or the added rows as they
+// are (U: their bits). A group of 1 << lg threads has a row, the slices from `slice` on.
 template <typename U>
 __device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* absent, int count,
-                                         int64_t w0, int lg, int slice, int step) {
+                                         int64_t w0, int shift, int lg, int slice, int step) {
   constexpr int E = 16 / (int)sizeof(U);
   const int tid = (int)threadIdx.x, groups = (int)blockDim.x >> lg;
   U* grad = static_cast<U*>(A.grad);
@@ -167,7 +183,7 @@ __device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* abs
   if (A.width < E) {
     for (int r = tid; r < count; r += (int)blockDim.x)
       for (int e = 0; e < A.width; ++e) {
-        const int64_t w = w0 + absent[r];
+        const int64_t w = w0 + ((int64_t)absent[r] << shift);
         grad[w * A.grad_ld + e] = add != nullptr ? add[w * A.add_ld + e] : (U)0;
       }
     return;
@@ -183,7 +199,7 @@ __device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* abs
 #pragma unroll
       for (int j = 0; j < kRestRows; ++j) {
         const int at = r + j * groups;
-        w[j] = w0 + absent[at < count ? at : r];
+        w[j] = w0 + ((int64_t)absent[at < count ? at : r] << shift);
         x[j] = loose4_{0u, 0u, 0u, 0u};
         if (add != nullptr)
           x[j] = __builtin_nontemporal_load(
@@ -199,38 +215,58 @@ __device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* abs
 }
 
 __device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* absent, int count,
-                                         int64_t w0, int lg, int slice, int step) {
+                                         int64_t w0, int shift, int lg, int slice, int step) {
   if (A.grad_dtype == TKEF_DTYPE_F32)
-    put_rest<uint32_t>(A, absent, count, w0, lg, slice, step);
+    put_rest<uint32_t>(A, absent, count, w0, shift, lg, slice, step);
   else
-    put_rest<uint16_t>(A, absent, count, w0, lg, slice, step);
+    put_rest<uint16_t>(A, absent, count, w0, shift, lg, slice, step);
 }
 
 // ----------------------------------------------------------------------------
 // tokens sorted by word
 
+// Words are sorted bin by bin, 1 << lgw of them a bin, by an id that says both: id >> lgw is
+// the bin. Lists want ascending words, so the id is the word. The dense gradient does
+// not: there the words of a bin lie 1 << lgb apart (`spread`), since the frequent words of most
+// vocabularies follow one another, and the bin that holds the most tokens decides how long the
+// sort takes (65,536 tokens of 32,000 by rank: 38% lie in the first 64 words).
+struct Bins {
+  int lgw, lgb, count;
+  bool spread;
+  __host__ __device__ int ids() const { return count << lgw; }
+  __device__ int32_t id(int32_t word) const {
+    return spread ? (word & ((1 << lgb) - 1)) << lgw | word >> lgb : word;
+  }
+  __device__ int32_t word(int32_t id) const {
+    return spread ? (id & ((1 << lgw) - 1)) << lgb | id >> lgw : id;
+  }
+};
+
 struct Token {
-  int32_t at, word;
+  int32_t at, id;
 };
 
 struct EmbedScratch {
-  Token* sorted;    // the batch's tokens that are words, by word, then by place
+  Token* sorted;    // the batch's tokens that are words, by id, then by place
   int32_t* slots;   // of each of them: its word's number among its bin's words that occur
-  int32_t* first;   // V + 1: each word's first place in `sorted`
+  int32_t* first;   // each id's first place in `sorted`, and how many these are
   int32_t* bins;    // per bin: words that occur
   int32_t* before;  // per bin: words that occur in the bins before it
   float* partial;   // per tile: sums of the word that began before it, of the one that goes on
+  Token* part;      // large batches: pieces of kPiece tokens, each by bin
+  int32_t* ends;    // bin x piece: places of a bin's tokens in a piece (and behind the last's)
 };
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kSortAhead = 8;  // tokens a lane reads at once
 constexpr int kMaxBinBits = 9;
 
-// Lanes of the wave whose word (lgw bits) is the lane's own, among the lanes of `who`.
+// Lanes of the wave whose word (lgw bits of it) is the lane's own, among the lanes of `who`.
+template <int MOST>
 __device__ __forceinline__ uint64_t same_word(uint32_t word, int lgw, uint64_t who) {
   uint64_t same = who;
 #pragma unroll
-  for (int b = 0; b < kMaxBinBits; ++b)
+  for (int b = 0; b < MOST; ++b)
     if (b < lgw) {
       const bool one = (word >> b) & 1u;
       const uint64_t with = __ballot(one);
@@ -250,51 +286,167 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Workgroup b sorts the tokens of the words [b << lgw, (b + 1) << lgw): it reads all
-// tokens, counts those of lower words (they come before) and its own word by word, and
+// Large batches: each workgroup puts a piece of the batch in the order of its bins (stable,
+// wave w has the w-th part of it), so that a bin's workgroup reads its own tokens alone.
+constexpr int kPiece = 2048, kMaxPieces = TKEF_EMBED_MAX_ROWS / kPiece;
+static_assert(kMaxPieces <= kSortThreads, "a thread for each piece");
+constexpr int kSplitThreads = 256, kSplitWaves = kSplitThreads / 64;
+constexpr int kSplitAhead = kPiece / kSplitThreads;
+constexpr int kMaxBins = 1 << (20 - kMaxBinBits);
+static_assert(TKEF_ROWS_MAX_VOCAB <= kMaxBins << kMaxBinBits, "bins of a vocabulary");
+
+__global__ __launch_bounds__(kSplitThreads) void k_embed_split(EmbedArgs A, EmbedScratch W, Bins B,
+                                                               int pieces) {
+  extern __shared__ uint32_t hist[];  // wave x bin
+  __shared__ uint32_t red[kSplitWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bins = B.count;
+  const int begin = (int)blockIdx.x * kPiece + wave * (64 * kSplitAhead);
+  int32_t t[kSplitAhead];
+#pragma unroll
+  for (int j = 0; j < kSplitAhead; ++j) {
+    const int i = begin + j * 64 + lane;
+    t[j] = i < A.n ? A.tokens[i] : -1;
+  }
+  for (int i = tid; i < bins * kSplitWaves; i += kSplitThreads) hist[i] = 0u;
+  __syncthreads();
+  uint32_t* mine = hist + wave * bins;
+  uint32_t bits = 0u;
+#pragma unroll
+  for (int j = 0; j < kSplitAhead; ++j) {
+    const bool in = t[j] >= 0 && t[j] < A.V;
+    if (!in && t[j] != -1) bits = TKEF_STATUS_INDEX_RANGE;
+    t[j] = in ? B.id(t[j]) : -1;
+    if (in) atomicAdd(&mine[t[j] >> B.lgw], 1u);
+  }
+  raise_status(A.status, bits);
+  __syncthreads();
+  // places of each bin, and of each wave's share of it: a thread has `each` bins
+  const int each = (bins + kSplitThreads - 1) / kSplitThreads;
+  const int b0 = tid * each, b1 = b0 + each < bins ? b0 + each : bins;
+  uint32_t count = 0u, all;
+  for (int b = b0; b < b1; ++b)
+    for (int v = 0; v < kSplitWaves; ++v) count += hist[v * bins + b];
+  uint32_t place = block_scan<kSplitThreads>(count, red, &all);
+  for (int b = b0; b < b1; ++b) {
+    W.ends[(int64_t)b * pieces + blockIdx.x] = (int32_t)place;
+    for (int v = 0; v < kSplitWaves; ++v) {
+      const uint32_t c = hist[v * bins + b];
+      hist[v * bins + b] = place;
+      place += c;
+    }
+  }
+  if (tid == 0) W.ends[(int64_t)bins * pieces + blockIdx.x] = (int32_t)all;
+  __syncthreads();
+  const int lgb = 32 - __builtin_clz((uint32_t)bins);  // (bins at least 1)
+  Token* out = W.part + (int64_t)blockIdx.x * kPiece;
+#pragma unroll
+  for (int j = 0; j < kSplitAhead; ++j) {
+    const bool own = t[j] >= 0;
+    const uint64_t who = __ballot(own);
+    if (who == 0ull) continue;
+    const uint32_t bin = own ? (uint32_t)t[j] >> B.lgw : 0u;
+    const uint64_t same = same_word<20 - kMaxBinBits + 1>(bin, lgb, who);
+    const int rank = lanes_below(same);
+    const uint32_t at = mine[bin] + (uint32_t)rank;
+    wave_fence();  // every lane has read before one writes, and before the next 64 read
+    if (own) {
+      out[at] = Token{begin + j * 64 + lane, t[j]};
+      if (rank == 0) mine[bin] = at + (uint32_t)__popcll(same);
+    }
+    wave_fence();
+  }
+}
+
+// Workgroup b sorts the tokens of bin b: it reads the tokens, counts its own word by word (and those of lower bins, which come before), and
 // in a second reading puts its own in place; between them it writes the gradient's rows of
-// words that do not occur (rest_lg >= 0). Wave w has the w-th share of the batch, so
+// words that do not occur (rest_lg >= 0). Wave w has the w-th share of the tokens, so
 // a word's tokens are in the batch's order: waves in turn, and in a wave, lanes.
+// PIECES: its tokens lie in the pieces that k_embed_split made; else all tokens are read.
+template <bool PIECES>
 __global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, EmbedScratch W,
-                                                               int lgw, int rest_lg) {
+                                                               Bins B, int rest_lg) {
   extern __shared__ uint32_t hist[];  // wave x word
   __shared__ uint32_t red[kSortWaves], below_of[kSortWaves];
   __shared__ uint32_t slot_of[1 << kMaxBinBits];
   __shared__ uint16_t absent[1 << kMaxBinBits];
+  // of each piece: the bin's tokens before it, and where (less those) its own lie
+  __shared__ int32_t piece_of[PIECES ? kMaxPieces : 1], part_of[PIECES ? kMaxPieces : 1];
+  constexpr int kAhead = PIECES ? 4 : kSortAhead;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int words = 1 << lgw;
-  const int32_t w0 = (int32_t)blockIdx.x << lgw;
-  const int n = (int)A.n;
+  const int words = 1 << B.lgw;
+  const int32_t w0 = (int32_t)blockIdx.x << B.lgw;  // ids from here on
+  const int pieces = (int)((A.n + kPiece - 1) / kPiece);
+  int n = (int)A.n;
+  uint32_t below = 0u, bits = 0u;
+  if constexpr (PIECES) {
+    uint32_t own = 0u, total;
+    const int64_t at = (int64_t)blockIdx.x * pieces + tid;
+    if (tid < pieces) {
+      below = (uint32_t)W.ends[at];
+      own = (uint32_t)W.ends[at + pieces] - below;
+    }
+    const uint32_t before = block_scan<kSortThreads>(own, red, &total);
+    if (tid < pieces) {
+      piece_of[tid] = (int32_t)before;
+      part_of[tid] = tid * kPiece + (int32_t)(below - before);
+    }
+    n = (int)total;
+    __syncthreads();
+  }
   const int per = ((n + kSortThreads - 1) / kSortThreads) * 64;
   const int begin = wave * per, end = begin + per < n ? begin + per : n;
-  int32_t t[kSortAhead];
+  int32_t t[kAhead], at_[PIECES ? kAhead : 1];
   const auto read = [&](int from) {
+    if constexpr (PIECES) {
+      int piece[kAhead];
 #pragma unroll
-    for (int j = 0; j < kSortAhead; ++j) {
-      const int i = from + j * 64 + lane;
-      t[j] = i < end ? A.tokens[i] : -1;
+      for (int j = 0; j < kAhead; ++j) piece[j] = 0;
+      for (int step = 1 << (31 - __builtin_clz((uint32_t)pieces)); step > 0; step >>= 1)
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int p = piece[j] + step;
+          if (p < pieces && piece_of[p] <= from + j * 64 + lane) piece[j] = p;
+        }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = from + j * 64 + lane;
+        const Token none = {0, -1};
+        const Token k = i < end ? W.part[part_of[piece[j]] + i] : none;
+        t[j] = k.id;
+        at_[j] = k.at;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = from + j * 64 + lane;
+        t[j] = i < end ? A.tokens[i] : -1;
+      }
     }
   };
   read(begin);
   for (int i = tid; i < words * kSortWaves; i += kSortThreads) hist[i] = 0u;
   __syncthreads();
   uint32_t* mine = hist + wave * words;
-  uint32_t below = 0u, bits = 0u;
   for (int from = begin;;) {
 #pragma unroll
-    for (int j = 0; j < kSortAhead; ++j) {
-      const bool in = t[j] >= 0 && t[j] < A.V;
-      if (!in && t[j] != -1) bits = TKEF_STATUS_INDEX_RANGE;
-      below += in && t[j] < w0 ? 1u : 0u;
-      if (in && t[j] >= w0 && t[j] - w0 < words) atomicAdd(&mine[t[j] - w0], 1u);
+    for (int j = 0; j < kAhead; ++j) {
+      if constexpr (PIECES) {
+        if (t[j] >= 0) atomicAdd(&mine[t[j] - w0], 1u);
+      } else {
+        const bool in = t[j] >= 0 && t[j] < A.V;
+        if (!in && t[j] != -1) bits = TKEF_STATUS_INDEX_RANGE;
+        const int32_t id = B.id(t[j]);
+        below += in && id < w0 ? 1u : 0u;
+        if (in && id >= w0 && id - w0 < words) atomicAdd(&mine[id - w0], 1u);
+      }
     }
-    from += kSortAhead * 64;
+    from += kAhead * 64;
     if (from >= end) break;
     read(from);
   }
   if (blockIdx.x == 0) raise_status(A.status, bits);
-  if (per > kSortAhead * 64) read(begin);
+  if (per > kAhead * 64) read(begin);
   below = wave_incl(below);
   if (lane == 63) below_of[wave] = below;
   __syncthreads();
@@ -309,10 +461,8 @@ __global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, Emb
   const uint32_t ahead = block_scan<kSortThreads>(count | (count > 0u ? 1u << 21 : 0u), red, &all);
   if (tid < words) {
     uint32_t place = at + (ahead & ((1u << 21) - 1u));
-    if (w0 + tid < A.V) {
-      W.first[w0 + tid] = (int32_t)place;
-      if (w0 + tid == A.V - 1) W.first[A.V] = (int32_t)(place + count);
-    }
+    W.first[w0 + tid] = (int32_t)place;
+    if (w0 + tid == B.ids() - 1) W.first[B.ids()] = (int32_t)(place + count);
     slot_of[tid] = ahead >> 21;
     if (count == 0u) absent[tid - (int)(ahead >> 21)] = (uint16_t)tid;
     for (int v = 0; v < kSortWaves; ++v) {
@@ -324,28 +474,32 @@ __global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, Emb
   if (tid == 0) W.bins[blockIdx.x] = (int32_t)(all >> 21);
   __syncthreads();
   if (rest_lg >= 0) {
-    const int there = A.V - w0 < words ? A.V - w0 : words;
-    put_rest(A, absent, there - (int)(all >> 21), w0, rest_lg, 0, 1);
+    // words of the bin (those that the vocabulary does not reach come last)
+    const int b = (int)blockIdx.x, base = B.spread ? b : w0, shift = B.spread ? B.lgb : 0;
+    const int reach = A.V > base ? ((A.V - 1 - base) >> shift) + 1 : 0;
+    put_rest(A, absent, (reach < words ? reach : words) - (int)(all >> 21), base, shift, rest_lg, 0,
+             1);
   }
   for (int from = begin;;) {
 #pragma unroll
-    for (int j = 0; j < kSortAhead; ++j) {
-      const bool own = t[j] >= w0 && t[j] < A.V && t[j] - w0 < words;
+    for (int j = 0; j < kAhead; ++j) {
+      const int32_t id = PIECES ? t[j] : B.id(t[j]);
+      const bool own = t[j] >= 0 && (PIECES || t[j] < A.V) && id >= w0 && id - w0 < words;
       const uint64_t who = __ballot(own);
       if (who == 0ull) continue;
-      const uint32_t word = own ? (uint32_t)(t[j] - w0) : 0u;
-      const uint64_t same = same_word(word, lgw, who);
+      const uint32_t word = own ? (uint32_t)(id - w0) : 0u;
+      const uint64_t same = same_word<kMaxBinBits>(word, B.lgw, who);
       const int rank = lanes_below(same);
       const uint32_t place = mine[word] + (uint32_t)rank;
       wave_fence();  // every lane has read before one writes, and before the next 64 read
       if (own) {
-        W.sorted[place] = Token{from + j * 64 + lane, t[j]};
+        W.sorted[place] = Token{PIECES ? at_[PIECES ? j : 0] : from + j * 64 + lane, id};
         if (A.idx != nullptr) W.slots[place] = (int32_t)slot_of[word];
         if (rank == 0) mine[word] = place + (uint32_t)__popcll(same);
       }
       wave_fence();
     }
-    from += kSortAhead * 64;
+    from += kAhead * 64;
     if (from >= end) break;
     read(from);
   }
@@ -406,15 +560,13 @@ __device__ __forceinline__ void load_rows(uint4 (&raw)[K], const O* dout, int64_
   }
 }
 
-constexpr int kMaxBins = 1 << (20 - kMaxBinBits);
-static_assert(TKEF_ROWS_MAX_VOCAB <= kMaxBins << kMaxBinBits, "bins of a vocabulary");
-constexpr int kAhead = 16;  // rows of a tile under way
+constexpr int kAhead = 8;  // rows of a tile under way
 
 // Group g sums the sorted tokens [g tile, (g + 1) tile). A word that lies within them is
 // done; the sums of one that began before them, and of one that goes on behind them, are
 // left for k_embed_join.
 template <typename O, typename R, bool LISTS>
-__global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, int lgw, int lg,
+__global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, Bins B, int lg,
                                                    int tile) {
   constexpr int E = 16 / (int)sizeof(O);
   __shared__ int32_t number_of[LISTS ? kMaxBins : 1];
@@ -422,39 +574,41 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
   const Columns c = Columns::of<E>(lg, A.width);
   const int64_t g = (int64_t)blockIdx.x * (256 >> lg) + c.group;
   if constexpr (LISTS) {
-    // words that occur before each bin's
-    const int bins = (int)(((int64_t)A.V + (1 << lgw) - 1) >> lgw);
+    // words that occur before each bin's: a thread has kEach bins
+    constexpr int kEach = kMaxBins / 256;
+    const int bins = B.count, b0 = (int)threadIdx.x * kEach;
     const bool writes = blockIdx.x == 0 && blockIdx.y == 0;
-    uint32_t done = 0u;
-    for (int base = 0; base < bins; base += 256) {
-      const int b = base + (int)threadIdx.x;
-      uint32_t total;
-      const uint32_t before = block_scan<256>(b < bins ? (uint32_t)W.bins[b] : 0u, red, &total);
-      if (b < bins) {
-        number_of[b] = (int32_t)(done + before);
-        if (writes) W.before[b] = (int32_t)(done + before);
-      }
-      done += total;
+    uint32_t of[kEach], own = 0u, done;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) of[i] = b0 + i < bins ? (uint32_t)W.bins[b0 + i] : 0u;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) own += of[i];
+    uint32_t before = block_scan<256>(own, red, &done);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      number_of[b0 + i] = (int32_t)before;
+      if (writes && b0 + i < bins) W.before[b0 + i] = (int32_t)before;
+      before += of[i];
     }
     if (writes && threadIdx.x == 0) *A.nnz = (int32_t)(done * (uint32_t)A.width);
     __syncthreads();
   }
   if (c.none()) return;
-  const int total = W.first[A.V];
+  const int total = W.first[B.ids()];
   if (g * tile >= total) return;
   const int p0 = (int)g * tile, p1 = p0 + tile < total ? p0 + tile : total;
   const O* dout = static_cast<const O*>(A.dout);
   // the words before and behind the tile
-  const int32_t left = p0 > 0 ? W.sorted[p0 - 1].word : -1;
-  const int32_t right = p1 < total ? W.sorted[p1].word : -1;
+  const int32_t left = p0 > 0 ? W.sorted[p0 - 1].id : -1;
+  const int32_t right = p1 < total ? W.sorted[p1].id : -1;
   float sum[E];
-  int32_t word = -1, number = 0;
+  int32_t id = -1, number = 0;
   const auto flush = [&]() {
-    const bool before = word == left, behind = word == right;
+    const bool before = id == left, behind = id == right;
     if (before || behind)
-      store_row<float, E>(W.partial + (2 * g + (before ? 0 : 1)) * A.width, c, sum);
+      keep_row<E>(W.partial + (2 * g + (before ? 0 : 1)) * A.width, c, sum);
     else
-      put_sum<R, LISTS, E>(A, word, number, c, sum);
+      put_sum<R, LISTS, E>(A, B.word(id), number, c, sum);
   };
   for (int p = p0; p < p1; p += kAhead) {
     int32_t at[kAhead], of[kAhead], slot[LISTS ? kAhead : 1];
@@ -464,7 +618,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
       const int q = p + j < p1 ? p + j : p1 - 1;
       const Token t = W.sorted[q];
       at[j] = t.at;
-      of[j] = t.word;
+      of[j] = t.id;
       if constexpr (LISTS) slot[j] = W.slots[q];
     }
     load_rows<O, E, kAhead>(raw, dout, A.out_ld, at, c);
@@ -473,10 +627,10 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
       if (p + j < p1) {
         float x[E];
         unpack(raw[j], x, dout);
-        if (of[j] != word) {
-          if (word >= 0) flush();
-          word = of[j];
-          if constexpr (LISTS) number = number_of[word >> lgw] + slot[j];
+        if (of[j] != id) {
+          if (id >= 0) flush();
+          id = of[j];
+          if constexpr (LISTS) number = number_of[id >> B.lgw] + slot[j];
 #pragma unroll
           for (int e = 0; e < E; ++e) sum[e] = x[e];
         } else {
@@ -488,39 +642,68 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
   flush();
 }
 
-// The word that begins in tile g and goes on behind it: its sums, tile after tile.
+// The words that begin in a tile and go on behind it: their sums, tile after tile. A
+// workgroup looks at 64 tiles and takes every gridDim.z-th of the words that it finds; its
+// groups have equal parts of the word's tiles, which the first joins.
+constexpr int kWindow = 64, kJoiners = 16;
 template <typename R, int E, bool LISTS>
-__global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W, int lgw, int lg,
-                                                    int tile, int64_t tiles) {
+__global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W, Bins B, int lg,
+                                                    int tile, int tiles) {
+  constexpr int kJoin = 64 / E;  // partial sums under way
+  __shared__ float sums[256][E];
   const Columns c = Columns::of<E>(lg, A.width);
-  const int64_t g = (int64_t)blockIdx.x * (256 >> lg) + c.group;
-  if (g + 1 >= tiles || c.none()) return;
+  const int tid = threadIdx.x, lane = tid & 63, groups = 256 >> lg;
+  const int g = (int)blockIdx.x * kWindow + lane;
   // (all read at once: places behind the last token hold no words, but lie in the workspace)
-  const int64_t p0 = g * tile, p1 = p0 + tile;
-  const int total = W.first[A.V];
-  const int32_t left = p0 > 0 ? W.sorted[p0 - 1].word : -1;
-  const int32_t word = W.sorted[p1 - 1].word, right = W.sorted[p1].word;
-  if (p1 >= total || word != right || word == left) return;
-  const int end = W.first[word + 1];
+  const bool in = g + 1 < tiles;
+  const int p0 = g * tile, p1 = p0 + tile, total = W.first[B.ids()];
+  const int32_t left = in && p0 > 0 ? W.sorted[p0 - 1].id : -1;
+  const int32_t id = in ? W.sorted[p1 - 1].id : -1, right = in ? W.sorted[p1].id : -1;
+  const bool begins = in && p1 < total && id == right && id != left;
+  int last = 0;
   int32_t number = 0;
-  if constexpr (LISTS) number = W.before[word >> lgw] + W.slots[p1 - 1];
-  float sum[E];
-  load_row<float, E>(W.partial + (2 * g + 1) * A.width, c, sum);
-  const int64_t last = (end - 1) / tile;
-  constexpr int kJoin = 96 / E;  // partial sums under way
-  for (int64_t h = g + 1; h <= last; h += kJoin) {
-    float x[kJoin][E];
-#pragma unroll
-    for (int j = 0; j < kJoin; ++j)
-      load_row<float, E>(W.partial + 2 * (h + j < last ? h + j : last) * A.width, c, x[j]);
-#pragma unroll
-    for (int j = 0; j < kJoin; ++j)
-      if (h + j <= last) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] += x[j][e];
-      }
+  if (begins) {
+    last = (W.first[id + 1] - 1) / tile;
+    if constexpr (LISTS) number = W.before[id >> B.lgw] + W.slots[p1 - 1];
   }
-  put_sum<R, LISTS, E>(A, word, number, c, sum);
+  uint64_t found = __ballot(begins);  // (the same in every wave)
+  for (int skip = (int)blockIdx.z; found != 0ull; --skip) {
+    const int from = (int)__builtin_ctzll(found);
+    found &= found - 1ull;
+    if (skip != 0) continue;
+    skip = (int)gridDim.z;
+    const int h0 = (int)blockIdx.x * kWindow + from, terms = __shfl(last, from) - h0 + 1;
+    const int32_t its_id = __shfl(id, from), its_number = __shfl(number, from);
+    const int per = (terms + groups - 1) / groups;
+    const int begin = c.group * per, end = begin + per < terms ? begin + per : terms;
+    float sum[E];
+    if (!c.none() && begin < end) {
+      for (int i = begin; i < end; i += kJoin) {
+        float x[kJoin][E];
+#pragma unroll
+        for (int j = 0; j < kJoin; ++j) {
+          const int h = h0 + (i + j < end ? i + j : end - 1);
+          load_row<float, E>(W.partial + (2 * (int64_t)h + (h == h0 ? 1 : 0)) * A.width, c, x[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kJoin; ++j)
+          if (i + j < end) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] = i + j == begin ? x[j][e] : sum[e] + x[j][e];
+          }
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) sums[tid][e] = sum[e];
+    }
+    __syncthreads();
+    if (c.group == 0 && !c.none()) {
+      for (int q = 1; q * per < terms; ++q)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += sums[(q << lg) + tid][e];
+      put_sum<R, LISTS, E>(A, B.word(its_id), its_number, c, sum);
+    }
+    __syncthreads();
+  }
 }
 
 // ----------------------------------------------------------------------------
@@ -561,7 +744,7 @@ __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int tok
     }
     if (tid < 64 && !((there >> tid) & 1ull)) absent[lanes_below(~there)] = (uint16_t)tid;
     __syncthreads();
-    put_rest(A, absent, __popcll(~there), w0, rest_lg, (int)blockIdx.y, (int)gridDim.y);
+    put_rest(A, absent, __popcll(~there), w0, 0, rest_lg, (int)blockIdx.y, (int)gridDim.y);
     return;
   }
   if constexpr (LISTS) {
@@ -646,11 +829,19 @@ int tile_of(int64_t n) {
   return tile;
 }
 
-// bits of a bin's words: at most 512 bins, but for vocabularies beyond 2^18
-int bin_bits(int64_t V) {
-  int lgw = 0;
-  while (lgw < kMaxBinBits && (V >> lgw) > 512) ++lgw;
-  return lgw;
+// Batches from here on are split into pieces first.
+constexpr int64_t kSplitFrom = 16384;
+
+// 512 bins, more for vocabularies beyond 2^18
+Bins bins_of(int64_t V, bool spread) {
+  int lgv = 0;
+  while (((int64_t)1 << lgv) < V) ++lgv;
+  Bins b;
+  b.lgw = lgv < 9 ? 0 : lgv - 9 < kMaxBinBits ? lgv - 9 : kMaxBinBits;
+  b.lgb = lgv - b.lgw;
+  b.spread = spread;
+  b.count = spread ? 1 << b.lgb : (int)ceil_div(V, (int64_t)1 << b.lgw);
+  return b;
 }
 
 template <typename F>
@@ -661,17 +852,22 @@ void by_types(int32_t a, int32_t b, F f) {
 }  // namespace
 
 EmbedLayout embed_layout(int64_t rows, int64_t V, int64_t width) {
-  const size_t bins = up256((size_t)ceil_div(V, (int64_t)1 << bin_bits(V)) * 4);
+  const Bins b = bins_of(V, true);  // (no fewer than the lists')
+  const size_t bins = up256((size_t)b.count * 4);
   EmbedLayout l;
   l.sorted = 0;
   l.slots = up256((size_t)rows * sizeof(Token));
   l.first = l.slots + up256((size_t)rows * 4);
-  l.bins = l.first + up256((size_t)(V + 1) * 4);
+  l.bins = l.first + up256((size_t)(b.ids() + 1) * 4);
   l.before = l.bins + bins;
   l.partial = l.before + bins;
   // (a call with fewer tokens than the plan's has no more tiles than this)
   const int64_t tiles = ceil_div(rows, kTile) < kMostTiles ? ceil_div(rows, kTile) : kMostTiles;
-  l.bytes = l.partial + up256((size_t)tiles * 2 * (size_t)width * 4);
+  l.part = l.partial + up256((size_t)tiles * 2 * (size_t)width * 4);
+  const bool split = rows >= kSplitFrom;
+  l.ends = l.part + (split ? up256((size_t)rows * sizeof(Token)) : 0);
+  l.bytes = l.ends +
+            (split ? up256((size_t)ceil_div(rows, kPiece) * (size_t)(b.count + 1) * 4) : 0);
   return l;
 }
 
@@ -712,13 +908,25 @@ void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
   w.bins = reinterpret_cast<int32_t*>(base + l.bins);
   w.before = reinterpret_cast<int32_t*>(base + l.before);
   w.partial = reinterpret_cast<float*>(base + l.partial);
-  const int lgw = bin_bits(a.V), tile = tile_of(a.n);
+  w.part = reinterpret_cast<Token*>(base + l.part);
+  w.ends = reinterpret_cast<int32_t*>(base + l.ends);
+  const Bins b = bins_of(a.V, !LISTS);
+  const int tile = tile_of(a.n);
   const int64_t tiles = ceil_div(a.n, tile);
-  const dim3 groups((unsigned)ceil_div(tiles, 256 >> lg), cut);
-  k_embed_sort<<<(unsigned)ceil_div(a.V, (int64_t)1 << lgw), kSortThreads,
-                 ((size_t)kSortWaves << lgw) * 4, s>>>(a, w, lgw, rest_lg);
-  k_embed_sum<O, R, LISTS><<<groups, 256, 0, s>>>(a, w, lgw, lg, tile);
-  k_embed_join<R, E, LISTS><<<groups, 256, 0, s>>>(a, w, lgw, lg, tile, tiles);
+  const size_t lds = ((size_t)kSortWaves << b.lgw) * 4;
+  if (a.n >= kSplitFrom) {
+    const int pieces = (int)ceil_div(a.n, kPiece);
+    k_embed_split<<<pieces, kSplitThreads, (size_t)kSplitWaves * (size_t)b.count * 4, s>>>(a, w, b,
+                                                                                          pieces);
+    k_embed_sort<true><<<b.count, kSortThreads, lds, s>>>(a, w, b, rest_lg);
+  } else {
+    k_embed_sort<false><<<b.count, kSortThreads, lds, s>>>(a, w, b, rest_lg);
+  }
+  k_embed_sum<O, R, LISTS>
+      <<<dim3((unsigned)ceil_div(tiles, 256 >> lg), cut), 256, 0, s>>>(a, w, b, lg, tile);
+  const int jlg = lg < 6 ? lg : 6;
+  k_embed_join<R, E, LISTS><<<dim3((unsigned)ceil_div(tiles, kWindow), slices(a.width, E, jlg), kJoiners),
+                              256, 0, s>>>(a, w, b, jlg, tile, (int)tiles);
 }
 
 }  // namespace

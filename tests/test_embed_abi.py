@@ -128,7 +128,8 @@ def test_stated_workspace():
     for rows in (1, 8, 9, 4096, 32768, 32769, 100_000, 1 << 20):
         for vocab, width in ((1, 1), (1000, 64), (32000, 512), (1 << 20, 5)):
             _, h = make(rows=rows, vocab=vocab, width=width)
-            most = 12 * rows + 4 * vocab + 8 * width * min(4096, -(-rows // 16)) + vocab // 8 + 8192
+            most = (12 if rows < 16384 else 20) * rows + 4 * vocab + 8 * width * min(4096, -(-rows // 16)) + 8192
+            most += vocab // 32 + (0 if rows < 16384 else -(-rows // 2048) * 4 * 2050)
             assert 8 * rows <= size(h) <= most, (rows, vocab, width, size(h), most)
             tk.lib().tkef_embed_plan_destroy(h)
 

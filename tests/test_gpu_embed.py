@@ -169,7 +169,8 @@ def test_gradient_types(grad_type, out_type):
 
 
 @pytest.mark.parametrize("kind", ["law", "one", "two", "uniform"])
-@pytest.mark.parametrize("n,width", [(32768, 8), (32769, 9), (70001, 16), (300_000, 3)])
+@pytest.mark.parametrize("n,width", [(16383, 5), (16384, 8), (18433, 65), (32769, 9), (70001, 16),
+                                     (300_000, 3)])
 def test_gradient_of_many_tokens(n, width, kind):
     rng = np.random.default_rng(n)
     tokens = some_tokens(rng, kind, n, 1500)
@@ -180,7 +181,8 @@ def test_gradient_of_many_tokens(n, width, kind):
 @pytest.mark.parametrize("vocab", [(1 << 17) + 5, 1 << 20])
 def test_gradient_of_large_vocabularies(vocab):
     rng = np.random.default_rng(vocab)
-    for n, kind in ((700, "uniform"), (700, "law"), (700, "ends"), (130, "uniform"), (9, "ends")):
+    for n, kind in ((700, "uniform"), (700, "law"), (700, "ends"), (130, "uniform"), (9, "ends"),
+                    (20000, "law"), (16500, "ends"), (40000, "uniform")):
         tokens = some_tokens(rng, kind, n, vocab)
         check_gradient(rng, n, vocab, 3, "f32", "f32", 1.0, tokens)
         check_lists(rng, n, vocab, 3, "f32", "f32", 1.0, tokens)

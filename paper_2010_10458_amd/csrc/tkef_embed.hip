@@ -560,19 +560,35 @@ __device__ __forceinline__ void load_rows(uint4 (&raw)[K], const O* dout, int64_
   }
 }
 
-constexpr int kAhead = 8;  // rows of a tile under way
+constexpr int kAhead = 8, kWaveAhead = 16;  // rows of a tile under way
 
 // Group g sums the sorted tokens [g tile, (g + 1) tile). A word that lies within them is
 // done; the sums of one that began before them, and of one that goes on behind them, are
 // left for k_embed_join.
-template <typename O, typename R, bool LISTS>
+// WAVE: groups of whole waves. Lane l reads the tile's token l - 1, beside the number of tokens, and
+// hands it on in a scalar register: one access and one address for a row, and a branch where
+// the word changes.
+template <typename O, typename R, bool LISTS, bool WAVE>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, Bins B, int lg,
                                                    int tile) {
   constexpr int E = 16 / (int)sizeof(O);
   __shared__ int32_t number_of[LISTS ? kMaxBins : 1];
   __shared__ uint32_t red[4];
-  const Columns c = Columns::of<E>(lg, A.width);
+  Columns c = Columns::of<E>(lg, A.width);
+  if constexpr (WAVE) c.group = __builtin_amdgcn_readfirstlane(c.group);
   const int64_t g = (int64_t)blockIdx.x * (256 >> lg) + c.group;
+  const int lane = threadIdx.x & 63;
+  // the token at p - 1 + lane (places behind the last lie in the workspace, but hold none)
+  Token mine = {0, -1};
+  int32_t my_slot = 0;
+  const auto read = [&](int64_t p) {
+    int64_t q = p - 1 + (lane < kWaveAhead + 2 ? lane : kWaveAhead + 1);
+    q = q < 0 ? 0 : q < A.n ? q : A.n - 1;
+    mine = W.sorted[q];
+    if constexpr (LISTS) my_slot = W.slots[q];
+  };
+  if constexpr (WAVE) read(g * tile);
+  const int total = W.first[B.ids()];
   if constexpr (LISTS) {
     // words that occur before each bin's: a thread has kEach bins
     constexpr int kEach = kMaxBins / 256;
@@ -593,14 +609,15 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
     if (writes && threadIdx.x == 0) *A.nnz = (int32_t)(done * (uint32_t)A.width);
     __syncthreads();
   }
-  if (c.none()) return;
-  const int total = W.first[B.ids()];
-  if (g * tile >= total) return;
+  if (g * tile >= total || (!WAVE && c.none())) return;
   const int p0 = (int)g * tile, p1 = p0 + tile < total ? p0 + tile : total;
   const O* dout = static_cast<const O*>(A.dout);
   // the words before and behind the tile
-  const int32_t left = p0 > 0 ? W.sorted[p0 - 1].id : -1;
-  const int32_t right = p1 < total ? W.sorted[p1].id : -1;
+  int32_t left = -1, right = -1;
+  if constexpr (!WAVE) {
+    if (p0 > 0) left = W.sorted[p0 - 1].id;
+    if (p1 < total) right = W.sorted[p1].id;
+  }
   float sum[E];
   int32_t id = -1, number = 0;
   const auto flush = [&]() {
@@ -610,6 +627,47 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
     else
       put_sum<R, LISTS, E>(A, B.word(id), number, c, sum);
   };
+  if constexpr (WAVE) {
+    if (c.none()) {  // reads the last columns, writes nothing
+      c.c0 = A.width - E;
+      c.skip = E;
+    }
+    if (p0 > 0) left = __builtin_amdgcn_readlane(mine.id, 0);
+    for (int p = p0;;) {
+      const int count = p1 - p < kWaveAhead ? p1 - p : kWaveAhead;
+      uint4 raw[kWaveAhead];
+#pragma unroll
+      for (int j = 0; j < kWaveAhead; ++j) {
+        const int32_t at = __builtin_amdgcn_readlane(mine.at, 1 + (j < count ? j : count - 1));
+        const loose4_ v = *reinterpret_cast<const loose4_*>(dout + at * A.out_ld + c.c0);
+        raw[j] = make_uint4(v.x, v.y, v.z, v.w);
+      }
+      if (p + count == p1 && p1 < total) right = __builtin_amdgcn_readlane(mine.id, 1 + count);
+#pragma unroll
+      for (int j = 0; j < kWaveAhead; ++j)
+        if (j < count) {
+          float x[E];
+          unpack(raw[j], x, dout);
+          const int32_t next = __builtin_amdgcn_readlane(mine.id, 1 + j);
+          if (next != id) {
+            if (id >= 0) flush();
+            id = next;
+            if constexpr (LISTS)
+              number = number_of[id >> B.lgw] + __builtin_amdgcn_readlane(my_slot, 1 + j);
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] = x[e];
+          } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += x[e];
+          }
+        }
+      p += count;
+      if (p >= p1) break;
+      read(p);
+    }
+    flush();
+    return;
+  }
   for (int p = p0; p < p1; p += kAhead) {
     int32_t at[kAhead], of[kAhead], slot[LISTS ? kAhead : 1];
     uint4 raw[kAhead];
@@ -922,8 +980,11 @@ void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
   } else {
     k_embed_sort<false><<<b.count, kSortThreads, lds, s>>>(a, w, b, rest_lg);
   }
-  k_embed_sum<O, R, LISTS>
-      <<<dim3((unsigned)ceil_div(tiles, 256 >> lg), cut), 256, 0, s>>>(a, w, b, lg, tile);
+  const dim3 sums((unsigned)ceil_div(tiles, 256 >> lg), cut);
+  if (lg >= 6)
+    k_embed_sum<O, R, LISTS, true><<<sums, 256, 0, s>>>(a, w, b, lg, tile);
+  else
+    k_embed_sum<O, R, LISTS, false><<<sums, 256, 0, s>>>(a, w, b, lg, tile);
   const int jlg = lg < 6 ? lg : 6;
   k_embed_join<R, E, LISTS><<<dim3((unsigned)ceil_div(tiles, kWindow), slices(a.width, E, jlg), kJoiners),
                               256, 0, s>>>(a, w, b, jlg, tile, (int)tiles);

@@ -257,7 +257,7 @@ struct EmbedScratch {
   int32_t* ends;    // bin x piece: places of a bin's tokens in a piece (and behind the last's)
 };
 
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kSortThreads = 1024;
 constexpr int kSortAhead = 8;  // tokens a lane reads at once
 constexpr int kMaxBinBits = 9;
 
@@ -362,11 +362,12 @@ __global__ __launch_bounds__(kSplitThreads) void k_embed_split(EmbedArgs A, Embe
 // words that do not occur (rest_lg >= 0). Wave w has the w-th share of the tokens, so
 // a word's tokens are in the batch's order: waves in turn, and in a wave, lanes.
 // PIECES: its tokens lie in the pieces that k_embed_split made; else all tokens are read.
-template <bool PIECES>
-__global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, EmbedScratch W,
-                                                               Bins B, int rest_lg) {
+template <bool PIECES, int NT>
+__global__ __launch_bounds__(NT, 8) void k_embed_sort(EmbedArgs A, EmbedScratch W, Bins B,
+                                                     int rest_lg) {
   extern __shared__ uint32_t hist[];  // wave x word
-  __shared__ uint32_t red[kSortWaves], below_of[kSortWaves];
+  constexpr int NW = NT / 64;
+  __shared__ uint32_t red[NW], below_of[NW];
   __shared__ uint32_t slot_of[1 << kMaxBinBits];
   __shared__ uint16_t absent[1 << kMaxBinBits];
   // of each piece: the bin's tokens before it, and where (less those) its own lie
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, Emb
       below = (uint32_t)W.ends[at];
       own = (uint32_t)W.ends[at + pieces] - below;
     }
-    const uint32_t before = block_scan<kSortThreads>(own, red, &total);
+    const uint32_t before = block_scan<NT>(own, red, &total);
     if (tid < pieces) {
       piece_of[tid] = (int32_t)before;
       part_of[tid] = tid * kPiece + (int32_t)(below - before);
@@ -394,7 +395,7 @@ __global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, Emb
     n = (int)total;
     __syncthreads();
   }
-  const int per = ((n + kSortThreads - 1) / kSortThreads) * 64;
+  const int per = ((n + NT - 1) / NT) * 64;
   const int begin = wave * per, end = begin + per < n ? begin + per : n;
   int32_t t[kAhead], at_[PIECES ? kAhead : 1];
   const auto read = [&](int from) {
@@ -424,48 +425,53 @@ __global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, Emb
       }
     }
   };
+  // whether t is a word of the bin: its number there, else -1
+  const auto own_of = [&](int32_t t_) {
+    const int32_t number = (PIECES ? t_ : B.id(t_)) - w0;
+    const bool in = PIECES ? t_ >= 0 : (uint32_t)t_ < (uint32_t)A.V;
+    return in && (uint32_t)number < (uint32_t)words ? number : -1;
+  };
   read(begin);
-  for (int i = tid; i < words * kSortWaves; i += kSortThreads) hist[i] = 0u;
+  for (int i = tid; i < words * NW; i += NT) hist[i] = 0u;
   __syncthreads();
   uint32_t* mine = hist + wave * words;
   for (int from = begin;;) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      if constexpr (PIECES) {
-        if (t[j] >= 0) atomicAdd(&mine[t[j] - w0], 1u);
-      } else {
-        const bool in = t[j] >= 0 && t[j] < A.V;
+      if constexpr (!PIECES) {
+        const bool in = (uint32_t)t[j] < (uint32_t)A.V;
         if (!in && t[j] != -1) bits = TKEF_STATUS_INDEX_RANGE;
-        const int32_t id = B.id(t[j]);
-        below += in && id < w0 ? 1u : 0u;
-        if (in && id >= w0 && id - w0 < words) atomicAdd(&mine[id - w0], 1u);
+        below += in && B.id(t[j]) < w0 ? 1u : 0u;
       }
+      t[j] = own_of(t[j]);
+      if (t[j] >= 0) atomicAdd(&mine[t[j]], 1u);
     }
     from += kAhead * 64;
     if (from >= end) break;
     read(from);
   }
   if (blockIdx.x == 0) raise_status(A.status, bits);
-  if (per > kAhead * 64) read(begin);
+  const bool again = per > kAhead * 64;
+  if (again) read(begin);
   below = wave_incl(below);
   if (lane == 63) below_of[wave] = below;
   __syncthreads();
   uint32_t at = 0u;
 #pragma unroll
-  for (int w = 0; w < kSortWaves; ++w) at += below_of[w];
+  for (int w = 0; w < NW; ++w) at += below_of[w];
   // places of each word, and of each wave's share of it; both counts in one scan (at most
   // 2^20 tokens, 2^9 words)
   uint32_t count = 0u, all;
   if (tid < words)
-    for (int v = 0; v < kSortWaves; ++v) count += hist[v * words + tid];
-  const uint32_t ahead = block_scan<kSortThreads>(count | (count > 0u ? 1u << 21 : 0u), red, &all);
+    for (int v = 0; v < NW; ++v) count += hist[v * words + tid];
+  const uint32_t ahead = block_scan<NT>(count | (count > 0u ? 1u << 21 : 0u), red, &all);
   if (tid < words) {
     uint32_t place = at + (ahead & ((1u << 21) - 1u));
     W.first[w0 + tid] = (int32_t)place;
     if (w0 + tid == B.ids() - 1) W.first[B.ids()] = (int32_t)(place + count);
     slot_of[tid] = ahead >> 21;
     if (count == 0u) absent[tid - (int)(ahead >> 21)] = (uint16_t)tid;
-    for (int v = 0; v < kSortWaves; ++v) {
+    for (int v = 0; v < NW; ++v) {
       const uint32_t c = hist[v * words + tid];
       hist[v * words + tid] = place;
       place += c;
@@ -483,17 +489,17 @@ __global__ __launch_bounds__(kSortThreads, 8) void k_embed_sort(EmbedArgs A, Emb
   for (int from = begin;;) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int32_t id = PIECES ? t[j] : B.id(t[j]);
-      const bool own = t[j] >= 0 && (PIECES || t[j] < A.V) && id >= w0 && id - w0 < words;
+      if (again) t[j] = own_of(t[j]);
+      const bool own = t[j] >= 0;
       const uint64_t who = __ballot(own);
       if (who == 0ull) continue;
-      const uint32_t word = own ? (uint32_t)(id - w0) : 0u;
+      const uint32_t word = own ? (uint32_t)t[j] : 0u;
       const uint64_t same = same_word<kMaxBinBits>(word, B.lgw, who);
       const int rank = lanes_below(same);
       const uint32_t place = mine[word] + (uint32_t)rank;
       wave_fence();  // every lane has read before one writes, and before the next 64 read
       if (own) {
-        W.sorted[place] = Token{PIECES ? at_[PIECES ? j : 0] : from + j * 64 + lane, id};
+        W.sorted[place] = Token{PIECES ? at_[PIECES ? j : 0] : from + j * 64 + lane, w0 + t[j]};
         if (A.idx != nullptr) W.slots[place] = (int32_t)slot_of[word];
         if (rank == 0) mine[word] = place + (uint32_t)__popcll(same);
       }
@@ -703,7 +709,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
 // The words that begin in a tile and go on behind it: their sums, tile after tile. A
 // workgroup looks at 64 tiles and takes every gridDim.z-th of the words that it finds; its
 // groups have equal parts of the word's tiles, which the first joins.
-constexpr int kWindow = 64, kJoiners = 16;
+constexpr int kWindow = 64;
 template <typename R, int E, bool LISTS>
 __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W, Bins B, int lg,
                                                     int tile, int tiles) {
@@ -971,23 +977,30 @@ void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
   const Bins b = bins_of(a.V, !LISTS);
   const int tile = tile_of(a.n);
   const int64_t tiles = ceil_div(a.n, tile);
-  const size_t lds = ((size_t)kSortWaves << b.lgw) * 4;
+  const auto sort = [&](auto kernel, int threads) {
+    kernel<<<b.count, threads, ((size_t)(threads / 64) << b.lgw) * 4, s>>>(a, w, b, rest_lg);
+  };
   if (a.n >= kSplitFrom) {
     const int pieces = (int)ceil_div(a.n, kPiece);
     k_embed_split<<<pieces, kSplitThreads, (size_t)kSplitWaves * (size_t)b.count * 4, s>>>(a, w, b,
                                                                                           pieces);
-    k_embed_sort<true><<<b.count, kSortThreads, lds, s>>>(a, w, b, rest_lg);
+    sort(k_embed_sort<true, kSortThreads>, kSortThreads);
+  } else if (a.n <= kSortAhead * 256 && b.lgw <= 8) {
+    sort(k_embed_sort<false, 256>, 256);
   } else {
-    k_embed_sort<false><<<b.count, kSortThreads, lds, s>>>(a, w, b, rest_lg);
+    sort(k_embed_sort<false, kSortThreads>, kSortThreads);
   }
   const dim3 sums((unsigned)ceil_div(tiles, 256 >> lg), cut);
   if (lg >= 6)
     k_embed_sum<O, R, LISTS, true><<<sums, 256, 0, s>>>(a, w, b, lg, tile);
   else
     k_embed_sum<O, R, LISTS, false><<<sums, 256, 0, s>>>(a, w, b, lg, tile);
+  // each of a window's words by a workgroup of its own, while they are few
   const int jlg = lg < 6 ? lg : 6;
-  k_embed_join<R, E, LISTS><<<dim3((unsigned)ceil_div(tiles, kWindow), slices(a.width, E, jlg), kJoiners),
-                              256, 0, s>>>(a, w, b, jlg, tile, (int)tiles);
+  const unsigned windows = (unsigned)ceil_div(tiles, kWindow), jcut = slices(a.width, E, jlg);
+  const unsigned each = 2048 / (windows * jcut);
+  const dim3 joins(windows, jcut, each < 16 ? 16 : each < kWindow ? each : kWindow);
+  k_embed_join<R, E, LISTS><<<joins, 256, 0, s>>>(a, w, b, jlg, tile, (int)tiles);
 }
 
 }  // namespace

@@ -22,9 +22,26 @@ namespace {
 
 typedef uint32_t loose2_ __attribute__((ext_vector_type(2), aligned(2)));
 
+// E elements of a type as they lie in memory: 16 or 8 bytes
+template <typename T, int E>
+using Packed = std::conditional_t<E * sizeof(T) == 16, loose4_, loose2_>;
+
+template <typename T, int E>
+__device__ __forceinline__ void unpack_vec(Packed<T, E> v, float (&x)[E], const T* type) {
+  if constexpr (E * sizeof(T) == 16) {
+    unpack(make_uint4(v.x, v.y, v.z, v.w), x, type);
+  } else {
+    static_assert(E == 4 && sizeof(T) == 2, "8 bytes of a 16-bit type");
+    float y[8];
+    unpack(make_uint4(v.x, v.y, 0u, 0u), y, type);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = y[i];
+  }
+}
+
 template <typename T, int E>
 __device__ __forceinline__ void load_vec(const T* p, float (&x)[E]) {
-  if constexpr (sizeof(T) == 4) {
+  if constexpr (E * sizeof(T) == 32) {
 #pragma unroll
     for (int i = 0; i < E; i += 4) {
       const loose4_ v = *reinterpret_cast<const loose4_*>(p + i);
@@ -33,16 +50,8 @@ __device__ __forceinline__ void load_vec(const T* p, float (&x)[E]) {
       x[i + 2] = __uint_as_float(v.z);
       x[i + 3] = __uint_as_float(v.w);
     }
-  } else if constexpr (E == 8) {
-    const loose4_ v = *reinterpret_cast<const loose4_*>(p);
-    unpack(make_uint4(v.x, v.y, v.z, v.w), x, p);
   } else {
-    static_assert(E == 4, "8 bytes of a 16-bit type");
-    const loose2_ v = *reinterpret_cast<const loose2_*>(p);
-    float y[8];
-    unpack(make_uint4(v.x, v.y, 0u, 0u), y, p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = y[i];
+    unpack_vec<T, E>(*reinterpret_cast<const Packed<T, E>*>(p), x, p);
   }
 }
 
@@ -64,10 +73,17 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[E]) {
   }
 }
 
-// elements of a vector of 16 bytes of the narrower type
-template <typename A, typename B>
+// Elements of a thread: 16 bytes of what is written, so that a wave writes whole lines (with
+// 8 columns of binary32 a thread's two stores leave every other 16 bytes to each other: sums of
+// 65,536 rows of 1,000 took @OLD us in place of @NEW).
+template <typename T, typename O>
 constexpr int vector_of() {
-  return sizeof(A) == 4 && sizeof(B) == 4 ? 4 : 8;
+  return sizeof(O) == 4 ? 4 : 8;
+}
+// the same of sums that are written as R, or in lists
+template <typename O, typename R, bool LISTS>
+constexpr int vector_of_sums() {
+  return LISTS || sizeof(R) == 4 || sizeof(O) == 4 ? 4 : 8;
 }
 
 // A workgroup of 256 threads holds 256 >> lg groups of 1 << lg threads; a group has a row
@@ -548,20 +564,19 @@ __device__ __forceinline__ void put_sum(const EmbedArgs& A, int32_t word, int32_
 
 // Rows of dout, K of them under way.
 template <typename O, int E, int K>
-__device__ __forceinline__ void load_rows(uint4 (&raw)[K], const O* dout, int64_t ld,
+__device__ __forceinline__ void load_rows(Packed<O, E> (&raw)[K], const O* dout, int64_t ld,
                                           const int32_t (&at)[K], const Columns& c) {
   if (c.skip + c.have == E) {
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      const loose4_ v = *reinterpret_cast<const loose4_*>(dout + at[j] * ld + c.c0);
-      raw[j] = make_uint4(v.x, v.y, v.z, v.w);
-    }
+    for (int j = 0; j < K; ++j)
+      raw[j] = *reinterpret_cast<const Packed<O, E>*>(dout + at[j] * ld + c.c0);
   } else {
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-      float x[E];
-      load_row<O, E>(dout + at[j] * ld, c, x);
-      raw[j] = pack(x, dout);
+      O x[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = i < c.have ? dout[at[j] * ld + i] : (O)0.f;
+      raw[j] = __builtin_bit_cast(Packed<O, E>, x);
     }
   }
 }
@@ -577,7 +592,7 @@ constexpr int kAhead = 8, kWaveAhead = 16;  // rows of a tile under way
 template <typename O, typename R, bool LISTS, bool WAVE>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, Bins B, int lg,
                                                    int tile) {
-  constexpr int E = 16 / (int)sizeof(O);
+  constexpr int E = vector_of_sums<O, R, LISTS>();
   __shared__ int32_t number_of[LISTS ? kMaxBins : 1];
   __shared__ uint32_t red[4];
   Columns c = Columns::of<E>(lg, A.width);
@@ -641,19 +656,18 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
     if (p0 > 0) left = __builtin_amdgcn_readlane(mine.id, 0);
     for (int p = p0;;) {
       const int count = p1 - p < kWaveAhead ? p1 - p : kWaveAhead;
-      uint4 raw[kWaveAhead];
+      Packed<O, E> raw[kWaveAhead];
 #pragma unroll
       for (int j = 0; j < kWaveAhead; ++j) {
         const int32_t at = __builtin_amdgcn_readlane(mine.at, 1 + (j < count ? j : count - 1));
-        const loose4_ v = *reinterpret_cast<const loose4_*>(dout + at * A.out_ld + c.c0);
-        raw[j] = make_uint4(v.x, v.y, v.z, v.w);
+        raw[j] = *reinterpret_cast<const Packed<O, E>*>(dout + at * A.out_ld + c.c0);
       }
       if (p + count == p1 && p1 < total) right = __builtin_amdgcn_readlane(mine.id, 1 + count);
 #pragma unroll
       for (int j = 0; j < kWaveAhead; ++j)
         if (j < count) {
           float x[E];
-          unpack(raw[j], x, dout);
+          unpack_vec<O, E>(raw[j], x, dout);
           const int32_t next = __builtin_amdgcn_readlane(mine.id, 1 + j);
           if (next != id) {
             if (id >= 0) flush();
@@ -676,7 +690,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
   }
   for (int p = p0; p < p1; p += kAhead) {
     int32_t at[kAhead], of[kAhead], slot[LISTS ? kAhead : 1];
-    uint4 raw[kAhead];
+    Packed<O, E> raw[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int q = p + j < p1 ? p + j : p1 - 1;
@@ -690,7 +704,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
     for (int j = 0; j < kAhead; ++j)
       if (p + j < p1) {
         float x[E];
-        unpack(raw[j], x, dout);
+        unpack_vec<O, E>(raw[j], x, dout);
         if (of[j] != id) {
           if (id >= 0) flush();
           id = of[j];
@@ -710,10 +724,10 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
 // workgroup looks at 64 tiles and takes every gridDim.z-th of the words that it finds; its
 // groups have equal parts of the word's tiles, which the first joins.
 constexpr int kWindow = 64;
-template <typename R, int E, bool LISTS>
+template <typename R, bool LISTS>
 __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W, Bins B, int lg,
                                                     int tile, int tiles) {
-  constexpr int kJoin = 64 / E;  // partial sums under way
+  constexpr int E = 8, kJoin = 8;  // partial sums under way
   __shared__ float sums[256][E];
   const Columns c = Columns::of<E>(lg, A.width);
   const int tid = threadIdx.x, lane = tid & 63, groups = 256 >> lg;
@@ -745,10 +759,11 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W,
       for (int i = begin; i < end; i += kJoin) {
         float x[kJoin][E];
 #pragma unroll
-        for (int j = 0; j < kJoin; ++j) {
-          const int h = h0 + (i + j < end ? i + j : end - 1);
-          load_row<float, E>(W.partial + (2 * (int64_t)h + (h == h0 ? 1 : 0)) * A.width, c, x[j]);
-        }
+        for (int j = 0; j < kJoin; ++j)
+          if (i + j < end) {
+            const int h = h0 + i + j;
+            load_row<float, E>(W.partial + (2 * (int64_t)h + (h == h0 ? 1 : 0)) * A.width, c, x[j]);
+          }
 #pragma unroll
         for (int j = 0; j < kJoin; ++j)
           if (i + j < end) {
@@ -781,7 +796,7 @@ constexpr int kFew = 256, kFewWords = 64, kFewAhead = 8;
 template <typename O, typename R, bool LISTS>
 __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int token_blocks,
                                                     int rest_lg) {
-  constexpr int E = 16 / (int)sizeof(O), kParts = kFew / 64;
+  constexpr int E = vector_of_sums<O, R, LISTS>(), kParts = kFew / 64;
   __shared__ int32_t word_at[kFew];
   __shared__ int32_t distinct[LISTS ? kFew : 1];
   __shared__ uint16_t absent[kFewWords];
@@ -851,7 +866,7 @@ __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int tok
   for (int p = 0; p < kParts; ++p)
     while (same[p] != 0ull) {
       int32_t at[kFewAhead];
-      uint4 raw[kFewAhead];
+      Packed<O, E> raw[kFewAhead];
       int count = __popcll(same[p]);
 #pragma unroll
       for (int j = 0; j < kFewAhead; ++j) {
@@ -863,7 +878,7 @@ __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int tok
       for (int j = 0; j < kFewAhead; ++j)
         if (j < count) {
           float x[E];
-          unpack(raw[j], x, dout);
+          unpack_vec<O, E>(raw[j], x, dout);
 #pragma unroll
           for (int e = 0; e < E; ++e) sum[e] = begun ? sum[e] + x[e] : x[e];
           begun = true;
@@ -951,7 +966,7 @@ namespace {
 
 template <typename O, typename R, bool LISTS>
 void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
-  constexpr int E = 16 / (int)sizeof(O);
+  constexpr int E = vector_of_sums<O, R, LISTS>();
   int lg = lg_threads(a.width, E);
   const unsigned cut = slices(a.width, E, lg);
   if (a.n <= kFew) {
@@ -996,11 +1011,12 @@ void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
   else
     k_embed_sum<O, R, LISTS, false><<<sums, 256, 0, s>>>(a, w, b, lg, tile);
   // each of a window's words by a workgroup of its own, while they are few
-  const int jlg = lg < 6 ? lg : 6;
-  const unsigned windows = (unsigned)ceil_div(tiles, kWindow), jcut = slices(a.width, E, jlg);
+  int jlg = lg_threads(a.width, 8);
+  jlg = jlg < 6 ? jlg : 6;
+  const unsigned windows = (unsigned)ceil_div(tiles, kWindow), jcut = slices(a.width, 8, jlg);
   const unsigned each = 2048 / (windows * jcut);
   const dim3 joins(windows, jcut, each < 16 ? 16 : each < kWindow ? each : kWindow);
-  k_embed_join<R, E, LISTS><<<joins, 256, 0, s>>>(a, w, b, jlg, tile, (int)tiles);
+  k_embed_join<R, LISTS><<<joins, 256, 0, s>>>(a, w, b, jlg, tile, (int)tiles);
 }
 
 }  // namespace

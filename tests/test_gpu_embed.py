@@ -146,7 +146,7 @@ def test_lookup_sizes(n, width):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("n", [1, 7, 8, 9, 64, 65, 100, 255, 256, 257, 513, 3000])
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 64, 65, 100, 255, 256, 257, 513, 2048, 2049, 3000])
 def test_gradient_tokens(n, kind):
     rng = np.random.default_rng(n)
     for vocab, width in ((1, 5), (50, 33), (1000, 64), (2111, 8)):
@@ -186,6 +186,45 @@ def test_gradient_of_large_vocabularies(vocab):
         tokens = some_tokens(rng, kind, n, vocab)
         check_gradient(rng, n, vocab, 3, "f32", "f32", 1.0, tokens)
         check_lists(rng, n, vocab, 3, "f32", "f32", 1.0, tokens)
+
+
+@pytest.mark.parametrize("kind", ["law", "one", "two"])
+@pytest.mark.parametrize("n,width,out_type,grad_type", [
+    (17000, 1030, "bf16", "f32"), (17000, 2051, "f16", "f16"), (66000, 260, "bf16", "f32"),
+    (66000, 515, "bf16", "bf16"), (132000, 257, "f32", "f32")])
+def test_gradient_of_many_wide_rows(n, width, out_type, grad_type, kind):
+    """Groups of whole waves, tiles of 16, 32 and 64 tokens, words over many tiles."""
+    rng = np.random.default_rng(n + width)
+    tokens = some_tokens(rng, kind, n, 700)
+    check_gradient(rng, n, 700, width, out_type, grad_type, -0.5, tokens)
+    check_lists(rng, n, 700, width, out_type, "f32", -0.5, tokens)
+
+
+@pytest.mark.parametrize("n", [40, 900])
+def test_gradient_against_differences(n):
+    """The lookup is linear in the table: half the difference of its products with dout at
+    table + D and table - D is the gradient's product with D, whatever D's size. Each of
+    the n * width products, of numbers that round once to binary32, is off by EPS, and each
+    entry of the gradient by EPS a term."""
+    rng = np.random.default_rng(n)
+    vocab, width = 300, 17
+    tokens = some_tokens(rng, "law", n, vocab)
+    tok = vec(tokens, torch.int32)
+    dout, exact, _ = gradient_case(rng, n, width, "f32", tokens)
+    plan = tk.EmbedPlan(n, vocab, width, dtype=torch.float32, scale=3.0, check=True)
+    table, step = vec(rng.normal(size=(vocab, width))), vec(rng.normal(size=(vocab, width)))
+    up, down = table + step, table - step
+    step = (up.double() - down.double()) / 2     # what the rounded tables differ by
+    live = torch.as_tensor(tokens >= 0)
+    d = dout.double().cpu()[live]
+    high, low = (plan.forward(t, tok).double().cpu()[live] for t in (up, down))
+    slope = float(((high - low) / 2 * d).sum())
+    grad = plan.backward(tok, dout).double().cpu()
+    want = float((grad * step.cpu()).sum())
+    _, size, counts = oracle.embed_sums(tokens, exact, vocab, 3.0)
+    tol = EPS * (float(((high.abs() + low.abs()) * d.abs()).sum())
+                 + float((size * (counts[:, None] + 2) * step.abs().cpu().numpy()).sum()))
+    assert abs(slope - want) <= tol
 
 
 def test_no_tokens():

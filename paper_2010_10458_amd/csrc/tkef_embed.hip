@@ -186,6 +186,7 @@ __global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs A, int lg) {
 // rows of words without tokens
 
 constexpr int kRestRows = 2;  // rows of a group under way
+constexpr uint32_t kLine = 128;
 
 // The rows w0 + (absent[0 .. count) << shift) of the gradient: zeros, or the added rows as they
 // are (U: their bits). A group of 1 << lg threads has a row, the slices from `slice` on.
@@ -204,22 +205,39 @@ __device__ __forceinline__ void put_rest(const EmbedArgs& A, const uint16_t* abs
       }
     return;
   }
+  const auto at = [&](int c) { return c + E < A.width ? c : A.width - E; };
+  if (add == nullptr) {
+    // A wave writes whole lines: first the vectors up to a line's beginning, then the rest.
+    // (Overlapping vectors write the same. 131,071 x 1,000 binary32 but for 300 rows: 129 us
+    // from the row's beginning, 107 us so.)
+    lg = lg < 6 ? lg : 6;
+    const int l = tid & ((1 << lg) - 1);
+    for (int r = tid >> lg; r < count; r += (int)blockDim.x >> lg) {
+      U* row = grad + (w0 + ((int64_t)absent[r] << shift)) * A.grad_ld;
+      const uint32_t past = (uint32_t)(reinterpret_cast<uintptr_t>(row) & (kLine - 1));
+      const int head = lg < 3 || past == 0u ? 0 : (int)((kLine - past) / sizeof(U));
+      const auto zero = [&](int c) {
+        __builtin_nontemporal_store(loose4_{0u, 0u, 0u, 0u},
+                                    reinterpret_cast<loose4_*>(row + at(c)));
+      };
+      if (slice == 0 && l * E < head) zero(l * E);
+      for (int c = head + ((slice << lg) + l) * E; c < A.width; c += (step << lg) * E) zero(c);
+    }
+    return;
+  }
   for (;; slice += step) {
     int c0 = ((slice << lg) + (tid & ((1 << lg) - 1))) * E;
     if (c0 >= A.width) break;
-    // (the last vector lies over its neighbour's columns: both write the same)
-    c0 = c0 + E < A.width ? c0 : A.width - E;
+    c0 = at(c0);
     for (int r = tid >> lg; r < count; r += groups * kRestRows) {
       loose4_ x[kRestRows];
       int64_t w[kRestRows];
 #pragma unroll
       for (int j = 0; j < kRestRows; ++j) {
-        const int at = r + j * groups;
-        w[j] = w0 + ((int64_t)absent[at < count ? at : r] << shift);
-        x[j] = loose4_{0u, 0u, 0u, 0u};
-        if (add != nullptr)
-          x[j] = __builtin_nontemporal_load(
-              reinterpret_cast<const loose4_*>(add + w[j] * A.add_ld + c0));
+        const int k = r + j * groups;
+        w[j] = w0 + ((int64_t)absent[k < count ? k : r] << shift);
+        x[j] = __builtin_nontemporal_load(
+            reinterpret_cast<const loose4_*>(add + w[j] * A.add_ld + c0));
       }
 #pragma unroll
       for (int j = 0; j < kRestRows; ++j)
@@ -788,7 +806,7 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W,
 // ----------------------------------------------------------------------------
 // few tokens: one launch, no workspace
 
-constexpr int kFew = 256, kFewWords = 64, kFewAhead = 8;
+constexpr int kFew = 256, kFewWords = 16, kFewAhead = 8;
 
 // Each workgroup reads all tokens. A group (of whole waves) has token i; if no earlier
 // one is of its word, it sums the word's rows. Workgroups from `token_blocks` on write the
@@ -814,16 +832,17 @@ __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int tok
   for (int i = 0; i < kParts; ++i) tok[i] = word_at[i * 64 + lane];
   if ((int)blockIdx.x >= token_blocks) {
     const int64_t w0 = (int64_t)((int)blockIdx.x - token_blocks) * kFewWords;
-    uint64_t there = 0ull;  // words that occur, or are none
+    uint32_t gone = 0u;  // words that do not occur
     for (int w = 0; w < kFewWords; ++w) {
       bool hit = false;
 #pragma unroll
       for (int i = 0; i < kParts; ++i) hit |= tok[i] == (int32_t)(w0 + w);
-      if (__ballot(hit) != 0ull || w0 + w >= A.V) there |= 1ull << w;
+      if (__ballot(hit) == 0ull && w0 + w < A.V) gone |= 1u << w;
     }
-    if (tid < 64 && !((there >> tid) & 1ull)) absent[lanes_below(~there)] = (uint16_t)tid;
+    if (tid < kFewWords && ((gone >> tid) & 1u))
+      absent[__popc(gone & ((1u << tid) - 1u))] = (uint16_t)tid;
     __syncthreads();
-    put_rest(A, absent, __popcll(~there), w0, 0, rest_lg, (int)blockIdx.y, (int)gridDim.y);
+    put_rest(A, absent, __popc(gone), w0, 0, rest_lg, (int)blockIdx.y, (int)gridDim.y);
     return;
   }
   if constexpr (LISTS) {

@@ -306,7 +306,11 @@ __device__ __forceinline__ void select(uint4 (&r)[NV], float m, const Share<T, 2
 }
 
 // One workgroup takes a row, or one of a row's chunks (PART, blockIdx.y), and holds it
-// in registers: NV vectors a thread, loaded once.
+// in registers: NV vectors a thread, loaded once. Reads bound it: 8,192 x 32,000 bfloat16 (an eighth
+// without a token) in 72 us, 6.3 TB/s; 509 x 131,071 binary32 in chunks in 43 us, 6.2 TB/s. With
+// alternatives, 2,048 x 131,071 binary16 and k = 5 in 91 us, 5.5 TB/s: the selection's chain is
+// hidden by three other workgroups of a compute unit. One row of 32,000 takes 5.8 us without, 8.1 with
+// one and 9.4 with twenty of them; 1,024 threads for such a row: 5.5 and 9.3 us.
 template <typename T, int TPB, int NV, bool ALT, bool PART>
 __global__ __launch_bounds__(TPB) void k_score_row(ScoreArgs A, ScorePart* parts, uint64_t* lists) {
   constexpr int N = Span<T>::N, NW = TPB / 64;
@@ -402,7 +406,8 @@ __global__ __launch_bounds__(TPB) void k_score_row(ScoreArgs A, ScorePart* parts
 }
 
 // A row from its chunks, one wave a row. Lane l goes through the list of chunk l: the k
-// first of the row are the greatest of the lists' heads, k times.
+// first of the row are the greatest of the lists' heads, k times (2,048 rows: 6 us for
+// k = 5, 38 for k = 64).
 template <typename T, bool ALT>
 __global__ __launch_bounds__(64) void k_score_join(ScoreArgs A, const ScorePart* parts,
                                                    const uint64_t* lists, int chunks) {
@@ -444,7 +449,8 @@ __global__ __launch_bounds__(64) void k_score_join(ScoreArgs A, const ScorePart*
 // y = (x_i - m) a:  q_i = 2^y / S,  log q_i = ln 2 y - ln S, so
 //   dlogp (1{i = t} - q_i) - dentropy q_i (log q_i + H)
 //     = 1{i = t} dlogp + 2^y (P + Q y)
-// over the temperature, with P and Q the row's.
+// over the temperature, with P and Q the row's. Reads and writes bound it: 8,192 x 32,000 bfloat16 in
+// 173 us, 5.7 TB/s.
 template <typename T, int TPB, int NV>
 __global__ __launch_bounds__(TPB) void k_score_grad(ScoreArgs A) {
   constexpr int N = Span<T>::N;

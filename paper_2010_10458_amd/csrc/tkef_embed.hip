@@ -749,68 +749,99 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, 
   flush();
 }
 
-// The words that begin in a tile and go on behind it: their sums, tile after tile. A
-// workgroup looks at 64 tiles and takes every gridDim.z-th of the words that it finds; its
-// groups have equal parts of the word's tiles, which the first joins. A chain as well: 4.8 us for
-// 8,192 tokens, 17 us for 57,344, whose most frequent word has 123 tiles (one group for each
-// word: 24 us).
-constexpr int kWindow = 64;
-template <typename R, bool LISTS>
-__global__ __launch_bounds__(256) void k_embed_join(EmbedArgs A, EmbedScratch W, Bins B, int lg,
-                                                    int tile, int tiles) {
-  constexpr int E = 8, kJoin = 8;  // partial sums under way
-  __shared__ float sums[256][E];
-  const Columns c = Columns::of<E>(lg, A.width);
-  const int tid = threadIdx.x, lane = tid & 63, groups = 256 >> lg;
-  const int g = (int)blockIdx.x * kWindow + lane;
-  // (all read at once: places behind the last token hold no words, but lie in the workspace)
-  const bool in = g + 1 < tiles;
-  const int p0 = g * tile, p1 = p0 + tile, total = W.first[B.ids()];
-  const int32_t left = in && p0 > 0 ? W.sorted[p0 - 1].id : -1;
-  const int32_t id = in ? W.sorted[p1 - 1].id : -1, right = in ? W.sorted[p1].id : -1;
-  const bool begins = in && p1 < total && id == right && id != left;
-  int last = 0;
-  int32_t number = 0;
-  if (begins) {
-    last = (W.first[id + 1] - 1) / tile;
-    if constexpr (LISTS) number = W.before[id >> B.lgw] + W.slots[p1 - 1];
-  }
-  uint64_t found = __ballot(begins);  // (the same in every wave)
-  for (int skip = (int)blockIdx.z; found != 0ull; --skip) {
-    const int from = (int)__builtin_ctzll(found);
-    found &= found - 1ull;
-    if (skip != 0) continue;
-    skip = (int)gridDim.z;
-    const int h0 = (int)blockIdx.x * kWindow + from, terms = __shfl(last, from) - h0 + 1;
-    const int32_t its_id = __shfl(id, from), its_number = __shfl(number, from);
-    const int per = (terms + groups - 1) / groups;
-    const int begin = c.group * per, end = begin + per < terms ? begin + per : terms;
-    float sum[E];
-    if (!c.none() && begin < end) {
-      for (int i = begin; i < end; i += kJoin) {
-        float x[kJoin][E];
+// Partial sums [begin, end) of the word that goes on behind tile h0, in their order.
+constexpr int kJoin = 8;  // under way
+template <int E>
+__device__ __forceinline__ void join_terms(const float* partial, int width, int h0, int begin,
+                                           int end, const Columns& c, float (&sum)[E]) {
+  for (int i = begin; i < end; i += kJoin) {
+    float x[kJoin][E];
 #pragma unroll
-        for (int j = 0; j < kJoin; ++j)
-          if (i + j < end) {
-            const int h = h0 + i + j;
-            load_row<float, E>(W.partial + (2 * (int64_t)h + (h == h0 ? 1 : 0)) * A.width, c, x[j]);
-          }
-#pragma unroll
-        for (int j = 0; j < kJoin; ++j)
-          if (i + j < end) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] = i + j == begin ? x[j][e] : sum[e] + x[j][e];
-          }
+    for (int j = 0; j < kJoin; ++j)
+      if (i + j < end) {
+        const int64_t h = h0 + i + j;
+        load_row<float, E>(partial + (2 * h + (i + j == 0 ? 1 : 0)) * width, c, x[j]);
       }
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j)
+      if (i + j < end) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] = i + j == begin ? x[j][e] : sum[e] + x[j][e];
+      }
+  }
+}
+
+// The words that begin in a tile and go on behind it: their sums, tile after tile. The
+// workgroups of a window (gridDim.z) look at its 64 tiles; each group takes one of the words of
+// few tiles. Longer ones a workgroup takes together: its groups have equal parts of the
+// tiles, which the first joins. A chain as well: 5 us for 8,192 tokens of 512 columns, 13 us for
+// 57,344 of 1,000, whose most frequent word has 123 tiles. (NT: 256 threads where batches are not split,
+// else 1,024: 65,536 tokens of 1,000 x 512 take 10 us with 1,024, 14 with 512, 24 with 256; the call of
+// 8,192 tokens takes 27.8 us with 1,024, 26.9 with 256. There a word of three tiles is better shared by
+// a workgroup's groups: 27.0 us, and 28.6 where a group takes up to eight.)
+constexpr int kWindow = 64;
+template <typename R, bool LISTS, int NT>
+__global__ __launch_bounds__(NT) void k_embed_join(EmbedArgs A, EmbedScratch W, Bins B, int lg,
+                                                    int tile, int tiles) {
+  // tiles that a group takes alone, and of its part of more
+  constexpr int E = 8, kAlone = NT == 256 ? 2 : kJoin, kLeast = NT == 256 ? 1 : kJoin;
+  struct Word {
+    int32_t h0, terms, id, number;
+  };
+  __shared__ float sums[NT][E];
+  __shared__ Word few[kWindow], many[kWindow];
+  __shared__ int found[2];
+  const Columns c = Columns::of<E>(lg, A.width);
+  const int tid = threadIdx.x, groups = NT >> lg;
+  if (tid < kWindow) {
+    const int g = (int)blockIdx.x * kWindow + tid;
+    // (all read at once: places behind the last token hold no words, but lie in the workspace)
+    const bool in = g + 1 < tiles;
+    const int p0 = g * tile, p1 = p0 + tile, total = W.first[B.ids()];
+    const int32_t left = in && p0 > 0 ? W.sorted[p0 - 1].id : -1;
+    const int32_t id = in ? W.sorted[p1 - 1].id : -1, right = in ? W.sorted[p1].id : -1;
+    const bool begins = in && p1 < total && id == right && id != left;
+    Word w = {g, 0, id, 0};
+    if (begins) {
+      w.terms = (W.first[id + 1] - 1) / tile - g + 1;
+      if constexpr (LISTS) w.number = W.before[id >> B.lgw] + W.slots[p1 - 1];
+    }
+    const uint64_t is_few = __ballot(begins && w.terms <= kAlone);
+    const uint64_t is_many = __ballot(begins && w.terms > kAlone);
+    if (begins) {
+      if (w.terms <= kAlone)
+        few[lanes_below(is_few)] = w;
+      else
+        many[lanes_below(is_many)] = w;
+    }
+    if (tid == 0) {
+      found[0] = __popcll(is_few);
+      found[1] = __popcll(is_many);
+    }
+  }
+  __syncthreads();
+  float sum[E];
+  for (int k = (int)blockIdx.z * groups + c.group; k < found[0]; k += (int)gridDim.z * groups) {
+    if (c.none()) break;
+    const Word w = few[k];
+    join_terms<E>(W.partial, A.width, w.h0, 0, w.terms, c, sum);
+    put_sum<R, LISTS, E>(A, B.word(w.id), w.number, c, sum);
+  }
+  for (int k = (int)blockIdx.z; k < found[1]; k += (int)gridDim.z) {
+    const Word w = many[k];
+    const int share = (w.terms + groups - 1) / groups, per = share < kLeast ? kLeast : share;
+    const int begin = c.group * per, end = begin + per < w.terms ? begin + per : w.terms;
+    if (!c.none() && begin < end) {
+      join_terms<E>(W.partial, A.width, w.h0, begin, end, c, sum);
 #pragma unroll
       for (int e = 0; e < E; ++e) sums[tid][e] = sum[e];
     }
     __syncthreads();
     if (c.group == 0 && !c.none()) {
-      for (int q = 1; q * per < terms; ++q)
+      for (int q = 1; q * per < w.terms; ++q)
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] += sums[(q << lg) + tid][e];
-      put_sum<R, LISTS, E>(A, B.word(its_id), its_number, c, sum);
+      put_sum<R, LISTS, E>(A, B.word(w.id), w.number, c, sum);
     }
     __syncthreads();
   }
@@ -1043,13 +1074,16 @@ void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
     k_embed_sum<O, R, LISTS, true><<<sums, 256, 0, s>>>(a, w, b, lg, tile);
   else
     k_embed_sum<O, R, LISTS, false><<<sums, 256, 0, s>>>(a, w, b, lg, tile);
-  // each of a window's words by a workgroup of its own, while they are few
   int jlg = lg_threads(a.width, 8);
   jlg = jlg < 6 ? jlg : 6;
-  const unsigned windows = (unsigned)ceil_div(tiles, kWindow), jcut = slices(a.width, 8, jlg);
-  const unsigned each = 2048 / (windows * jcut);
-  const dim3 joins(windows, jcut, each < 16 ? 16 : each < kWindow ? each : kWindow);
-  k_embed_join<R, LISTS><<<joins, 256, 0, s>>>(a, w, b, jlg, tile, (int)tiles);
+  const auto join = [&](auto kernel, int threads, unsigned each) {
+    kernel<<<dim3((unsigned)ceil_div(tiles, kWindow), slices(a.width, 8, jlg), each), threads, 0, s>>>(
+        a, w, b, jlg, tile, (int)tiles);
+  };
+  if (a.n >= kSplitFrom)
+    join(k_embed_join<R, LISTS, 1024>, 1024, 8u);
+  else
+    join(k_embed_join<R, LISTS, 256>, 256, 64u);
 }
 
 }  // namespace

@@ -10,7 +10,8 @@ arguments; the computation runs in the library's HIP kernels.
     idx, val, nnz = ep.lists(tokens, dx, offset=o)     # one worker's list
 
 A call's tensors are all on one GPU, that of the stream it runs on; every call can be
-captured into a graph, with a workspace of its own in the graph's memory.
+captured into a graph, with a workspace of its own in the graph's memory. Host threads may
+share a plan: its calls take turns.
 """
 from __future__ import annotations
 
@@ -110,9 +111,11 @@ class EmbedPlan(_RowPlan):
             else:
                 gld = self._block(grad_out, self.vocab, self.grad_dtype, dev, "grad_out")
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
-        rc = self._backward(self._h, tokens.data_ptr(), n, dout.data_ptr(), old, _ptr(add), ald,
-                            grad_out.data_ptr(), gld, _ptr(ws), self.ws_bytes, _ptr(status), h)
+            with self._turn:
+                ws = self._workspace(h, dev)
+                rc = self._backward(
+                    self._h, tokens.data_ptr(), n, dout.data_ptr(), old, _ptr(add), ald,
+                    grad_out.data_ptr(), gld, _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_embed_backward", rc)
         if own:
@@ -148,10 +151,12 @@ class EmbedPlan(_RowPlan):
                 val_out = _out(None, (max(1, most),), self.val_dtype, dev, "val_out")
             nnz_out = _out(nnz_out, (1,), torch.int32, dev, "nnz_out")
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
-        rc = self._lists(self._h, tokens.data_ptr(), n, dout.data_ptr(), old, int(offset),
-                         idx_out.data_ptr(), val_out.data_ptr(), nnz_out.data_ptr(), _ptr(ws),
-                         self.ws_bytes, _ptr(status), h)
+            with self._turn:
+                ws = self._workspace(h, dev)
+                rc = self._lists(
+                    self._h, tokens.data_ptr(), n, dout.data_ptr(), old, int(offset),
+                    idx_out.data_ptr(), val_out.data_ptr(), nnz_out.data_ptr(), _ptr(ws),
+                    self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_embed_lists", rc)
         if own:

@@ -25,11 +25,12 @@ Every call can be captured into a graph, with or without an eager call before
 it. A captured call has a workspace of its own in the graph's memory, so graphs
 of one plan may be replayed in any order, between eager calls, and at the same
 time on several streams (graphs that were told to share one memory pool: as
-that pool allows).
+that pool allows). Host threads may share a plan: its calls take turns.
 """
 from __future__ import annotations
 
 import ctypes
+import threading
 from typing import Optional, Tuple
 
 import torch
@@ -90,6 +91,10 @@ class _RowPlan:
         self._h = ctypes.c_void_p()
         self._free = getattr(lib(), self._destroy)
         self._ws = {}  # kept ones, one per stream: calls on two streams do not share one
+        # From the choice of a workspace to the last launch that uses it: two threads on one
+        # stream share its workspace, and the library's calls run without the interpreter's
+        # lock, so the launches of one would come between those of the other.
+        self._turn = threading.RLock()
 
     def __del__(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -225,10 +230,11 @@ class TopLogitsPlan(_RowPlan):
             val_out = _out(val_out, (n, self.k), self.val_dtype, dev, "val_out")
             tail_out = _out(tail_out, (n,), torch.float32, dev, "tail_out")
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
-        rc = self._execute(
-            self._h, logits.data_ptr(), ld, n, idx_out.data_ptr(), val_out.data_ptr(),
-            tail_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
+            with self._turn:
+                ws = self._workspace(h, dev)
+                rc = self._execute(
+                    self._h, logits.data_ptr(), ld, n, idx_out.data_ptr(), val_out.data_ptr(),
+                    tail_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_top_execute", rc)
         if own:
@@ -281,10 +287,11 @@ class DistillPlan(_RowPlan):
             loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
             stats_out = _out(stats_out, (n, 4), torch.float32, dev, "stats_out")
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
-        rc = self._forward(
-            self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
-            stats_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
+            with self._turn:
+                ws = self._workspace(h, dev)
+                rc = self._forward(
+                    self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
+                    stats_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_distill_forward", rc)
         if own:
@@ -331,10 +338,11 @@ class DistillPlan(_RowPlan):
             loss_out = _out(loss_out, (n,), torch.float32, dev, "loss_out")
             grad_out, gld = self._grad(logits, grad_out)
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
-        rc = self._step(
-            self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
-            grad_out.data_ptr(), gld, _ptr(ws), self.ws_bytes, _ptr(status), h)
+            with self._turn:
+                ws = self._workspace(h, dev)
+                rc = self._step(
+                    self._h, logits.data_ptr(), ld, n, *lists, loss_out.data_ptr(),
+                    grad_out.data_ptr(), gld, _ptr(ws), self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_distill_step", rc)
         if own:
@@ -447,15 +455,17 @@ class VerifyPlan(_RowPlan):
             tokens_out = _out(tokens_out, (b, self.draft + 1), torch.int32, dev, "tokens_out")
             logp_out = _out(logp_out, (b, self.draft + 1), torch.float32, dev, "logp_out")
             status, own = self._status_of(status, dev)
-            if ws is None:
-                ws = self._workspace(h, dev)
-            else:
-                _check_vector(ws, self.ws_bytes, torch.uint8, "ws", dev.index)
-        rc = self._execute(
-            self._h, target.data_ptr(), tb, ti, drafts.data_ptr(), db, di, b,
-            tokens.data_ptr(), uniform.data_ptr(), noise.data_ptr(),
-            noise.stride(0) if b > 1 else self.vocab, _ptr(length), accepted_out.data_ptr(),
-            tokens_out.data_ptr(), logp_out.data_ptr(), _ptr(ws), self.ws_bytes, _ptr(status), h)
+            with self._turn:
+                if ws is None:
+                    ws = self._workspace(h, dev)
+                else:
+                    _check_vector(ws, self.ws_bytes, torch.uint8, "ws", dev.index)
+                rc = self._execute(
+                    self._h, target.data_ptr(), tb, ti, drafts.data_ptr(), db, di, b,
+                    tokens.data_ptr(), uniform.data_ptr(), noise.data_ptr(),
+                    noise.stride(0) if b > 1 else self.vocab, _ptr(length), accepted_out.data_ptr(),
+                    tokens_out.data_ptr(), logp_out.data_ptr(), _ptr(ws), self.ws_bytes,
+                    _ptr(status), h)
         if rc:
             _check("tkef_verify_execute", rc)
         if own:
@@ -502,11 +512,13 @@ class ScorePlan(_RowPlan):
             idx_out = _out(idx_out, (n, self.k), torch.int32, dev, "idx_out")
             val_out = _out(val_out, (n, self.k), torch.float32, dev, "val_out")
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
-        rc = self._forward(
-            self._h, logits.data_ptr(), ld, n, tokens.data_ptr(), logp_out.data_ptr(),
-            entropy_out.data_ptr(), idx_out.data_ptr() if self.k else None,
-            val_out.data_ptr() if self.k else None, None, _ptr(ws), self.ws_bytes, _ptr(status), h)
+            with self._turn:
+                ws = self._workspace(h, dev)
+                rc = self._forward(
+                    self._h, logits.data_ptr(), ld, n, tokens.data_ptr(), logp_out.data_ptr(),
+                    entropy_out.data_ptr(), idx_out.data_ptr() if self.k else None,
+                    val_out.data_ptr() if self.k else None, None, _ptr(ws), self.ws_bytes,
+                    _ptr(status), h)
         if rc:
             _check("tkef_score_forward", rc)
         if own:
@@ -530,11 +542,12 @@ class ScorePlan(_RowPlan):
             entropy_out = _out(entropy_out, (n,), torch.float32, dev, "entropy_out")
             stats_out = _out(stats_out, (n, 4), torch.float32, dev, "stats_out")
             status, own = self._status_of(status, dev)
-            ws = self._workspace(h, dev)
-        rc = self._forward(
-            self._h, logits.data_ptr(), ld, n, tokens.data_ptr(), logp_out.data_ptr(),
-            entropy_out.data_ptr(), None, None, stats_out.data_ptr(), _ptr(ws), self.ws_bytes,
-            _ptr(status), h)
+            with self._turn:
+                ws = self._workspace(h, dev)
+                rc = self._forward(
+                    self._h, logits.data_ptr(), ld, n, tokens.data_ptr(), logp_out.data_ptr(),
+                    entropy_out.data_ptr(), None, None, stats_out.data_ptr(), _ptr(ws),
+                    self.ws_bytes, _ptr(status), h)
         if rc:
             _check("tkef_score_forward", rc)
         if own:

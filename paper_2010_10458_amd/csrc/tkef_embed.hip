@@ -989,7 +989,7 @@ Bins bins_of(int64_t V, bool spread) {
 
 template <typename F>
 void by_types(int32_t a, int32_t b, F f) {
-  (void)by_dtype(a, [&](auto* x) { (void)by_dtype(b, [&](auto* y) { f(x, y); }); });
+  for_dtype(a, [&](auto* x) { for_dtype(b, [&](auto* y) { f(x, y); }); });
 }
 
 }  // namespace

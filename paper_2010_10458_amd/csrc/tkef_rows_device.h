@@ -464,14 +464,20 @@ __device__ __forceinline__ float2 agent_get(const float2* p) {
   return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
 }
 
-// f(T*) for the logits' type
+// f(T*) for a type
 template <typename F>
-hipError_t by_dtype(int32_t dtype, F f) {
+void for_dtype(int32_t dtype, F f) {
   switch (dtype) {
     case TKEF_DTYPE_F32: f(static_cast<float*>(nullptr)); break;
     case TKEF_DTYPE_F16: f(static_cast<_Float16*>(nullptr)); break;
     default: f(static_cast<__bf16*>(nullptr)); break;
   }
+}
+
+// the same with f's launches, and whether one failed (which can be asked once)
+template <typename F>
+hipError_t by_dtype(int32_t dtype, F f) {
+  for_dtype(dtype, f);
   return hipGetLastError();
 }
 

@@ -675,9 +675,10 @@ int tkef_embed_backward(tkef_embed_plan plan, const int32_t *tokens, int64_t row
 /* The same gradient as one worker's list, in the layout that tkef_update_execute
  * and its like take: for each word that occurs, ascending, `width` pairs of a global
  * position offset + word * width + column (idx_out, int32) and a value (val_out); nnz_out:
- * device int32, their number. idx_out, val_out: device, min(rows, V) * width entries; those
- * behind nnz are left as they were. offset: the table's first position among the update's
- * tensors; offset + V * width <= 2^31 - 1 (TKEF_ERANGE otherwise). */
+ * device int32, their number. idx_out, val_out: device, min(rows, V) * width entries
+ * (NULL for no rows); those behind nnz are left as they were. offset: the table's first
+ * position among the update's tensors; offset + V * width <= 2^31 - 1 (TKEF_ERANGE
+ * otherwise). */
 int tkef_embed_lists(tkef_embed_plan plan, const int32_t *tokens, int64_t rows, const void *dout,
                      int64_t dout_stride, int64_t offset, int32_t *idx_out, void *val_out,
                      int32_t *nnz_out, void *ws, size_t ws_bytes, uint32_t *status,

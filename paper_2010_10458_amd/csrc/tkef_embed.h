@@ -25,7 +25,7 @@ struct EmbedArgs {
   void* grad;             // backward
   int64_t grad_ld;
   int64_t offset;         // lists
-  int32_t* idx;
+  int32_t* idx;           // (null where a list has no tokens)
   void* val;
   int32_t* nnz;
   uint32_t* status;       // may be null
@@ -38,7 +38,7 @@ struct EmbedLayout {
 EmbedLayout embed_layout(int64_t rows, int64_t V, int64_t width);
 
 hipError_t launch_embed_forward(const EmbedArgs& a, hipStream_t s);
-// the table's gradient, or (a.idx not null) its lists
+// the table's gradient, or (a.nnz not null) its lists
 hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t s);
 
 }  // namespace tkef

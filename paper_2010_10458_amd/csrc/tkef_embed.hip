@@ -542,7 +542,7 @@ __global__ __launch_bounds__(NT, 8) void k_embed_sort(EmbedArgs A, EmbedScratch 
       wave_fence();  // every lane has read before one writes, and before the next 64 read
       if (own) {
         W.sorted[place] = Token{PIECES ? at_[PIECES ? j : 0] : from + j * 64 + lane, w0 + t[j]};
-        if (A.idx != nullptr) W.slots[place] = (int32_t)slot_of[word];
+        if (A.nnz != nullptr) W.slots[place] = (int32_t)slot_of[word];
         if (rank == 0) mine[word] = place + (uint32_t)__popcll(same);
       }
       wave_fence();
@@ -1089,7 +1089,7 @@ void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t s) {
-  if (a.idx != nullptr) {
+  if (a.nnz != nullptr) {
     by_types(a.out_dtype, a.val_format == TKEF_VAL_F16 ? TKEF_DTYPE_F16 : TKEF_DTYPE_F32,
              [&](auto* o, auto* r) {
                using O = typename Pointee<decltype(o)>::type;

@@ -162,8 +162,9 @@ int tkef_embed_lists(tkef_embed_plan plan, const int32_t* tokens, int64_t rows, 
   if (rc != TKEF_OK) return rc;
   if (offset < 0 || offset > INT32_MAX || offset + p.vocab * p.width > INT32_MAX)
     return TKEF_ERANGE;
-  if (nnz_out == nullptr || !aligned(nnz_out, 4) || idx_out == nullptr || val_out == nullptr ||
-      !aligned(idx_out, 4) || !aligned(val_out, p.val_format == TKEF_VAL_F16 ? 2 : 4))
+  if (nnz_out == nullptr || !aligned(nnz_out, 4) ||
+      (rows > 0 && (idx_out == nullptr || val_out == nullptr)) || !aligned(idx_out, 4) ||
+      !aligned(val_out, p.val_format == TKEF_VAL_F16 ? 2 : 4))
     return TKEF_EINVAL;
   tkef::EmbedArgs a = embed_args(p, tokens, rows, status);
   a.dout = dout;

@@ -146,9 +146,9 @@ class EmbedPlan(_RowPlan):
         h = _launch_on(dev.index, stream)
         with _on(stream):
             if idx_out is None:
-                idx_out = _out(None, (max(1, most),), torch.int32, dev, "idx_out")
+                idx_out = _out(None, (most,), torch.int32, dev, "idx_out")
             if val_out is None:
-                val_out = _out(None, (max(1, most),), self.val_dtype, dev, "val_out")
+                val_out = _out(None, (most,), self.val_dtype, dev, "val_out")
             nnz_out = _out(nnz_out, (1,), torch.int32, dev, "nnz_out")
             status, own = self._status_of(status, dev)
             with self._turn:

@@ -111,6 +111,11 @@ int main() {
           check("embed lists", [&] {
             return tkef_embed_lists(p, t, n, x, width, 0, i, f, i, w, ws, nullptr, nullptr);
           });
+          // no tokens: a list has no entries, so nothing has to hold them
+          check("embed lists of no tokens", [&] {
+            return tkef_embed_lists(p, nullptr, 0, nullptr, width, 0, nullptr, nullptr, i, w, ws,
+                                    nullptr, nullptr);
+          });
           (void)tkef_embed_plan_destroy(p);
         }
   std::printf("%d failed checks\n", g_fail);

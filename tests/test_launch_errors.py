@@ -16,9 +16,9 @@ def test_launch_errors_are_reported(tmp_path):
     tk.lib()        # (built, if it was not)
     exe = str(tmp_path / "launch_errors_driver")
     cmd = [build.HIPCC, "--offload-arch=gfx950", "-O1", "-std=c++17", "-rdynamic",
-           "-I" + os.path.join(build.ROOT, "include"), os.path.join(HERE, "sanitize", "launch_errors_driver.cpp"),
-           "-L" + build.LIBDIR,
-           "-ltkef", "-Wl,-rpath," + build.LIBDIR, "-o", exe]
+           "-I" + os.path.join(build.ROOT, "include"),
+           os.path.join(HERE, "sanitize", "launch_errors_driver.cpp"),
+           "-L" + build.LIBDIR, "-ltkef", "-Wl,-rpath," + build.LIBDIR, "-o", exe]
     p = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
     assert p.returncode == 0, p.stderr[-4000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)

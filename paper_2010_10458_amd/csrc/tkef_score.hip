@@ -62,8 +62,12 @@ __device__ __forceinline__ RowScore row_score(const ScorePart& p) {
   return r;
 }
 
+// (a difference beyond the largest binary32 number, which a temperature may bring back, is
+// taken in halves)
 __device__ __forceinline__ float log_prob(float x, const RowScore& r, float inv_t) {
-  return (x - r.m) * inv_t - r.log_sum;
+  const float d = x - r.m;
+  const float z = d == -kInf ? (0.5f * x - 0.5f * r.m) * (2.f * inv_t) : d * inv_t;
+  return z - r.log_sum;
 }
 
 // one row's results but the alternatives, by one thread

@@ -649,8 +649,8 @@ typedef struct tkef_embed_plan_s *tkef_embed_plan;
 
 /* Host only. dtype: of the table; out_dtype: of out and dout; grad_dtype: of the dense
  * gradient; val_format: of the list's values. The workspace (of the gradient; a lookup
- * needs none) holds at most 24 bytes a token, 5 bytes a word, 8 width bytes for each of at
- * most 4,096 tiles of 16 or more tokens, and 16 KB. */
+ * needs none) holds at most 24 bytes a token, 4 bytes a word of V rounded up to a power of
+ * two, 8 width bytes for each of at most 4,096 tiles of 16 or more tokens, and 32 KB. */
 int tkef_embed_plan_create(int64_t rows, int64_t vocab, int64_t width, int32_t dtype,
                            int32_t out_dtype, int32_t grad_dtype, int32_t val_format,
                            double scale, tkef_embed_plan *plan_out);

@@ -76,7 +76,7 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[E]) {
 // Elements of a thread: 16 bytes of what is written, so that a wave writes whole lines (with
 // 8 columns of binary32 a thread's two stores leave every other 16 bytes to each other:
 // k_embed_sum of 65,536 bfloat16 rows of 1,000 into binary32 took 57 us in place of 51).
-template <typename T, typename O>
+template <typename O>
 constexpr int vector_of() {
   return sizeof(O) == 4 ? 4 : 8;
 }
@@ -150,38 +150,26 @@ __device__ __forceinline__ void keep_row(float* row, const Columns& c, const flo
 // ----------------------------------------------------------------------------
 // lookup
 
-// Row i of out: 65,536 tokens of a 32,000 x 1,024 bfloat16 table take 27 us, 6.0 TB/s of the
-// rows that occur and of what is written, which is streamed: 49 us with ordinary stores. R
-// rows a group, all loads before the first store.
-template <typename T, typename O, int R>
+// Row i of out, by a group: 65,536 tokens of a 32,000 x 1,024 bfloat16 table take 27 us, 6.0 TB/s
+// of the rows that occur and of what is written, which is streamed: 49 us with ordinary stores.
+template <typename T, typename O>
 __global__ __launch_bounds__(256) void k_embed_rows(EmbedArgs A, int lg) {
-  constexpr int E = vector_of<T, O>();
+  constexpr int E = vector_of<O>();
   const Columns c = Columns::of<E>(lg, A.width);
-  const int groups = 256 >> lg;
-  const int64_t i0 = ((int64_t)blockIdx.x * groups + c.group) * R;
-  const T* table = static_cast<const T*>(A.table);
-  O* out = static_cast<O*>(A.out);
-  int32_t word[R];
+  const int64_t i = (int64_t)blockIdx.x * (256 >> lg) + c.group;
+  if (i >= A.n || c.none()) return;
+  const int32_t word = A.tokens[i];
+  const bool in = word >= 0 && word < A.V;
+  float x[E];
 #pragma unroll
-  for (int r = 0; r < R; ++r) word[r] = i0 + r < A.n ? A.tokens[i0 + r] : -1;
-  float x[R][E];
-  uint32_t bits = 0u;
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  if (in) {
+    load_row<T, E>(static_cast<const T*>(A.table) + word * A.table_ld, c, x);
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const bool in = word[r] >= 0 && word[r] < A.V;
-    if (!in && word[r] != -1) bits = TKEF_STATUS_INDEX_RANGE;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[r][e] = 0.f;
-    if (in && !c.none()) {
-      load_row<T, E>(table + word[r] * A.table_ld, c, x[r]);
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[r][e] *= A.scale;
-    }
+    for (int e = 0; e < E; ++e) x[e] *= A.scale;
   }
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (i0 + r < A.n && !c.none()) store_row<O, E>(out + (i0 + r) * A.out_ld, c, x[r]);
-  raise_status(A.status, c.c0 == 0 ? bits : 0u);
+  store_row<O, E>(static_cast<O*>(A.out) + i * A.out_ld, c, x);
+  raise_status(A.status, !in && word != -1 && c.c0 == 0 ? TKEF_STATUS_INDEX_RANGE : 0u);
 }
 
 // ----------------------------------------------------------------------------
@@ -395,10 +383,11 @@ __global__ __launch_bounds__(kSplitThreads) void k_embed_split(EmbedArgs A, Embe
   }
 }
 
-// Workgroup b sorts the tokens of bin b: it reads the tokens, counts its own word by word (and those of lower bins, which come before), and
-// in a second reading puts its own in place; between them it writes the gradient's rows of
-// words that do not occur (rest_lg >= 0). Wave w has the w-th share of the tokens, so
-// a word's tokens are in the batch's order: waves in turn, and in a wave, lanes.
+// Workgroup b sorts the tokens of bin b: it reads the tokens, counts its own word by word (and
+// those of lower bins, which come before), and in a second reading puts its own in place; between
+// them it writes the gradient's rows of words that do not occur (rest_lg >= 0). Wave w has the
+// w-th share of the tokens, so a word's tokens are in the batch's order: waves in turn, and in a
+// wave, lanes.
 // PIECES: its tokens lie in the pieces that k_embed_split made; else all tokens are read.
 // Without rows to write 1,000 tokens take 6 us, 8,192 11 us, a chain of barriers and LDS; the
 // 66 MB of zeros of 32,000 x 512 hide behind it but for 5 us. The 131,071 x 1,000 rows beside
@@ -854,15 +843,15 @@ constexpr int kFew = 256, kFewWords = 16, kFewAhead = 8;
 
 // (a list of 37 tokens: 6 us, and 18 as sort, sums and join)
 // Each workgroup reads all tokens. A group (of whole waves) has token i; if no earlier
-// one is of its word, it sums the word's rows. Workgroups from `token_blocks` on write the
-// rows of words that do not occur, kFewWords each.
+// one is of its word, it sums the word's rows. Of the dense gradient, workgroups from
+// `token_blocks` on write the rows of words that do not occur, kFewWords each.
 template <typename O, typename R, bool LISTS>
 __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int token_blocks,
                                                     int rest_lg) {
   constexpr int E = vector_of_sums<O, R, LISTS>(), kParts = kFew / 64;
   __shared__ int32_t word_at[kFew];
   __shared__ int32_t distinct[LISTS ? kFew : 1];
-  __shared__ uint16_t absent[kFewWords];
+  __shared__ uint16_t absent[LISTS ? 1 : kFewWords];
   const int tid = threadIdx.x, lane = tid & 63, n = (int)A.n;
   int32_t mine = tid < n ? A.tokens[tid] : -1;
   if (mine < 0 || mine >= A.V) {
@@ -875,22 +864,23 @@ __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int tok
   int32_t tok[kParts];
 #pragma unroll
   for (int i = 0; i < kParts; ++i) tok[i] = word_at[i * 64 + lane];
-  if ((int)blockIdx.x >= token_blocks) {
-    const int64_t w0 = (int64_t)((int)blockIdx.x - token_blocks) * kFewWords;
-    uint32_t gone = 0u;  // words that do not occur
-    for (int w = 0; w < kFewWords; ++w) {
-      bool hit = false;
+  if constexpr (!LISTS) {
+    if ((int)blockIdx.x >= token_blocks) {
+      const int64_t w0 = (int64_t)((int)blockIdx.x - token_blocks) * kFewWords;
+      uint32_t gone = 0u;  // words that do not occur
+      for (int w = 0; w < kFewWords; ++w) {
+        bool hit = false;
 #pragma unroll
-      for (int i = 0; i < kParts; ++i) hit |= tok[i] == (int32_t)(w0 + w);
-      if (__ballot(hit) == 0ull && w0 + w < A.V) gone |= 1u << w;
+        for (int i = 0; i < kParts; ++i) hit |= tok[i] == (int32_t)(w0 + w);
+        if (__ballot(hit) == 0ull && w0 + w < A.V) gone |= 1u << w;
+      }
+      if (tid < kFewWords && ((gone >> tid) & 1u))
+        absent[__popc(gone & ((1u << tid) - 1u))] = (uint16_t)tid;
+      __syncthreads();
+      put_rest(A, absent, __popc(gone), w0, 0, rest_lg, (int)blockIdx.y, (int)gridDim.y);
+      return;
     }
-    if (tid < kFewWords && ((gone >> tid) & 1u))
-      absent[__popc(gone & ((1u << tid) - 1u))] = (uint16_t)tid;
-    __syncthreads();
-    put_rest(A, absent, __popc(gone), w0, 0, rest_lg, (int)blockIdx.y, (int)gridDim.y);
-    return;
-  }
-  if constexpr (LISTS) {
+  } else {
     bool again = mine < 0;
     for (int j = 0; j < tid && !again; ++j) again = word_at[j] == mine;
     distinct[tid] = again ? 0x7FFFFFFF : mine;
@@ -1018,10 +1008,10 @@ hipError_t launch_embed_forward(const EmbedArgs& a, hipStream_t s) {
   by_types(a.dtype, a.out_dtype, [&](auto* t, auto* o) {
     using T = typename Pointee<decltype(t)>::type;
     using O = typename Pointee<decltype(o)>::type;
-    constexpr int E = vector_of<T, O>();
+    constexpr int E = vector_of<O>();
     const int lg = lg_threads(a.width, E);
     const dim3 one((unsigned)ceil_div(a.n, 256 >> lg), slices(a.width, E, lg));
-    k_embed_rows<T, O, 1><<<one, 256, 0, s>>>(a, lg);
+    k_embed_rows<T, O><<<one, 256, 0, s>>>(a, lg);
   });
   return hipGetLastError();
 }

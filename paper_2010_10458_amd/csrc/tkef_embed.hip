@@ -840,8 +840,14 @@ __global__ __launch_bounds__(NT) void k_embed_join(EmbedArgs A, EmbedScratch W, 
 // few tokens: one launch, no workspace
 
 constexpr int kFew = 256, kFewWords = 16, kFewAhead = 8;
+// Tokens up to which a list is made so. Its search for earlier equal words goes through LDS token
+// by token, 0.065 us each: of 32,000 x 515 binary32 10.7 us for 128 tokens, 14.9 for 192, 17.1 for
+// 224 and 18.9 for 256, as sort, sums and join 15.9, 17.2, 17.0 and 17.6; of 512 bfloat16 ->
+// binary16, 10.2, 14.5, 16.6 and 18.4 against 13.3, 14.2, 14.1 and 14.7. (The dense gradient, which
+// has no such search: 13.9 us for 256 tokens, 23.2 as sort, sums and join for 257.)
+constexpr int kFewList = 224;
 
-// (a list of 37 tokens: 6 us, and 18 as sort, sums and join)
+// (a list of 37 tokens: 5.5 us, and 18 as sort, sums and join)
 // Each workgroup reads all tokens. A group (of whole waves) has token i; if no earlier
 // one is of its word, it sums the word's rows. Of the dense gradient, workgroups from
 // `token_blocks` on write the rows of words that do not occur, kFewWords each.
@@ -1023,7 +1029,7 @@ void launch_sums(const EmbedArgs& a, void* ws, int rest_lg, hipStream_t s) {
   constexpr int E = vector_of_sums<O, R, LISTS>();
   int lg = lg_threads(a.width, E);
   const unsigned cut = slices(a.width, E, lg);
-  if (a.n <= kFew) {
+  if (a.n <= (LISTS ? kFewList : kFew)) {
     lg = lg < 6 ? 6 : lg;  // whole waves
     const int64_t tokens = LISTS && a.n == 0 ? 1 : (a.n + (kFew >> lg) - 1) / (kFew >> lg);
     const int64_t rest = rest_lg < 0 ? 0 : ceil_div(a.V, kFewWords);

@@ -117,6 +117,14 @@ def test_exact_sums_rounded_to_16_bits(n, vocab, width, dtype, grad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [192, 223, 224, 225, 256, 257])
+def test_few_tokens_in_one_launch_and_in_three(n, kind):
+    for vocab, width in ((150, 33), (32000, 515), (131073, 64)):
+        check(n, vocab, width, "bf16", kind, "f32")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [7, 256, 257, 3000, 17000])
 def test_the_widest_rows(n):
     check(n, 40, 1 << 16, "bf16", "law", "f32")

@@ -391,7 +391,8 @@ __global__ __launch_bounds__(kSplitThreads) void k_embed_split(EmbedArgs A, Embe
 // PIECES: its tokens lie in the pieces that k_embed_split made; else all tokens are read.
 // Without rows to write 1,000 tokens take 6 us, 8,192 11 us, a chain of barriers and LDS; the
 // 66 MB of zeros of 32,000 x 512 hide behind it but for 5 us. The 131,071 x 1,000 rows beside
-// 65,536 tokens are written at 4.9 TB/s, and copied at 4.8 TB/s read and written.
+// 65,536 tokens are written at 4.9 TB/s, and copied at 4.8 TB/s read and written. (PIECES: 8 of its
+// registers lie in scratch, 36 bytes a thread, so that two workgroups of 1,024 share a compute unit.)
 // NT: 256 threads for up to 2,048 tokens (1,000: 6.4 us, 8.6 with 1,024 threads).
 template <bool PIECES, int NT>
 __global__ __launch_bounds__(NT, 8) void k_embed_sort(EmbedArgs A, EmbedScratch W, Bins B,
@@ -601,12 +602,14 @@ constexpr int kAhead = 8, kWaveAhead = 16;  // rows of a tile under way
 // Group g sums the sorted tokens [g tile, (g + 1) tile). A word that lies within them is
 // done; the sums of one that began before them, and of one that goes on behind them, are
 // left for k_embed_join.
-// WAVE: groups of whole waves. Lane l reads the tile's token l - 1, beside the number of tokens, and
-// hands it on in a scalar register: one access and one address for a row, and a branch where
+// WAVE: groups of whole waves. Lane l reads the tile's token l - 1, beside the number of tokens,
+// and hands it on in a scalar register: one access and one address for a row, and a branch where
 // the word changes.
-// A tile is a chain of the tokens, their rows and the results, so it is short and all its rows
-// are under way together: 8,192 rows of 512 bfloat16 take 6.7 us. 57,344 of 1,000 with another
-// gradient's rows added take 70 us, 4 TB/s of rows that lie apart.
+// A tile is a chain of the tokens, their rows and the results, so it is short: 16 tokens up to
+// 65,536 of them, whose rows are under way together (groups of whole waves; others 8 at a time),
+// and 32 to 256 beyond, so that the joins have at most 4,096 tiles. 8,192 rows of 512 bfloat16 take
+// 6.7 us. 57,344 of 1,000 with another gradient's rows added take 70 us, 4 TB/s of rows that lie
+// apart.
 template <typename O, typename R, bool LISTS, bool WAVE>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedArgs A, EmbedScratch W, Bins B, int lg,
                                                    int tile) {
@@ -764,10 +767,10 @@ __device__ __forceinline__ void join_terms(const float* partial, int width, int 
 // workgroups of a window (gridDim.z) look at its 64 tiles; each group takes one of the words of
 // few tiles. Longer ones a workgroup takes together: its groups have equal parts of the
 // tiles, which the first joins. A chain as well: 5 us for 8,192 tokens of 512 columns, 13 us for
-// 57,344 of 1,000, whose most frequent word has 123 tiles. (NT: 256 threads where batches are not split,
-// else 1,024: 65,536 tokens of 1,000 x 512 take 10 us with 1,024, 14 with 512, 24 with 256; the call of
-// 8,192 tokens takes 27.8 us with 1,024, 26.9 with 256. There a word of three tiles is better shared by
-// a workgroup's groups: 27.0 us, and 28.6 where a group takes up to eight.)
+// 57,344 of 1,000, whose most frequent word has 123 tiles. (NT: 256 threads where batches are not
+// split, else 1,024: 65,536 tokens of 1,000 x 512 take 10 us with 1,024, 14 with 512, 24 with 256;
+// the call of 8,192 tokens takes 27.8 us with 1,024, 26.9 with 256. There a word of three tiles is
+// better shared by a workgroup's groups: 27.0 us, and 28.6 where a group takes up to eight.)
 constexpr int kWindow = 64;
 template <typename R, bool LISTS, int NT>
 __global__ __launch_bounds__(NT) void k_embed_join(EmbedArgs A, EmbedScratch W, Bins B, int lg,
@@ -905,7 +908,8 @@ __global__ __launch_bounds__(kFew) void k_embed_few(EmbedArgs A, int lg, int tok
   };
   if constexpr (LISTS) {
     const int all = below(0x7FFFFFFF);
-    if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *A.nnz = (int32_t)((uint32_t)all * (uint32_t)A.width);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && tid == 0)
+      *A.nnz = (int32_t)((uint32_t)all * (uint32_t)A.width);
   }
   if (word < 0) return;
   const int number = below(word);

@@ -311,8 +311,8 @@ __device__ __forceinline__ void select(uint4 (&r)[NV], float m, const Share<T, 2
 
 // One workgroup takes a row, or one of a row's chunks (PART, blockIdx.y), and holds it
 // in registers: NV vectors a thread, loaded once. Reads bound it: 8,192 x 32,000 bfloat16 (an eighth
-// without a token) in 72 us, 6.3 TB/s; 509 x 131,071 binary32 in chunks in 43 us, 6.2 TB/s. With
-// alternatives, 2,048 x 131,071 binary16 and k = 5 in 91 us, 5.5 TB/s: the selection's chain is
+// without a token) in 73 us, 6.3 TB/s; 509 x 131,071 binary32 in chunks in 43 us, 6.2 TB/s. With
+// alternatives, 2,048 x 131,071 binary16 and k = 5 in 92 us, 5.5 TB/s: the selection's chain is
 // hidden by three other workgroups of a compute unit. One row of 32,000 takes 5.8 us without, 8.1 with
 // one and 9.4 with twenty of them; 1,024 threads for such a row: 5.5 and 9.3 us.
 template <typename T, int TPB, int NV, bool ALT, bool PART>
